@@ -304,6 +304,68 @@ iflow_status_t iflow_rope_append(uint16_t *q, const uint16_t *k_new, const uint1
                                  int head_dim, int64_t position, int64_t max_seq, float base, iflow_rope_pairing_t pair_mode,
                                  uint16_t *k_cache, uint16_t *v_cache, void *stream);
 
+/* A key/value cache held in 4 or 8 bits, in pages: Table 3's blocks (Q4_B32, Q4_B64, Q8_B32, Q8_B64), along the components of a head.  A block of a key or
+ * a value is quantized as iflow_quantize quantizes a block of a row and stands for what iflow_dequant makes of it, fp16(level * scale + offset).
+ * A page holds `page_positions` consecutive positions of ONE sequence, for all key/value heads; a pool of n_pages pages is one array, and a sequence's pages lie anywhere in it.
+ *   page  = n_kv_heads x (page_positions / 32) tiles: head after head, tiles of 32 positions in order.
+ *   tile  = [key codes][value codes][key headers][value headers], D = head_dim, w = 4 or 8 bits, B = the format's block:
+ *     codes    32 D w / 8 bytes of either, as 16-byte pieces [n][g: 4][i: 16].  The pieces n = 0, 1, .. of one (g, i) are one run of 32-bit words:
+ *              keys: for h = 0, 1 the components g D/4 .. (g + 1) D/4 - 1 of position 16 h + i; values: for c = 0 .. D/16 - 1 component 16 c + i of the
+ *              positions 4g .. 4g + 3, 16 + 4g .. 16 + 4g + 3.  8 bits: four levels in a word, in order.  4 bits: eight, v0 v2 v4 v6 v1 v3 v5 v7 from the least significant.
+ *     headers  keys: [block][i][h], pairs scale, offset (fp16) of position 16 h + i; values: [block][g], the eight scales and then the eight offsets of the
+ *              positions of g in the order above.
+ *   (Every 16-byte piece, and every run, is what a lane of the attention's matrix instructions takes.)
+ *   144 bytes per position and head at 4 bits in blocks of 64 with 128 components, where fp16 takes 512.
+ *
+ * iflow_kv_batch_t says which positions a call is about.  Sequence b has n_b = first_token[b + 1] - first_token[b] tokens in this call, rows first_token[b] .. of the call's
+ * arrays, and they are its last: with seq_lens[b] the number of its positions, these included, token i of the sequence is position seq_lens[b] - n_b + i.  first_token null: one
+ * token each, row b.  Position p lies in page page_table[b][p / page_positions]; page_table null: sequence b's pages are b * max_pages, b * max_pages + 1, ..
+ *   The three arrays are int32, on the device, and read when the kernels run, so that a captured graph serves other lengths and pages.  What they hold cannot lead a kernel out of the
+ *   caller's buffers: rows outside 0 .. n_tokens - 1, tokens of a sequence past max_tokens and positions outside 0 .. max_seq - 1 are left out; a page outside 0 .. n_pages - 1 is
+ *   not there: nothing is written to it, it reads back as zeros, attention passes its positions over.  Rows of no token are left as they were; of a row that
+ *   two sequences claim, it is unspecified whose it becomes.
+ *   Two sequences of one iflow_kv_append call must not share the page that either of them writes to (what they write there is unspecified); pages that are only read may be shared.
+ * Values are assumed finite, and so is what they stand for.  Sizes: head_dim 64 or 128; 1 <= n_kv_heads <= 64; page_positions a multiple of 32, at most 2^20; 1 <= n_pages < 2^31, at most 2^46 bytes;
+ * 1 <= n_seqs <= 65536; 1 <= max_tokens <= max_seq <= max_pages * page_positions, max_seq <= 2^20; 1 <= n_tokens <= 2^24. */
+typedef struct iflow_kv_cache_t {
+    iflow_format_t format;
+    int32_t n_kv_heads, head_dim, page_positions;
+    int64_t n_pages;
+    void *pages;                    /* device, iflow_kv_cache_bytes() bytes */
+} iflow_kv_cache_t;
+typedef struct iflow_kv_batch_t {
+    int32_t n_seqs, max_pages;      /* max_pages: entries of a row of page_table */
+    const int32_t *page_table;      /* device [n_seqs][max_pages], or null */
+    const int32_t *seq_lens;        /* device [n_seqs] */
+    const int32_t *first_token;     /* device [n_seqs + 1], or null (then n_tokens >= n_seqs, max_tokens = 1) */
+    int64_t n_tokens;               /* rows of the call's arrays */
+    int32_t max_tokens, max_seq;    /* no sequence has more tokens in this call, or more positions */
+} iflow_kv_batch_t;
+/* Bytes of the pages (`pages` is not read). */
+iflow_status_t iflow_kv_cache_bytes(const iflow_kv_cache_t *cache, size_t *bytes);
+
+/* iflow_rope_append for a batch and this cache: every token's queries and keys are rotated by its position (angles, sines and rotation in fp64, rounded to fp16 once), keys and
+ * values are quantized into its sequence's page.  No other position's code or header changes.
+ *   q, q_out [n_tokens][n_heads][head_dim] fp16 (q_out may be q: in place; otherwise they must not overlap), k_new, v_new [n_tokens][n_kv_heads][head_dim] fp16
+ *   n_heads 1 .. 512, a multiple of n_kv_heads; base and pair_mode as for iflow_rope_append.  A token without a position keeps its row of q_out. */
+iflow_status_t iflow_kv_append(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new, int n_heads,
+                               float base, iflow_rope_pairing_t pair_mode, uint16_t *q_out, void *stream);
+
+/* What the cache stands for: keys and values of the batch's tokens, k_out, v_out [n_tokens][n_kv_heads][head_dim] fp16.  (A whole sequence: n_b = seq_lens[b].) */
+iflow_status_t iflow_kv_read(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, uint16_t *k_out, uint16_t *v_out, void *stream);
+
+/* Grouped-query attention of the batch's tokens over the cache, causal: with K, V what iflow_kv_read gives, token i of sequence b, at position p, and query head h
+ *   out = fp16( sum_{t <= p} softmax_t(scale * q . K[j][t]) V[j][t] ),   j = h / (n_heads / n_kv_heads),
+ * zeros where it sees no position.  The tokens' own keys and values are in the cache already (iflow_kv_append first).  One token per sequence is a decode step, a few a check of drafted
+ * tokens, many a prompt or its next chunk.
+ *   q, out [n_tokens][n_heads][head_dim] fp16, not overlapping; n_heads as for iflow_kv_append; scale > 0.
+ *   workspace: device memory of iflow_kv_attn_workspace_bytes() bytes for this description, 16-byte aligned (null if that is 0): partial results of the position ranges, which mean
+ *   nothing before and after the call.  Calls that share one must be ordered.
+ * Sums, maxima and the output before its one rounding are fp32; sums are taken in a fixed order. */
+iflow_status_t iflow_kv_attn_workspace_bytes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, int n_heads, size_t *bytes);
+iflow_status_t iflow_kv_attn(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
 /* A whole decode step of a decoder stack in ONE launch (Section 5: Infer() = one pass over all layers for the step's token;
  * Section 2's module table for the LLaMA family: "rms" normalization, "rope" position embedding, "silu" activation with a gate;
  * section "Grouped-query attention").  Per layer, with h the layer's input [hidden]:

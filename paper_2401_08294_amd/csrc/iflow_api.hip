@@ -3,7 +3,7 @@
 // record of the last HIP error).
 #include <algorithm>
 
-#include "iflow_common.h"
+#include "iflow_kv.h"
 
 namespace {
 
@@ -362,6 +362,116 @@ iflow_status_t iflow_rope_append(uint16_t *q, const uint16_t *k_new, const uint1
     if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k_cache) || !aligned16(v_cache)) return IFLOW_ERR_ALIGN;
     return device_status(iflow::launch_rope_append(q, k_new, v_new, n_heads, n_kv_heads, head_dim, position, max_seq, (double)base, (int)pair_mode,
                                                    k_cache, v_cache, (hipStream_t)stream));
+}
+
+// ---- the quantized key/value cache -----------------------------------------------------------------------------------------------
+
+static iflow_status_t kv_cache_shape(const iflow_kv_cache_t *c, int64_t *page_bytes)
+{
+    if (!c) return IFLOW_ERR_NULL;
+    if (c->format != IFLOW_Q4_B32 && c->format != IFLOW_Q4_B64 && c->format != IFLOW_Q8_B32 && c->format != IFLOW_Q8_B64) return IFLOW_ERR_FORMAT;
+    if (c->head_dim != 64 && c->head_dim != 128) return IFLOW_ERR_SHAPE;
+    if (c->n_kv_heads < 1 || c->n_kv_heads > 64) return IFLOW_ERR_SHAPE;
+    if (c->page_positions < 32 || c->page_positions % 32 != 0 || c->page_positions > (1 << 20)) return IFLOW_ERR_SHAPE;
+    if (c->n_pages < 1 || c->n_pages >= (1LL << 31)) return IFLOW_ERR_SHAPE;
+    *page_bytes = (int64_t)c->n_kv_heads * (c->page_positions / 32) * iflow::kv_tile_bytes((int)c->format, c->head_dim);
+    return c->n_pages > (1LL << 46) / *page_bytes ? IFLOW_ERR_SHAPE : IFLOW_OK;
+}
+
+// the sizes of a cache and a batch, without their pointers; n_heads 0 where a call has no query heads
+static iflow_status_t kv_shapes(const iflow_kv_cache_t *c, const iflow_kv_batch_t *b, bool heads, int n_heads, iflow::KvView *v)
+{
+    int64_t page_bytes = 0;
+    const iflow_status_t st = kv_cache_shape(c, &page_bytes);
+    if (st != IFLOW_OK) return st;
+    if (!b) return IFLOW_ERR_NULL;
+    if (heads && (n_heads < 1 || n_heads > 512 || n_heads % c->n_kv_heads != 0)) return IFLOW_ERR_SHAPE;
+    if (b->n_seqs < 1 || b->n_seqs > 65536 || b->max_pages < 1) return IFLOW_ERR_SHAPE;
+    if (b->max_seq < 1 || b->max_seq > (1 << 20) || b->max_seq > (int64_t)b->max_pages * c->page_positions) return IFLOW_ERR_SHAPE;
+    if (b->max_tokens < 1 || b->max_tokens > b->max_seq || b->n_tokens < 1 || b->n_tokens > (1LL << 24)) return IFLOW_ERR_SHAPE;
+    if (!b->first_token && (b->max_tokens != 1 || b->n_tokens < b->n_seqs)) return IFLOW_ERR_SHAPE;
+    if (!b->page_table && (int64_t)b->n_seqs * b->max_pages > c->n_pages) return IFLOW_ERR_SHAPE;
+    *v = {static_cast<uint8_t *>(c->pages), b->page_table, b->seq_lens, b->first_token, c->n_pages, b->n_tokens, page_bytes,
+          b->n_seqs, b->max_pages, b->max_tokens, b->max_seq, c->n_kv_heads, c->page_positions / 32};
+    return IFLOW_OK;
+}
+
+static iflow_status_t kv_pointers(const iflow::KvView &v)
+{
+    if (!v.pages || !v.lens) return IFLOW_ERR_NULL;
+    if (!aligned16(v.pages) || !aligned16(v.lens) || !aligned16(v.table) || !aligned16(v.first)) return IFLOW_ERR_ALIGN;
+    return IFLOW_OK;
+}
+
+iflow_status_t iflow_kv_cache_bytes(const iflow_kv_cache_t *cache, size_t *bytes)
+{
+    int64_t page_bytes = 0;
+    if (!bytes) return IFLOW_ERR_NULL;
+    const iflow_status_t st = kv_cache_shape(cache, &page_bytes);
+    if (st != IFLOW_OK) return st;
+    *bytes = (size_t)cache->n_pages * (size_t)page_bytes;
+    return IFLOW_OK;
+}
+
+iflow_status_t iflow_kv_append(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new, int n_heads,
+                               float base, iflow_rope_pairing_t pair_mode, uint16_t *q_out, void *stream)
+{
+    iflow::KvView v;
+    iflow_status_t st = kv_shapes(cache, batch, true, n_heads, &v);
+    if (st != IFLOW_OK) return st;
+    if (!(base > 1.0f && base < 3.0e38f)) return IFLOW_ERR_SHAPE;
+    if (pair_mode != IFLOW_ROPE_ADJACENT && pair_mode != IFLOW_ROPE_HALVES) return IFLOW_ERR_SHAPE;
+    if (!q || !k_new || !v_new || !q_out) return IFLOW_ERR_NULL;
+    st = kv_pointers(v);
+    if (st != IFLOW_OK) return st;
+    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out)) return IFLOW_ERR_ALIGN;
+    const int64_t q_bytes = v.n_tokens * n_heads * cache->head_dim * 2, kv_bytes = v.n_tokens * v.n_kv_heads * cache->head_dim * 2;
+    // rows are read and written by different workgroups: only a row in its own place is read before it is written
+    if (q_out != q && overlaps(q_out, q_bytes, q, q_bytes)) return IFLOW_ERR_SHAPE;
+    if (overlaps(q_out, q_bytes, k_new, kv_bytes) || overlaps(q_out, q_bytes, v_new, kv_bytes)) return IFLOW_ERR_SHAPE;
+    return device_status(iflow::launch_kv_append((int)cache->format, cache->head_dim, v, q, k_new, v_new, n_heads, (double)base, (int)pair_mode, q_out, (hipStream_t)stream));
+}
+
+iflow_status_t iflow_kv_read(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, uint16_t *k_out, uint16_t *v_out, void *stream)
+{
+    iflow::KvView v;
+    iflow_status_t st = kv_shapes(cache, batch, false, 0, &v);
+    if (st != IFLOW_OK) return st;
+    if (!k_out || !v_out) return IFLOW_ERR_NULL;
+    st = kv_pointers(v);
+    if (st != IFLOW_OK) return st;
+    if (!aligned16(k_out) || !aligned16(v_out)) return IFLOW_ERR_ALIGN;
+    const int64_t bytes = v.n_tokens * v.n_kv_heads * cache->head_dim * 2;
+    if (overlaps(k_out, bytes, v_out, bytes)) return IFLOW_ERR_SHAPE;
+    return device_status(iflow::launch_kv_read((int)cache->format, cache->head_dim, v, k_out, v_out, (hipStream_t)stream));
+}
+
+iflow_status_t iflow_kv_attn_workspace_bytes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, int n_heads, size_t *bytes)
+{
+    iflow::KvView v;
+    if (!bytes) return IFLOW_ERR_NULL;
+    const iflow_status_t st = kv_shapes(cache, batch, true, n_heads, &v);
+    if (st != IFLOW_OK) return st;
+    *bytes = iflow::kv_attn_workspace_bytes(v, cache->head_dim, n_heads);
+    return IFLOW_OK;
+}
+
+iflow_status_t iflow_kv_attn(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace,
+                             size_t workspace_bytes, void *stream)
+{
+    iflow::KvView v;
+    iflow_status_t st = kv_shapes(cache, batch, true, n_heads, &v);
+    if (st != IFLOW_OK) return st;
+    if (!(scale > 0.0f && scale < 3.0e38f)) return IFLOW_ERR_SHAPE;
+    const size_t need = iflow::kv_attn_workspace_bytes(v, cache->head_dim, n_heads);
+    if (!q || !out || (need && !workspace)) return IFLOW_ERR_NULL;
+    st = kv_pointers(v);
+    if (st != IFLOW_OK) return st;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return IFLOW_ERR_ALIGN;
+    if (workspace_bytes < need) return IFLOW_ERR_SIZE;
+    const int64_t bytes = v.n_tokens * n_heads * cache->head_dim * 2;
+    if (overlaps(out, bytes, q, bytes)) return IFLOW_ERR_SHAPE;
+    return device_status(iflow::launch_kv_attn((int)cache->format, cache->head_dim, v, q, n_heads, scale, out, workspace, (hipStream_t)stream));
 }
 
 // ---- the chained launch ---------------------------------------------------------------------------------------------

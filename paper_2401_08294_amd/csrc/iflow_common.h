@@ -231,6 +231,13 @@ hipError_t launch_attn_decode(const uint16_t *q, const uint16_t *k_cache, const 
                               int head_dim, int64_t seq_len, int64_t max_seq, float scale, uint16_t *out, void *workspace, hipStream_t s);
 hipError_t launch_attn_decode_static(const uint16_t *q, const uint16_t *k_cache, const uint16_t *v_cache, int n_heads, int n_kv_heads,
                                      int head_dim, int64_t seq_len, int64_t max_seq, float scale, uint16_t *out, hipStream_t s);
+struct KvView;                        // iflow_kv.h
+int kv_tile_bytes(int format, int head_dim);
+hipError_t launch_kv_append(int format, int head_dim, const KvView &v, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new, int n_heads, double base, int pair_mode,
+                            uint16_t *q_out, hipStream_t s);
+hipError_t launch_kv_read(int format, int head_dim, const KvView &v, uint16_t *k_out, uint16_t *v_out, hipStream_t s);
+size_t kv_attn_workspace_bytes(const KvView &v, int head_dim, int n_heads);
+hipError_t launch_kv_attn(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace, hipStream_t s);
 // ---- the chained launch: description of a chain (host arrays of the caller), plan builder, model, launcher ----
 struct ChainSpec {
     int format;                        // iflow_format_t

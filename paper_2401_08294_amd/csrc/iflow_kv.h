@@ -1,0 +1,128 @@
+// The quantized key/value cache: where its pages, tiles and codes lie, and how a code becomes an fp16 number.  Shared by the kernels that write the
+// cache, read it back and attend over it; the layout itself is stated in include/iflow.h.
+#pragma once
+
+#include "iflow_common.h"
+
+namespace iflow {
+
+constexpr int KV_TILE = 32;                                   // positions of a tile (first_tile() shifts by it)
+
+template <int BITS_, int BLOCK_, int D_>
+struct KvTile {
+    static constexpr int BITS = BITS_, BLOCK = BLOCK_, D = D_, L = (1 << BITS_) - 1;
+    static constexpr int NB = D / BLOCK;                      // blocks of a position
+    static constexpr int CODES = KV_TILE * D * BITS / 8;      // bytes of the keys' codes; the values have as many
+    static constexpr int PIECES = CODES / 1024;               // 16 bytes for each of 64 lanes
+    static constexpr int RUN = CODES / 256;                   // 32-bit words of a lane's run
+    static constexpr int HEADERS = KV_TILE * NB * 4;
+    static constexpr int V_AT = CODES, KH_AT = 2 * CODES, VH_AT = 2 * CODES + HEADERS, BYTES = 2 * (CODES + HEADERS);
+    static constexpr int PER_WORD = 32 / BITS;
+};
+
+// Host side: run fn(KvTile<..>{}) for a format and head dimension; hipErrorInvalidValue for one that a cache does not take.
+template <typename Fn>
+inline hipError_t for_kv_tile(int format, int head_dim, Fn fn)
+{
+    switch (format * 1000 + head_dim) {
+    case IFLOW_Q4_B32 * 1000 + 64: return fn(KvTile<4, 32, 64>{});
+    case IFLOW_Q4_B32 * 1000 + 128: return fn(KvTile<4, 32, 128>{});
+    case IFLOW_Q4_B64 * 1000 + 64: return fn(KvTile<4, 64, 64>{});
+    case IFLOW_Q4_B64 * 1000 + 128: return fn(KvTile<4, 64, 128>{});
+    case IFLOW_Q8_B32 * 1000 + 64: return fn(KvTile<8, 32, 64>{});
+    case IFLOW_Q8_B32 * 1000 + 128: return fn(KvTile<8, 32, 128>{});
+    case IFLOW_Q8_B64 * 1000 + 64: return fn(KvTile<8, 64, 64>{});
+    case IFLOW_Q8_B64 * 1000 + 128: return fn(KvTile<8, 64, 128>{});
+    default: return hipErrorInvalidValue;
+    }
+}
+
+// What a kernel knows of the cache and the batch (by value; every array is the caller's).
+struct KvView {
+    uint8_t *pages;
+    const int32_t *table, *lens, *first;                      // table, first: may be null
+    int64_t n_pages, n_tokens, page_bytes;
+    int32_t n_seqs, max_pages, max_tokens, max_seq, n_kv_heads, tiles_per_page;
+};
+
+// One sequence's new tokens as the kernels take them: rows row .. row + count - 1 of the batch's tokens at positions position .. .  Whatever the arrays
+// hold, what comes out of here stays inside the call's buffers: count at most max_tokens, and every token is asked for with has().
+struct KvSequence {
+    int64_t row, position, n_tokens;
+    int count, max_seq;
+    __device__ __forceinline__ KvSequence(const KvView &v, int b)
+    {
+        const int64_t at = v.first ? v.first[b] : b, n = v.first ? (int64_t)v.first[b + 1] - at : 1;
+        row = at; n_tokens = v.n_tokens; max_seq = v.max_seq;
+        position = (int64_t)v.lens[b] - n;
+        count = (int)max((int64_t)0, min(n, (int64_t)v.max_tokens));
+    }
+    // token i has a row, and a position that the cache has
+    __device__ __forceinline__ bool has_row(int64_t i) const { return i >= 0 && i < count && row + i >= 0 && row + i < n_tokens; }
+    __device__ __forceinline__ bool has(int64_t i) const { return has_row(i) && position + i >= 0 && position + i < max_seq; }
+    __device__ __forceinline__ int64_t first_tile() const { return position >> 5; }      // (rounded down, also below zero)
+    // positions that token i sees: its own and all before
+    __device__ __forceinline__ int sees(int i) const { return (int)max((int64_t)0, min(position + i + 1, (int64_t)max_seq)); }
+};
+
+// The tile that holds positions 32 t .. 32 t + 31 of sequence b; null where its page is none of the cache's.  (t < max_seq / 32, rounded up: inside the table's row.)
+__device__ __forceinline__ uint8_t *kv_tile_at(const KvView &v, int b, int kv_head, int t, int tile_bytes)
+{
+    const int p = t / v.tiles_per_page;
+    const int64_t entry = (int64_t)b * v.max_pages + p;
+    const int64_t page = v.table ? (int64_t)v.table[entry] : entry;
+    if (page < 0 || page >= v.n_pages) return nullptr;
+    return v.pages + page * v.page_bytes + ((int64_t)kv_head * v.tiles_per_page + (t - p * v.tiles_per_page)) * tile_bytes;
+}
+
+// ---- where an element lies in its tile ------------------------------------------------------------------------------------
+// key codes: 32-bit word that holds the first of PER_WORD consecutive components 'c' (a multiple of it) of position r
+template <typename T> __host__ __device__ constexpr int kv_key_word(int r, int c)
+{
+    const int g = c / (T::D / 4), at = (r >> 4) * (T::RUN / 2) + (c - g * (T::D / 4)) / T::PER_WORD;
+    return ((at >> 2) * 64 + g * 16 + (r & 15)) * 4 + (at & 3);
+}
+// value codes: the word that holds element k (a multiple of PER_WORD) of the eight positions of g, of component c
+template <typename T> __host__ __device__ constexpr int kv_value_word(int g, int k, int c)
+{
+    const int at = (c >> 4) * (8 / T::PER_WORD) + k / T::PER_WORD;
+    return ((at >> 2) * 64 + g * 16 + (c & 15)) * 4 + (at & 3);
+}
+__host__ __device__ constexpr int kv_value_position(int g, int k) { return (k >> 2) * 16 + 4 * g + (k & 3); }
+// headers, in 16-bit units from the tile's headers of keys or of values: the scale; the offset 1 (keys) or 8 (values) behind it
+__host__ __device__ constexpr int kv_key_header(int r, int block) { return ((block * 16 + (r & 15)) * 2 + (r >> 4)) * 2; }
+__host__ __device__ constexpr int kv_value_header(int r, int block) { return (block * 4 + ((r & 15) >> 2)) * 16 + (r >> 4) * 4 + (r & 3); }
+
+// ---- codes to fp16 ----------------------------------------------------------------------------------------------------------
+typedef uint32_t kv_u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t kv_u32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 kv_half8 __attribute__((ext_vector_type(8)));
+typedef float kv_float4 __attribute__((ext_vector_type(4)));
+struct KvPairs { half2_t p[4]; };                             // eight consecutive elements
+
+// the eight levels that begin at `word` (one word of nibbles, two of bytes) as fp16 numbers: or-ed into the mantissa of 1024 (64 for the nibbles four bits up), which is subtracted, exactly
+template <int BITS>
+__device__ __forceinline__ KvPairs kv_levels(const uint32_t *word)
+{
+    KvPairs v;
+    if constexpr (BITS == 4) {
+        const uint32_t w = word[0], w8 = w >> 8;
+        const half2_t b0 = {(half_t)1024.f, (half_t)1024.f}, b4 = {(half_t)64.f, (half_t)64.f};
+        v.p[0] = as_h2((w & 0x000F000Fu) | 0x64006400u) - b0;
+        v.p[1] = as_h2((w & 0x00F000F0u) | 0x54005400u) - b4;
+        v.p[2] = as_h2((w8 & 0x000F000Fu) | 0x64006400u) - b0;
+        v.p[3] = as_h2((w8 & 0x00F000F0u) | 0x54005400u) - b4;
+    } else {
+        const half2_t b0 = {(half_t)1024.f, (half_t)1024.f};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            v.p[2 * i] = as_h2(__builtin_amdgcn_perm(0x64646464u, word[i], 0x04010400u)) - b0;
+            v.p[2 * i + 1] = as_h2(__builtin_amdgcn_perm(0x64646464u, word[i], 0x04030402u)) - b0;
+        }
+    }
+    return v;
+}
+// level * scale + offset, rounded once: what iflow_dequant makes of the same three numbers
+__device__ __forceinline__ half2_t kv_value(half2_t level, half2_t scale, half2_t offset) { return __builtin_elementwise_fma(level, scale, offset); }
+
+}  // namespace iflow

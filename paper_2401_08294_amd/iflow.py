@@ -49,6 +49,17 @@ class DecodeStack(C.Structure):
                 ("scratch", C.c_void_p)]
 
 
+class KvCache(C.Structure):
+    """iflow_kv_cache_t: a pool of pages that holds keys and values in 4 or 8 bits."""
+    _fields_ = [("format", C.c_int), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_positions", C.c_int32), ("n_pages", C.c_int64), ("pages", C.c_void_p)]
+
+
+class KvBatch(C.Structure):
+    """iflow_kv_batch_t: the tokens that a call is about, and where their sequences' pages are."""
+    _fields_ = [("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("page_table", C.c_void_p), ("seq_lens", C.c_void_p), ("first_token", C.c_void_p),
+                ("n_tokens", C.c_int64), ("max_tokens", C.c_int32), ("max_seq", C.c_int32)]
+
+
 class IflowError(RuntimeError):
     def __init__(self, status: int, what: str):
         self.status = status
@@ -172,6 +183,12 @@ def lib():
         L.iflow_attn_decode.argtypes = [p, p, p, C.c_int, C.c_int, C.c_int, i64, i64, C.c_float, p, p, sz, p]
         L.iflow_attn_decode_static.argtypes = [p, p, p, C.c_int, C.c_int, C.c_int, i64, i64, C.c_float, p, p]
         L.iflow_rope_append.argtypes = [p, p, p, C.c_int, C.c_int, C.c_int, i64, i64, C.c_float, C.c_int, p, p, p]
+        cache, batch = C.POINTER(KvCache), C.POINTER(KvBatch)
+        L.iflow_kv_cache_bytes.argtypes = [cache, C.POINTER(sz)]
+        L.iflow_kv_append.argtypes = [cache, batch, p, p, p, C.c_int, C.c_float, C.c_int, p, p]
+        L.iflow_kv_read.argtypes = [cache, batch, p, p, p]
+        L.iflow_kv_attn_workspace_bytes.argtypes = [cache, batch, C.c_int, C.POINTER(sz)]
+        L.iflow_kv_attn.argtypes = [cache, batch, p, C.c_int, C.c_float, p, p, sz, p]
         L.iflow_qgemv_chain_workspace_bytes.argtypes = [C.c_int, C.POINTER(i64), C.POINTER(sz)]
         L.iflow_qgemv_chain_plan_bytes.argtypes = [C.c_int, C.c_int, C.POINTER(sz)]
         L.iflow_qgemv_chain_plan.argtypes = [C.c_int, C.c_int, C.POINTER(C.c_int), C.POINTER(i64), C.POINTER(p), C.POINTER(p),
@@ -355,6 +372,50 @@ def rope_append(q, k_new, v_new, n_heads: int, n_kv_heads: int, head_dim: int, p
     of the caches [n_kv_heads][max_seq][head_dim]."""
     _check((_native or _calls()).rope_append(q, k_new, v_new, n_heads, n_kv_heads, head_dim, position, max_seq, base, pair_mode, k_cache, v_cache,
                                              _stream(stream)), "iflow_rope_append")
+
+
+def kv_cache(fmt: int, n_kv_heads: int, head_dim: int, page_positions: int, n_pages: int, pages=None) -> KvCache:
+    """Describes a quantized key/value cache: `pages` (a device tensor of kv_cache_bytes() bytes, which the description keeps) holds n_pages pages of page_positions positions of all
+    key/value heads.  For a size query `pages` may be left out."""
+    d = KvCache(fmt, n_kv_heads, head_dim, page_positions, n_pages, _ptr(pages))
+    d._keep = pages
+    return d
+
+
+def kv_batch(n_seqs: int, max_pages: int, page_table, seq_lens, max_seq: int, first_token=None, n_tokens=None, max_tokens: int = 1) -> KvBatch:
+    """Describes the tokens of a call: int32 device tensors page_table [n_seqs][max_pages] (None: sequence b's pages are b * max_pages ..), seq_lens [n_seqs], and, unless every
+    sequence has one token, first_token [n_seqs + 1].  The description keeps the tensors; their contents are read when a call's kernels run."""
+    d = KvBatch(n_seqs, max_pages, _ptr(page_table), _ptr(seq_lens), _ptr(first_token), n_seqs if n_tokens is None else n_tokens, max_tokens, max_seq)
+    d._keep = (page_table, seq_lens, first_token)
+    return d
+
+
+def kv_cache_bytes(cache: KvCache) -> int:
+    out = C.c_size_t(0)
+    _check(lib().iflow_kv_cache_bytes(C.byref(cache), C.byref(out)), "iflow_kv_cache_bytes")
+    return int(out.value)
+
+
+def kv_append(cache: KvCache, batch: KvBatch, q, k_new, v_new, n_heads: int, base: float, pair_mode: int, q_out, stream=None) -> None:
+    """Rotary position embedding of the batch's tokens: q [n_tokens][n_heads][head_dim] rotated into q_out (or q itself), rotated k_new and v_new [n_tokens][n_kv_heads][head_dim]
+    quantized into the cache."""
+    _check(lib().iflow_kv_append(C.byref(cache), C.byref(batch), _ptr(q), _ptr(k_new), _ptr(v_new), n_heads, base, pair_mode, _ptr(q_out), _stream(stream)), "iflow_kv_append")
+
+
+def kv_read(cache: KvCache, batch: KvBatch, k_out, v_out, stream=None) -> None:
+    """The keys and values of the batch's tokens as the cache holds them, fp16 [n_tokens][n_kv_heads][head_dim]."""
+    _check(lib().iflow_kv_read(C.byref(cache), C.byref(batch), _ptr(k_out), _ptr(v_out), _stream(stream)), "iflow_kv_read")
+
+
+def kv_attn_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().iflow_kv_attn_workspace_bytes(C.byref(cache), C.byref(batch), n_heads, C.byref(out)), "iflow_kv_attn_workspace_bytes")
+    return int(out.value)
+
+
+def kv_attn(cache: KvCache, batch: KvBatch, q, n_heads: int, scale: float, out, workspace, workspace_bytes: int, stream=None) -> None:
+    """Causal grouped-query attention of the batch's tokens, q [n_tokens][n_heads][head_dim], over their sequences' cached positions."""
+    _check(lib().iflow_kv_attn(C.byref(cache), C.byref(batch), _ptr(q), n_heads, scale, _ptr(out), _ptr(workspace), workspace_bytes, _stream(stream)), "iflow_kv_attn")
 
 
 def qgemv_chain_workspace_bytes(rows_list) -> int:

@@ -1,0 +1,355 @@
+"""GPU parity of the quantized key/value cache (iflow_kv_append, iflow_kv_read, iflow_kv_attn) against oracle/kv_cache.py, through the C ABI.
+
+Append and read: bit for bit, the whole pool of pages compared, so that a code or header outside the batch's positions that changed fails too.  (Rotated values are fp16 roundings of
+fp64 results; two fp64 evaluations differ by 1e-15 relative and would round apart once in 10^11 values.)
+Attention: against fp64, relative to the larger of the value and its row's rms.  The output's rounding is 2^-11 of the value at most.  Where many tokens share a pass the
+probabilities are rounded to fp16 once: each product of a sum is off by at most 2^-11 of itself, by 2^-11 / sqrt(12) in the root mean square, and the sum, of independent
+terms, by that of its own rms: six of these are 1.7 x 2^-11.  Together 2.8 x 2^-11 = 1.4e-3; fp32 sums and exponentials add 1e-5.  TOL = 2e-3, the products' tolerance.
+"""
+import numpy as np
+import pytest
+
+from paper_2401_08294_amd import synth
+from test_gpu_parity import TOL, gpu, say  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+FORMATS = ["Q4_B32", "Q4_B64", "Q8_B32", "Q8_B64"]
+BASE = 10000.0
+
+
+class Setup:
+    """A pool, page table and batch on the host (for the oracle) and on the device."""
+
+    def __init__(self, gpu, name, n_kv, d, page, lens, counts, seed, n_heads, max_seq=None, max_tokens=None, max_pages=None, spare_pages=2, first=None, n_tokens=None):
+        from oracle import kv_cache, oracle
+        self.torch, self.iflow = gpu
+        torch, iflow = gpu
+        self.fmt, self.n_kv, self.d, self.page, self.n_heads = iflow.FORMATS[name], n_kv, d, page, n_heads
+        self.rng = rng = np.random.default_rng(synth.BASE_SEED + seed)
+        self.lens = np.array(lens, np.int32)
+        self.single = counts is None
+        counts = [1] * len(lens) if counts is None else counts
+        self.first = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32) if first is None else np.array(first, np.int32)
+        self.max_seq = max(1, int(self.lens.max())) if max_seq is None else max_seq
+        self.max_tokens = max(1, max(counts)) if max_tokens is None else max_tokens
+        self.max_pages = -(-self.max_seq // page) if max_pages is None else max_pages
+        self.n_tokens = max(1, int(self.first.max())) if n_tokens is None else n_tokens
+        n_pages = len(lens) * self.max_pages + spare_pages
+        self.table = rng.permutation(n_pages)[:len(lens) * self.max_pages].reshape(len(lens), -1).astype(np.int32)
+        tile = kv_cache.tile_bytes(self.fmt, d)
+        # what nobody has written: any bytes, headers that are no numbers among them
+        self.pages = rng.integers(0, 256, (n_pages, n_kv * (page // 32) * tile), np.uint8)
+        self.cache = kv_cache.Cache(self.fmt, n_kv, d, page, self.pages)
+        self.oracle, self.kv_cache = oracle, kv_cache
+
+    def fill(self, upto=None):
+        """Keys and values for every position (of the first `upto` of each sequence), through the oracle."""
+        upto = self.lens if upto is None else upto
+        for b, n in enumerate(upto):
+            k, v = self.values(max(0, int(n)))
+            for p in range(max(0, int(n))):
+                self.cache.store(self.table[b], p, k[p], v[p])
+
+    def values(self, n):
+        channel = 1.0 + 4.0 * (self.rng.random((self.n_kv, self.d)) < 0.04)
+        k = (self.rng.standard_normal((n, self.n_kv, self.d)) * channel).astype(np.float16)
+        return k.view(np.uint16), self.rng.standard_normal((n, self.n_kv, self.d)).astype(np.float16).view(np.uint16)
+
+    def queries(self, scale=1.0):
+        return (scale * self.rng.standard_normal((self.n_tokens, self.n_heads, self.d))).astype(np.float16).view(np.uint16)
+
+    def dev(self, a):
+        a = np.ascontiguousarray(a)
+        return self.torch.from_numpy(a.view(np.int16) if a.dtype == np.uint16 else a).cuda()
+
+    def describe(self, table=True):
+        it = self.iflow
+        self.d_pages, self.d_table, self.d_lens, self.d_first = self.dev(self.pages), self.dev(self.table), self.dev(self.lens), self.dev(self.first)
+        self.d_cache = it.kv_cache(self.fmt, self.n_kv, self.d, self.page, self.pages.shape[0], self.d_pages)
+        assert it.kv_cache_bytes(self.d_cache) == self.pages.size
+        self.d_batch = it.kv_batch(len(self.lens), self.max_pages, self.d_table if table else None, self.d_lens, self.max_seq, None if self.single else self.d_first, self.n_tokens,
+                                   self.max_tokens)
+        return self.d_cache, self.d_batch
+
+    def args(self):
+        return self.table, self.lens, None if self.single else self.first, self.max_tokens, self.max_seq
+
+    def attend(self, q, scale, out=None, ws=None):
+        torch, it = self.torch, self.iflow
+        need = it.kv_attn_workspace_bytes(self.d_cache, self.d_batch, self.n_heads)
+        if ws is None:
+            ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+        out = torch.full((self.n_tokens, self.n_heads, self.d), 7.0, dtype=torch.float16, device="cuda") if out is None else out
+        it.kv_attn(self.d_cache, self.d_batch, self.dev(q), self.n_heads, scale, out, ws, need)
+        torch.cuda.synchronize()
+        return out.cpu().numpy().astype(np.float64)
+
+    def check_attend(self, q, scale, tol=TOL, rows=slice(None)):
+        want = np.full((self.n_tokens, self.n_heads, self.d), 7.0)
+        self.kv_cache.attend(self.cache, *self.args(), q, scale, want)
+        got, want = self.attend(q, scale)[rows], want[rows]
+        rms = np.sqrt(np.mean(want ** 2, axis=-1, keepdims=True))
+        e = np.abs(got - want) / np.maximum(np.abs(want), np.maximum(rms, 1e-30))
+        assert np.isfinite(got).all() and e.max() <= tol, (float(e.max()), np.unravel_index(e.argmax(), e.shape))
+        say(f"        max rel err {e.max():.2e}")
+        return float(e.max())
+
+
+def append_and_compare(s, mode, in_place=False, rows=slice(None)):
+    torch, it = s.torch, s.iflow
+    s.describe()
+    k, v = s.values(s.n_tokens)
+    q = s.queries()
+    qd = s.dev(q)
+    q_out = qd if in_place else torch.full((s.n_tokens, s.n_heads, s.d), 7.0, dtype=torch.float16, device="cuda")
+    it.kv_append(s.d_cache, s.d_batch, qd, s.dev(k), s.dev(v), s.n_heads, BASE, mode, q_out)
+    torch.cuda.synchronize()
+    want = q.copy() if in_place else np.full(q.shape, np.float16(7.0).view(np.uint16))
+    s.kv_cache.append(s.cache, *s.args(), q, k, v, BASE, mode, want)
+    assert np.array_equal(q_out.cpu().numpy().view(np.uint16).reshape(want.shape), want), "rotated queries differ"
+    got = s.d_pages.cpu().numpy()
+    assert np.array_equal(got, s.pages), f"{int((got != s.pages).sum())} bytes of the pages differ"
+    k_out, v_out = [torch.full((s.n_tokens, s.n_kv, s.d), 7.0, dtype=torch.float16, device="cuda") for _ in range(2)]
+    it.kv_read(s.d_cache, s.d_batch, k_out, v_out)
+    torch.cuda.synchronize()
+    k_want, v_want = [np.full(k.shape, np.float16(7.0).view(np.uint16)) for _ in range(2)]
+    s.kv_cache.read(s.cache, *s.args(), k_want, v_want)
+    assert np.array_equal(k_out.cpu().numpy().view(np.uint16)[rows], k_want[rows]), "keys read back differ"
+    assert np.array_equal(v_out.cpu().numpy().view(np.uint16)[rows], v_want[rows]), "values read back differ"
+
+
+@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("name", FORMATS)
+def test_append_and_read(gpu, name, d, mode):  # noqa: F811
+    """Prompts that begin and end anywhere in a tile and a page, one token, none; then one token each, by the form without first_token."""
+    say(f"[case] kv append + read {name} head_dim={d} pairing={mode}")
+    lens, counts = [1, 40, 64, 131, 33, 96, 200], [1, 9, 64, 70, 0, 1, 33]
+    append_and_compare(Setup(gpu, name, 2, d, 64, lens, counts, 3000 + d + mode, 6), mode)
+    append_and_compare(Setup(gpu, name, 3, d, 32, [1, 2, 31, 32, 33, 64, 65, 100], None, 3100 + d + mode, 3), mode, in_place=True)
+
+
+@pytest.mark.parametrize("name,n_kv,n_heads,d,page,lens,counts", [("Q4_B64", 8, 64, 128, 256, [700], [700]), ("Q4_B64", 1, 71, 64, 32, [300, 5], [1, 2]), ("Q8_B32", 32, 32, 128, 96, [333, 95], [100, 95]),
+                                                                 ("Q4_B32", 8, 32, 128, 128, [1000] * 70, None)])
+def test_append_head_counts(gpu, name, n_kv, n_heads, d, page, lens, counts):  # noqa: F811
+    say(f"[case] kv append {name} {n_heads}/{n_kv} heads, {len(lens)} sequences")
+    append_and_compare(Setup(gpu, name, n_kv, d, page, lens, counts, 3200 + n_heads, n_heads), 1)
+
+
+def test_append_far_positions_and_ties(gpu):  # noqa: F811
+    """Positions of hundreds of thousands (angles of 10^6 radians), and blocks that are constant, zero, of few values: a scale of zero, levels at ties."""
+    say("[case] kv append at far positions")
+    s = Setup(gpu, "Q4_B64", 2, 128, 1 << 15, [1 << 20, 777777], [2, 3], 3300, 2, max_seq=1 << 20, max_pages=32, spare_pages=-60)
+    s.table = np.array([[0] * 31 + [1], [0] * 23 + [2] + [0] * 8], np.int32)       # (only the written pages matter)
+    append_and_compare(s, 1)
+    s = Setup(gpu, "Q4_B32", 2, 64, 32, [3, 30], [3, 20], 3301, 2)
+    values = s.values
+
+    def few(n):
+        k, v = values(n)
+        v = v.view(np.float16)
+        v[0::4] = 0.0
+        v[1::4] = -2.5
+        v[2::4] = np.round(v[2::4] * 2) / 2                    # (w - o) / s at and next to ties
+        return k, v.view(np.uint16)
+    s.values = few
+    append_and_compare(s, 0)
+
+
+def test_what_arrays_hold_cannot_lead_out(gpu):  # noqa: F811
+    """Rows and tokens that do not exist, lengths beyond the limit and below the number of tokens, pages that are none: left out, and everything else as it was."""
+    say("[case] kv: arrays that hold anything")
+    # sequence 0: rows beyond n_tokens; 1: more tokens than max_tokens; 2: fewer positions than tokens; 3: a length beyond max_seq; 4: length 0; 5: fine; 6: first_token falls; 7: a length below zero
+    first = [0, 3, 15, 20, 24, 25, 27, 26, 29]
+    s = Setup(gpu, "Q4_B64", 2, 128, 64, [50, 60, 3, 131, 0, 90, 40, -5], [3, 12, 5, 4, 1, 2, 0, 3], 3400, 4, max_seq=128, max_tokens=8, first=first, n_tokens=27)
+    s.fill([50, 60, 3, 128, 0, 90, 40, 0])
+    s.table[5, 0], s.table[0, 0], s.table[1, 1] = -1, s.pages.shape[0], 2 ** 31 - 1
+    rows = slice(0, 26)                                        # (row 26 is claimed by two sequences, and whose it is is nowhere said)
+    append_and_compare(s, 1, rows=rows)
+    s.check_attend(s.queries(), 128 ** -0.5, rows=rows)
+    s = Setup(gpu, "Q8_B64", 1, 64, 32, [70, 70], [70, 1], 3401, 2)
+    s.fill()
+    s.table[0] = -7                                            # nothing of it is there: zeros
+    s.describe()
+    got = s.attend(s.queries(), 0.125)
+    assert (got[:70] == 0).all() and np.isfinite(got).all()
+    s.check_attend(s.queries(), 0.125)
+
+
+@pytest.mark.parametrize("name", FORMATS)
+@pytest.mark.parametrize("n_heads,n_kv,d", [(4, 4, 128), (8, 1, 128), (17, 1, 64), (6, 2, 64), (71, 1, 64), (16, 2, 128)])
+def test_decode_attention(gpu, name, n_heads, n_kv, d):  # noqa: F811
+    """One token per sequence at lengths around a tile, a range and none; what lies behind them is no number."""
+    say(f"[case] kv decode attention {name} {n_heads}/{n_kv} heads of {d}")
+    s = Setup(gpu, name, n_kv, d, 96, [1, 2, 15, 16, 17, 31, 32, 33, 0, 63, 64, 65, 127, 129, 255, 257, 300, 513, 700], None, 3500 + n_heads, n_heads)
+    s.fill()
+    s.describe()
+    s.check_attend(s.queries(), d ** -0.5)
+
+
+@pytest.mark.parametrize("name,n_heads,n_kv,d,lens,counts", [("Q4_B64", 32, 8, 128, [300, 70, 9], [4, 3, 1]), ("Q4_B32", 71, 1, 64, [130, 64], [3, 4]), ("Q8_B32", 8, 8, 128, [100, 33], [7, 8]),
+                                                            ("Q4_B64", 8, 2, 128, [200], [200]), ("Q8_B64", 12, 4, 64, [150, 333, 40], [150, 100, 17]), ("Q4_B32", 16, 2, 128, [260, 31], [129, 31]),
+                                                            ("Q4_B64", 5, 5, 64, [400], [77]), ("Q8_B32", 6, 1, 128, [90, 0, 64], [64, 0, 64])])
+def test_attention_of_several_tokens(gpu, name, n_heads, n_kv, d, lens, counts):  # noqa: F811
+    """Drafts, chunks and whole prompts: token i sees its own position and those before."""
+    say(f"[case] kv attention {name} {n_heads}/{n_kv} heads of {d}, lengths {lens}, tokens {counts}")
+    s = Setup(gpu, name, n_kv, d, 64, lens, counts, 3600 + n_heads + d, n_heads)
+    s.fill()
+    s.describe()
+    s.check_attend(s.queries(), d ** -0.5)
+
+
+@pytest.mark.parametrize("counts", [None, [3], [150]])
+def test_attention_peaked_and_climbing_scores(gpu, counts):  # noqa: F811
+    """Large scores: one position outweighs the rest, wherever it is, and scores that climb by up to 40 (log2) from tile to tile, each head by another step: the reference follows in some
+    rows of a tile and not in others."""
+    n_kv, d, n_heads, n = 2, 64, 16, 900
+    s = Setup(gpu, "Q8_B32", n_kv, d, 64, [n], counts, 3700, n_heads)
+    s.fill()
+    s.describe()
+    say("[case] kv attention, peaked scores")
+    s.check_attend(s.queries(6.0), 0.5, tol=4e-3)              # (scores of several hundred, fp32: 3e-5 each; and their differences' part of probabilities)
+    for name, climb in (("tiles", np.arange(n) // 32), ("positions", np.arange(n) / 8.0), ("down", -(np.arange(n) // 32)), ("wavefronts", np.arange(n) // 128)):
+        say(f"[case] kv attention, climbing scores: {name}")
+        k, v = s.values(n)
+        k, q = k.view(np.float16), s.queries().view(np.float16)
+        k[:, :, :32] = 0.0                                     # a block of its own for what climbs
+        k[:, :, 0] = climb[:, None]
+        q[..., 1:32] = 0.0
+        q[..., 0] = np.resize([0.0, 6.0, 7.9, 8.0, 10.0, 14.9, 20.0, 40.0, -6.0, -20.0, 3.0], n_heads) * np.log(2.0) / 0.125 / max(1.0, np.abs(climb).max() / 30.0)
+        for p in range(n):
+            s.cache.store(s.table[0], p, k[p].view(np.uint16), v[p])
+        s.d_pages.copy_(s.dev(s.pages))
+        s.check_attend(q.view(np.uint16), 0.125)
+
+
+def test_attention_of_one_workspace_streams_and_graphs(gpu):  # noqa: F811
+    """A captured append and attention, replayed at other lengths, tokens and pages, with eager calls between; and calls of other shapes on the same workspace."""
+    torch, it = gpu
+    s = Setup(gpu, "Q4_B64", 4, 128, 64, [700, 65, 300], None, 3800, 16, max_seq=1024)
+    s.fill()
+    s.describe()
+    say("[case] kv append + attention under HIP-graph replay")
+    stream = torch.cuda.Stream()
+    need = it.kv_attn_workspace_bytes(s.d_cache, s.d_batch, 16)
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    q, (k, v) = s.queries(), s.values(3)
+    qd, kd, vd = s.dev(q), s.dev(k), s.dev(v)
+    q_rot, out = torch.zeros((3, 16, 128), dtype=torch.float16, device="cuda"), torch.zeros((3, 16, 128), dtype=torch.float16, device="cuda")
+
+    def step():
+        it.kv_append(s.d_cache, s.d_batch, qd, kd, vd, 16, BASE, 1, q_rot, stream=stream)
+        it.kv_attn(s.d_cache, s.d_batch, q_rot, 16, 128 ** -0.5, out, ws, need, stream=stream)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        step()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream), torch.cuda.graph(graph, stream=stream):
+        step()
+    s.pages[:] = s.d_pages.cpu().numpy()
+    for n, lens in enumerate(([701, 66, 301], [702, 67, 302], [10, 1000, 1], [1024, 0, 500])):
+        if n == 2:
+            s.fill([10, 1000, 1])
+            s.d_pages.copy_(s.dev(s.pages))
+        if n == 3:
+            s.table[0], s.table[1] = s.table[1].copy(), s.table[0].copy()
+            s.fill([1024, 0, 500])
+            s.d_pages.copy_(s.dev(s.pages))
+        s.lens = np.array(lens, np.int32)
+        q, (k, v) = s.queries(), s.values(3)
+        for d, a in ((qd, q), (kd, k), (vd, v), (s.d_lens, s.lens), (s.d_table, s.table)):
+            d.copy_(s.dev(a).view(d.dtype))
+        out.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want_q = q_rot.cpu().numpy().view(np.uint16).copy()
+        s.kv_cache.append(s.cache, *s.args(), q, k, v, BASE, 1, want_q)
+        assert np.array_equal(q_rot.cpu().numpy().view(np.uint16), want_q) and np.array_equal(s.d_pages.cpu().numpy(), s.pages)
+        want = np.full((3, 16, 128), 7.0)
+        s.kv_cache.attend(s.cache, *s.args(), want_q, 128 ** -0.5, want)
+        got = out.cpu().numpy().astype(np.float64)
+        rms = np.maximum(np.sqrt(np.mean(want ** 2, axis=-1, keepdims=True)), 1e-30)
+        assert (np.abs(got - want) / np.maximum(np.abs(want), rms)).max() <= TOL
+        eager = torch.full((3, 16, 128), 7.0, dtype=torch.float16, device="cuda")
+        it.kv_attn(s.d_cache, s.d_batch, q_rot, 16, 128 ** -0.5, eager, ws, need)
+        torch.cuda.synchronize()
+        assert torch.equal(eager, out)
+
+
+def test_steps_together(gpu):  # noqa: F811
+    """A program's life with the cache: two prompts in chunks, then decode steps with a drafted token now and then, one pool, pages handed out as sequences grow, a page of a common
+    prefix shared by a third sequence; every step's attention and the whole cache against the oracle."""
+    torch, it = gpu
+    n_kv, d, n_heads, page = 2, 128, 8, 32
+    lens, free = [0, 0], list(range(39, -1, -1))
+    s = Setup(gpu, "Q4_B64", n_kv, d, page, [320, 320], [1, 1], 3900, n_heads, max_pages=20, spare_pages=0)
+    s.table[:] = -1
+    s.max_seq = 640
+    steps = [[37, 0], [64, 50], [1, 1], [3, 1], [1, 4], [0, 33], [1, 1]]
+    for n, counts in enumerate(steps):
+        say(f"[case] kv step {n}: tokens {counts}")
+        lens = [a + c for a, c in zip(lens, counts)]
+        for b, length in enumerate(lens):
+            for i in range(-(-length // page)):
+                if s.table[b, i] < 0:
+                    s.table[b, i] = free.pop()
+        s.lens, s.first = np.array(lens, np.int32), np.array([0, counts[0], sum(counts)], np.int32)
+        s.n_tokens, s.max_tokens, s.single = sum(counts), max(counts), False
+        append_and_compare(s, 1)
+        s.check_attend(s.queries(), d ** -0.5)
+    # a third sequence shares the first one's two full pages and goes on by itself
+    s.table = np.concatenate([s.table, np.full((1, 20), -1, np.int32)])
+    s.table[2, :3] = s.table[0, 0], s.table[0, 1], free.pop()
+    s.lens, s.first = np.array(lens + [70], np.int32), np.array([0, 1, 2, 8], np.int32)
+    s.lens[:2] += 1
+    for b in (0, 1):
+        if s.table[b, (s.lens[b] - 1) // page] < 0:
+            s.table[b, (s.lens[b] - 1) // page] = free.pop()
+    s.n_tokens, s.max_tokens = 8, 6
+    append_and_compare(s, 1)
+    s.check_attend(s.queries(), d ** -0.5)
+
+
+def test_pages_beyond_32_bits(gpu):  # noqa: F811
+    """A pool of more than 4 GiB: a sequence in its last pages."""
+    torch, it = gpu
+    say("[case] kv cache above 2^32 bytes")
+    s = Setup(gpu, "Q4_B64", 2, 128, 64, [100, 130], [20, 1], 4000, 8)
+    s.fill([80, 129])
+    tile = s.kv_cache.tile_bytes(s.fmt, 128) * 2 * 2
+    n = (5 << 30) // tile
+    pool = torch.empty((n, tile), dtype=torch.uint8, device="cuda")
+    mark = pool[:8].clone()
+    low = s.pages.shape[0]
+    pool[n - low:] = s.dev(s.pages)
+    s.describe()
+    s.d_table += n - low
+    s.d_cache = it.kv_cache(s.fmt, 2, 128, 64, n, pool)
+    k, v = s.values(21)
+    q = s.queries()
+    q_out = torch.empty((21, 8, 128), dtype=torch.float16, device="cuda")
+    it.kv_append(s.d_cache, s.d_batch, s.dev(q), s.dev(k), s.dev(v), 8, BASE, 1, q_out)
+    want = np.zeros_like(q)
+    s.kv_cache.append(s.cache, *s.args(), q, k, v, BASE, 1, want)
+    torch.cuda.synchronize()
+    assert np.array_equal(pool[n - low:].cpu().numpy(), s.pages) and torch.equal(pool[:8], mark)
+    s.check_attend(want, 128 ** -0.5)
+
+
+def test_refusals_name_themselves(gpu):  # noqa: F811
+    torch, it = gpu
+    say("[case] kv refusals")
+    s = Setup(gpu, "Q4_B64", 2, 64, 32, [700, 40], None, 4100, 4)
+    s.describe()
+    q = s.dev(s.queries())
+    out = torch.zeros((2, 4, 64), dtype=torch.float16, device="cuda")
+    need = it.kv_attn_workspace_bytes(s.d_cache, s.d_batch, 4)
+    ws = torch.zeros((need,), dtype=torch.uint8, device="cuda")
+    for call, status in ((lambda: it.kv_attn(s.d_cache, s.d_batch, q, 4, 0.1, out, ws, need - 1), it.ERR_SIZE), (lambda: it.kv_attn(s.d_cache, s.d_batch, q, 3, 0.1, out, ws, need), it.ERR_SHAPE),
+                         (lambda: it.kv_attn(s.d_cache, s.d_batch, q, 4, 0.1, q, ws, need), it.ERR_SHAPE), (lambda: it.kv_append(s.d_cache, s.d_batch, q, out, q, 4, BASE, 1, out), it.ERR_SHAPE)):
+        with pytest.raises(it.IflowError) as info:
+            call()
+        assert info.value.status == status
