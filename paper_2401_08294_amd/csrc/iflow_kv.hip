@@ -3,100 +3,101 @@
 
 namespace iflow {
 
-// the block's extremes over the eight lanes of a position (or the four of a quad)
-template <bool EIGHT> __device__ __forceinline__ float kv_min(float v)
-{
-    v = fminf(v, dpp_f32<0xB1, 0xF>(v));
-    v = fminf(v, dpp_f32<0x4E, 0xF>(v));
-    if (EIGHT) v = fminf(v, dpp_f32<0x141, 0xF>(v));
-    return v;
-}
-template <bool EIGHT> __device__ __forceinline__ float kv_max(float v)
-{
-    v = fmaxf(v, dpp_f32<0xB1, 0xF>(v));
-    v = fmaxf(v, dpp_f32<0x4E, 0xF>(v));
-    if (EIGHT) v = fmaxf(v, dpp_f32<0x141, 0xF>(v));
-    return v;
-}
-
 // ---- append -------------------------------------------------------------------------------------------------------------------
-// One workgroup per sequence, tile of positions and key/value head or query heads.  Eight lanes share a position; a lane holds components
-// s D/16 .. of both halves of the head, so that the pairs of either pairing are its own.
-template <typename T>
-__global__ __launch_bounds__(256) void kv_append_kernel(KvView v, const uint16_t *q, const uint16_t *__restrict__ k_new, const uint16_t *__restrict__ v_new, int n_heads,
-                                                        double log2_base, int pair_mode, uint16_t *q_out, int tiles_per_seq)
-{
-    constexpr int D = T::D, H = D / 16;                       // H: components of either half that a lane holds
-    __shared__ uint8_t s_level[2][KV_TILE][D];
-    const int tid = threadIdx.x, r = tid >> 3, s = tid & 7;
-    const int b = blockIdx.x / tiles_per_seq;
-    const KvSequence seq(v, b);
-    const int64_t t = seq.first_tile() + (blockIdx.x - b * tiles_per_seq);
-    const int64_t token = t * KV_TILE + r - seq.position;
-    const bool mine = seq.has(token);
-    const int64_t row = seq.row + token;
+// Eight lanes share a position of a head; lane s holds components s D/16 .. (s + 1) D/16 - 1 of both halves of the head, so that the pairs of either pairing, and a word of key codes (half
+// of one at 64 components in 4 bits), are its own.
+template <typename T> constexpr int KV_PART = T::D / 16;      // components of either half that a lane holds, and pairs
 
-    double sn[H], cs[H];
-#pragma unroll
-    for (int e = 0; e < H; ++e) {
-        const int pair = pair_mode == IFLOW_ROPE_HALVES ? s * H + e : e < H / 2 ? s * H / 2 + e : D / 4 + s * H / 2 + e - H / 2;
-        sincos((double)(seq.position + token) * exp2(-(2.0 * pair / D) * log2_base), &sn[e], &cs[e]);
+// Turns of the pairs of a lane: pair first() + e for e < KV_PART, or in two halves of consecutive ones (adjacent pairing).
+struct KvTurns {
+    double log2_base;
+    double ratio[8];                                          // base^(-2e/d): frequencies of consecutive pairs
+    int pair_mode;
+};
+
+// sin and cos of an angle of up to 2^21 in fp64: the multiple of pi/2 is taken off in two parts with one rounding each (the first exact but for the rounding of the small
+// difference), then Taylor's series to r^15 and r^14, |r| <= pi/4: 2^-51 is left out.  (The library's functions, which take any angle, were most of the append's time: 157 us of it for
+// 5000 tokens of 32/8 heads, one per pair and head.)
+__device__ __forceinline__ void kv_sincos(double angle, double *sn, double *cs)
+{
+    const double turns = rint(angle * 0.63661977236758134308);                       // 2 / pi
+    const double r = __builtin_fma(-turns, 6.123233995736766036e-17, __builtin_fma(-turns, 1.57079632679489661923, angle));      // pi / 2 = 1.57.. + 6.1e-17
+    const int quadrant = (int)turns;
+    const double r2 = r * r;
+    double a = -1.0 / 1307674368000.0, b = -1.0 / 87178291200.0;                     // 1/15!, 1/14!
+    a = __builtin_fma(a, r2, 1.0 / 6227020800.0);  b = __builtin_fma(b, r2, 1.0 / 479001600.0);
+    a = __builtin_fma(a, r2, -1.0 / 39916800.0);   b = __builtin_fma(b, r2, -1.0 / 3628800.0);
+    a = __builtin_fma(a, r2, 1.0 / 362880.0);      b = __builtin_fma(b, r2, 1.0 / 40320.0);
+    a = __builtin_fma(a, r2, -1.0 / 5040.0);       b = __builtin_fma(b, r2, -1.0 / 720.0);
+    a = __builtin_fma(a, r2, 1.0 / 120.0);         b = __builtin_fma(b, r2, 1.0 / 24.0);
+    a = __builtin_fma(a, r2, -1.0 / 6.0);          b = __builtin_fma(b, r2, -0.5);
+    a = __builtin_fma(a * r2, r, r);               b = __builtin_fma(b, r2, 1.0);
+    const double s = quadrant & 1 ? b : a, c = quadrant & 1 ? a : b;
+    *sn = quadrant & 2 ? -s : s;
+    *cs = (quadrant + 1) & 2 ? -c : c;
+}
+
+// fp64 to fp16 with one rounding: cut to 24 bits, the last of them set where something was cut off, so that the second rounding sees what the first one saw
+__device__ __forceinline__ half_t kv_half_once(double x)
+{
+    const float f = (float)x;
+    const double back = (double)f;
+    uint32_t u = __builtin_bit_cast(uint32_t, f);
+    u -= fabs(back) > fabs(x) ? 1u : 0u;
+    u |= back != x ? 1u : 0u;
+    return (half_t)__builtin_bit_cast(float, u);
+}
+
+template <typename T> struct KvLane {
+    static constexpr int H = KV_PART<T>, D = T::D;
+    half_t x[2 * H];                                          // both halves' components
+
+    static __device__ __forceinline__ int pair_of(int s, int e, int pair_mode)
+    {
+        return pair_mode == IFLOW_ROPE_HALVES ? s * H + e : e < H / 2 ? s * H / 2 + e : D / 4 + s * H / 2 + e - H / 2;
     }
-    auto load = [&](const uint16_t *from, half_t (&x)[2 * H]) {
+    __device__ __forceinline__ void load(const uint16_t *row, int s)
+    {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             uint32_t w[H / 2];
-            if constexpr (H == 8) *reinterpret_cast<kv_u32x4 *>(w) = *reinterpret_cast<const kv_u32x4 *>(from + half * (D / 2) + s * H);
-            else *reinterpret_cast<kv_u32x2 *>(w) = *reinterpret_cast<const kv_u32x2 *>(from + half * (D / 2) + s * H);
+            if constexpr (H == 8) *reinterpret_cast<kv_u32x4 *>(w) = *reinterpret_cast<const kv_u32x4 *>(row + half * (D / 2) + s * H);
+            else *reinterpret_cast<kv_u32x2 *>(w) = *reinterpret_cast<const kv_u32x2 *>(row + half * (D / 2) + s * H);
 #pragma unroll
             for (int e = 0; e < H / 2; ++e) { const half2_t p = as_h2(w[e]); x[half * H + 2 * e] = p.x; x[half * H + 2 * e + 1] = p.y; }
         }
-    };
-    auto rotate = [&](half_t (&x)[2 * H]) {
-#pragma unroll
-        for (int e = 0; e < H; ++e) {
-            const int ia = pair_mode == IFLOW_ROPE_HALVES ? e : 2 * e, ib = pair_mode == IFLOW_ROPE_HALVES ? H + e : 2 * e + 1;
-            const double a = (double)(float)x[ia], c = (double)(float)x[ib];
-            x[ia] = (half_t)(a * cs[e] - c * sn[e]);
-            x[ib] = (half_t)(a * sn[e] + c * cs[e]);
-        }
-    };
-
-    if ((int)blockIdx.y >= v.n_kv_heads) {                    // a query head
-        const int h = blockIdx.y - v.n_kv_heads;
-        if (!mine) return;
-        half_t x[2 * H];
-        load(q + (row * n_heads + h) * D, x);
-        rotate(x);
+    }
+    __device__ __forceinline__ void store(uint16_t *row, int s) const
+    {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             uint32_t w[H / 2];
 #pragma unroll
             for (int e = 0; e < H / 2; ++e) w[e] = as_u32((half2_t){x[half * H + 2 * e], x[half * H + 2 * e + 1]});
-            uint16_t *to = q_out + (row * n_heads + h) * D + half * (D / 2) + s * H;
-            if constexpr (H == 8) *reinterpret_cast<kv_u32x4 *>(to) = *reinterpret_cast<kv_u32x4 *>(w);
-            else *reinterpret_cast<kv_u32x2 *>(to) = *reinterpret_cast<kv_u32x2 *>(w);
+            if constexpr (H == 8) *reinterpret_cast<kv_u32x4 *>(row + half * (D / 2) + s * H) = *reinterpret_cast<kv_u32x4 *>(w);
+            else *reinterpret_cast<kv_u32x2 *>(row + half * (D / 2) + s * H) = *reinterpret_cast<kv_u32x2 *>(w);
         }
-        return;
     }
-    const int head = blockIdx.y;
-    // (t of a tile with a token is in 0 .. max_seq / 32: no other is looked up)
-    const int64_t first_token = t * KV_TILE - seq.position;
-    bool any = false;
-    for (int i = 0; i < KV_TILE; ++i) any |= seq.has(first_token + i);
-    if (!any) return;
-    uint8_t *tile = kv_tile_at(v, b, head, (int)t, T::BYTES);
-    if (!tile) return;
-
-    for (int which = 0; which < 2; ++which) {
-        half_t x[2 * H];
-        if (mine) {
-            load((which ? v_new : k_new) + (row * v.n_kv_heads + head) * D, x);
-            if (!which) rotate(x);
-        } else {
+    template <typename Turn> __device__ __forceinline__ void rotate(int pair_mode, Turn turn)
+    {
 #pragma unroll
-            for (int e = 0; e < 2 * H; ++e) x[e] = (half_t)0.f;
+        for (int e = 0; e < H; ++e) {
+            double sn, cs;
+            turn(e, &sn, &cs);
+            if (pair_mode == IFLOW_ROPE_HALVES) {
+                const double a = (double)(float)x[e], b = (double)(float)x[H + e];
+                x[e] = kv_half_once(__builtin_fma(a, cs, -(b * sn)));
+                x[H + e] = kv_half_once(__builtin_fma(a, sn, b * cs));
+            } else {
+                const double a = (double)(float)x[2 * e], b = (double)(float)x[2 * e + 1];
+                x[2 * e] = kv_half_once(__builtin_fma(a, cs, -(b * sn)));
+                x[2 * e + 1] = kv_half_once(__builtin_fma(a, sn, b * cs));
+            }
         }
+    }
+    // The lane's levels, as iflow_quantize_'s kernel finds them (multiplied by the reciprocal, divided where that could decide differently), and the headers of its blocks, by half of the head.
+    __device__ __forceinline__ void quantize(uint32_t (&level)[2 * H], uint32_t (&header)[2]) const
+    {
         float mn[2], mx[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -107,59 +108,248 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView v, const uint16_t
         if (T::NB == 1) { mn[0] = mn[1] = fminf(mn[0], mn[1]); mx[0] = mx[1] = fmaxf(mx[0], mx[1]); }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            constexpr bool EIGHT = T::NB <= 2;                // a half of the head, or (128 components in blocks of 32) a quarter of it
-            const float low = kv_min<EIGHT>(mn[half]) + 0.0f, high = kv_max<EIGHT>(mx[half]) + 0.0f;
+            // over the eight lanes, or, where a half has two blocks, over four
+            float low = mn[half], high = mx[half];
+            low = fminf(low, dpp_f32<0xB1, 0xF>(low));  high = fmaxf(high, dpp_f32<0xB1, 0xF>(high));
+            low = fminf(low, dpp_f32<0x4E, 0xF>(low));  high = fmaxf(high, dpp_f32<0x4E, 0xF>(high));
+            if (T::NB <= 2) { low = fminf(low, dpp_f32<0x141, 0xF>(low)); high = fmaxf(high, dpp_f32<0x141, 0xF>(high)); }
+            low += 0.0f; high += 0.0f;                        // a zero of either sign becomes +0
             const half_t sh = (half_t)((high - low) / (float)T::L), oh = (half_t)low;
-            const float sc = (float)sh, of = (float)oh;
+            header[half] = as_u16(sh) | (uint32_t)as_u16(oh) << 16;
+            const float sc = (float)sh, of = (float)oh, rs = sc == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sc);
+            float edge = 0.f;
 #pragma unroll
             for (int e = 0; e < H; ++e) {
-                const float quotient = ((float)x[half * H + e] - of) / sc;
-                float f = floorf(quotient);
-                f = quotient - f >= 0.5f ? f + 1.0f : f;
-                f = f >= 0.0f ? f : 0.0f;
-                f = fminf(f, (float)T::L);
-                s_level[which][r][half * (D / 2) + s * H + e] = sc == 0.0f ? 0 : (uint8_t)f;
+                const float f = __builtin_amdgcn_fmed3f(((float)x[half * H + e] - of) * rs, -1.0f, (float)T::L + 1.0f) + 0.5f;
+                const float r = floorf(f);
+                edge = fmaxf(edge, fabsf((f - r) - 0.5f));
+                level[half * H + e] = (uint32_t)__builtin_amdgcn_fmed3f(r, 0.0f, (float)T::L);
             }
-            const int block = T::NB == 1 ? 0 : T::NB == 2 ? half : half * 2 + (s >> 2);
-            const bool writes = mine && (T::NB == 4 ? (s & 3) == 0 : s == 0) && (T::NB > 1 || half == 0);
-            if (writes) {
-                uint16_t *headers = reinterpret_cast<uint16_t *>(tile + (which ? T::VH_AT : T::KH_AT));
-                const int at = which ? kv_value_header(r, block) : kv_key_header(r, block);
-                headers[at] = as_u16(sh);
-                headers[at + (which ? 8 : 1)] = as_u16(oh);
+            if (edge > 0.5f - 0.0001220703125f) {
+#pragma unroll
+                for (int e = 0; e < H; ++e) {
+                    const float t = ((float)x[half * H + e] - of) / sc;
+                    float r = floorf(t);
+                    r = t - r >= 0.5f ? r + 1.0f : r;
+                    r = r >= 0.0f ? r : 0.0f;
+                    level[half * H + e] = sc == 0.0f ? 0u : (uint32_t)fminf(r, (float)T::L);
+                }
+            }
+        }
+    }
+    // which lanes hold a block's header, and whose
+    static __device__ __forceinline__ bool has_header(int s, int half) { return T::NB == 4 ? (s & 3) == 0 : s == 0 && (T::NB == 2 || half == 0); }
+    static __device__ __forceinline__ int block_of(int s, int half) { return T::NB == 1 ? 0 : T::NB == 2 ? half : half * 2 + (s >> 2); }
+    // words of key codes of one half: put(first component, word)
+    template <typename Put> static __device__ __forceinline__ void key_words(const uint32_t *level, int s, int half, Put put)
+    {
+        const int c = half * (D / 2) + s * H;
+        if constexpr (T::BITS == 8) {
+#pragma unroll
+            for (int e = 0; e < H; e += 4) put(c + e, level[e] | level[e + 1] << 8 | level[e + 2] << 16 | level[e + 3] << 24);
+        } else if constexpr (H == 8) {
+            put(c, level[0] | level[2] << 4 | level[4] << 8 | level[6] << 12 | level[1] << 16 | level[3] << 20 | level[5] << 24 | level[7] << 28);
+        } else {
+            uint32_t part = level[0] | level[2] << 4 | level[1] << 16 | level[3] << 20;
+            if (s & 1) part <<= 8;
+            const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)part, 0xB1, 0xF, 0xF, true);
+            if (!(s & 1)) put(c, part | other);
+        }
+    }
+};
+
+// One token per sequence: a workgroup takes 32 rows of one token, keys' heads first, then values', then queries'.  Bound by the latency of what follows on one another: the sequence's length, its page, the
+// row, and for values the words that eight positions share (read, changed, written by one lane; requested as soon as the page is known).
+template <typename T>
+__global__ __launch_bounds__(256) void kv_append_token_kernel(KvView v, const uint16_t *q, const uint16_t *__restrict__ k_new, const uint16_t *__restrict__ v_new, int n_heads, KvTurns turns,
+                                                              uint16_t *q_out)
+{
+    constexpr int D = T::D, H = KV_PART<T>;
+    __shared__ double s_turn[2][D / 2];
+    __shared__ uint8_t s_level[32][D];
+    const int tid = threadIdx.x, r = tid >> 3, s = tid & 7, b = blockIdx.x;
+    const KvSequence seq(v, b);
+    if (!seq.has(0)) return;
+    const int line = blockIdx.y * 32 + r, kind = line < v.n_kv_heads ? 0 : line < 2 * v.n_kv_heads ? 1 : line < 2 * v.n_kv_heads + n_heads ? 2 : 3;
+    const int head = line - (kind == 2 ? 2 : kind) * v.n_kv_heads, heads = kind == 2 ? n_heads : v.n_kv_heads;
+    KvLane<T> lane;
+    if (kind < 3) lane.load((kind == 0 ? k_new : kind == 1 ? v_new : q) + (seq.row * heads + head) * D, s);
+    uint8_t *tile = kind < 2 ? kv_tile_at(v, b, head, (int)(seq.position / KV_TILE), T::BYTES) : nullptr;
+    const int at = (int)(seq.position % KV_TILE), g = (at & 15) >> 2, k = (at >> 4) * 4 + (at & 3);
+    // the values' pieces: a lane takes those of components s and s + 8 of every sixteen
+    kv_u32x4 old[T::PIECES][2];
+    if (kind == 1 && tile) {
+#pragma unroll
+        for (int n = 0; n < T::PIECES; ++n)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) old[n][u] = *reinterpret_cast<const kv_u32x4 *>(tile + T::V_AT + (n * 64 + g * 16 + s + 8 * u) * 16);
+    }
+    if (tid < D / 2) kv_sincos((double)seq.position * exp2(-(2.0 * tid / D) * turns.log2_base), &s_turn[0][tid], &s_turn[1][tid]);
+    __syncthreads();
+    if (kind == 0 || kind == 2) {
+        lane.rotate(turns.pair_mode, [&](int e, double *sn, double *cs) {
+            const int pair = KvLane<T>::pair_of(s, e, turns.pair_mode);
+            *sn = s_turn[0][pair]; *cs = s_turn[1][pair];
+        });
+    }
+    if (kind == 2) lane.store(q_out + (seq.row * heads + head) * D, s);
+    uint32_t level[2 * H], header[2];
+    if (kind < 2) {
+        lane.quantize(level, header);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            if (tile && KvLane<T>::has_header(s, half)) {
+                const int block = KvLane<T>::block_of(s, half);
+                if (kind == 0) {
+                    *reinterpret_cast<uint32_t *>(tile + T::KH_AT + 2 * kv_key_header(at, block)) = header[half];
+                } else {
+                    uint16_t *to = reinterpret_cast<uint16_t *>(tile + T::VH_AT) + kv_value_header(at, block);
+                    to[0] = (uint16_t)header[half]; to[8] = (uint16_t)(header[half] >> 16);
+                }
+            }
+            if (kind == 0) {
+                KvLane<T>::key_words(level + half * H, s, half, [&](int c, uint32_t w) { if (tile) reinterpret_cast<uint32_t *>(tile)[kv_key_word<T>(at, c)] = w; });
+            } else {
+#pragma unroll
+                for (int e = 0; e < H; ++e) s_level[r][half * (D / 2) + s * H + e] = (uint8_t)level[half * H + e];
             }
         }
     }
     __syncthreads();
-    auto is_new = [&](int p) { return seq.has(first_token + p); };
-    auto place = [](int e) { return T::BITS == 8 ? 8 * e : (e >> 1) * 4 + (e & 1) * 16; };
-    for (int n = tid; n < KV_TILE * D / T::PER_WORD; n += 256) {
-        // keys: a word is PER_WORD components of one position
-        {
-            const int p = n / (D / T::PER_WORD), c = n % (D / T::PER_WORD) * T::PER_WORD;
-            if (is_new(p)) {
-                uint32_t w = 0;
+    if (kind == 1 && tile) {
+        // word w of piece n holds, of component i, element k of the eight positions in 4 bits: components 64 n + 16 w + i; in 8 bits four positions to a word, two words to a component
 #pragma unroll
-                for (int e = 0; e < T::PER_WORD; ++e) w |= (uint32_t)s_level[0][p][c + e] << place(e);
-                reinterpret_cast<uint32_t *>(tile)[kv_key_word<T>(p, c)] = w;
+        for (int n = 0; n < T::PIECES; ++n)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int i = s + 8 * u;
+                kv_u32x4 x = old[n][u];
+                if constexpr (T::BITS == 4) {
+                    const int shift = (k >> 1) * 4 + (k & 1) * 16;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) x[w] = (x[w] & ~(15u << shift)) | (uint32_t)s_level[r][64 * n + 16 * w + i] << shift;
+                } else {
+                    const int shift = (k & 3) * 8;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t changed = (x[w] & ~(255u << shift)) | (uint32_t)s_level[r][32 * n + 16 * (w >> 1) + i] << shift;
+                        x[w] = (w & 1) == (k >> 2) ? changed : x[w];
+                    }
+                }
+                *reinterpret_cast<kv_u32x4 *>(tile + T::V_AT + (n * 64 + g * 16 + i) * 16) = x;
             }
+    }
+}
+
+// Any number of tokens: a workgroup takes the new positions of one tile, of one key/value head or of several query heads.  A tile is put together in LDS, over what it held where
+// positions of it are older, and leaves in 16-byte pieces; nobody else writes it in this call.
+template <typename T>
+__global__ __launch_bounds__(256) void kv_append_tile_kernel(KvView v, const uint16_t *q, const uint16_t *__restrict__ k_new, const uint16_t *__restrict__ v_new, int n_heads, KvTurns turns,
+                                                             uint16_t *q_out, int tiles_per_seq, int heads_per_group)
+{
+    constexpr int D = T::D, H = KV_PART<T>;
+    __shared__ __align__(16) uint32_t s_image[T::BYTES / 4];
+    __shared__ __align__(16) uint8_t s_level[KV_TILE][D];
+    const int tid = threadIdx.x, r = tid >> 3, s = tid & 7;
+    const int b = blockIdx.x / tiles_per_seq;
+    const KvSequence seq(v, b);
+    const int64_t t = seq.first_tile() + (blockIdx.x - b * tiles_per_seq);
+    const int64_t first_token = t * KV_TILE - seq.position, token = first_token + r, row = seq.row + token;
+    const uint32_t fresh = (uint32_t)__builtin_amdgcn_ballot_w64(seq.has(first_token + (tid & 31)));       // positions of the tile that are new
+    if (fresh == 0) return;
+    const bool mine = fresh >> r & 1;
+
+    double sn[H], cs[H];
+    auto take_turns = [&] {
+        const double position = (double)(seq.position + token);
+        const double f0 = exp2(-(2.0 * KvLane<T>::pair_of(s, 0, turns.pair_mode) / D) * turns.log2_base);
+        const double f1 = turns.pair_mode == IFLOW_ROPE_HALVES ? f0 * turns.ratio[H / 2] : exp2(-(2.0 * KvLane<T>::pair_of(s, H / 2, turns.pair_mode) / D) * turns.log2_base);
+#pragma unroll
+        for (int e = 0; e < H; ++e) kv_sincos(position * ((e < H / 2 ? f0 : f1) * turns.ratio[e % (H / 2)]), &sn[e], &cs[e]);
+    };
+    auto turn = [&](int e, double *a, double *c) { *a = sn[e]; *c = cs[e]; };
+
+    if ((int)blockIdx.y >= v.n_kv_heads) {                    // query heads
+        const int h0 = (blockIdx.y - v.n_kv_heads) * heads_per_group, h1 = min(n_heads, h0 + heads_per_group);
+        if (!mine) return;
+        KvLane<T> next;
+        next.load(q + (row * n_heads + h0) * D, s);
+        take_turns();
+        for (int h = h0; h < h1; ++h) {
+            KvLane<T> lane = next;
+            if (h + 1 < h1) next.load(q + (row * n_heads + h + 1) * D, s);
+            lane.rotate(turns.pair_mode, turn);
+            lane.store(q_out + (row * n_heads + h) * D, s);
         }
-        // values: PER_WORD positions of one component, of which some may be older
-        {
-            const int c = n % D, x = n / D, g = x / (8 / T::PER_WORD), k = x % (8 / T::PER_WORD) * T::PER_WORD;
-            uint32_t w = 0, keep = 0;
+        return;
+    }
+    const int head = blockIdx.y;
+    // (a position that is new is in 0 .. max_seq - 1: no other tile is looked up)
+    uint8_t *tile = kv_tile_at(v, b, head, (int)t, T::BYTES);
+    if (!tile) return;
+    KvLane<T> key, value;
+    if (mine) {
+        key.load(k_new + (row * v.n_kv_heads + head) * D, s);
+        value.load(v_new + (row * v.n_kv_heads + head) * D, s);
+    } else {
 #pragma unroll
-            for (int e = 0; e < T::PER_WORD; ++e) {
-                const int p = kv_value_position(g, k + e);
-                if (is_new(p)) w |= (uint32_t)s_level[1][p][c] << place(e);
-                else keep |= (uint32_t)T::L << place(e);
-            }
-            if (keep != 0xFFFFFFFFu) {
-                uint32_t *at = reinterpret_cast<uint32_t *>(tile + T::V_AT) + kv_value_word<T>(g, k, c);
-                *at = keep ? w | (*at & keep) : w;
-            }
+        for (int e = 0; e < 2 * H; ++e) key.x[e] = value.x[e] = (half_t)0.f;
+    }
+    if (fresh != 0xFFFFFFFFu) {
+        for (int n = tid; n < T::BYTES / 16; n += 256) reinterpret_cast<kv_u32x4 *>(s_image)[n] = reinterpret_cast<const kv_u32x4 *>(tile)[n];
+        __syncthreads();
+    }
+    take_turns();
+    key.rotate(turns.pair_mode, turn);
+    uint32_t level[2 * H], header[2];
+    key.quantize(level, header);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        if (mine && KvLane<T>::has_header(s, half)) s_image[T::KH_AT / 4 + kv_key_header(r, KvLane<T>::block_of(s, half)) / 2] = header[half];
+        KvLane<T>::key_words(level + half * H, s, half, [&](int c, uint32_t w) { if (mine) s_image[kv_key_word<T>(r, c)] = w; });
+    }
+    value.quantize(level, header);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        if (mine && KvLane<T>::has_header(s, half)) {
+            uint16_t *to = reinterpret_cast<uint16_t *>(s_image) + T::VH_AT / 2 + kv_value_header(r, KvLane<T>::block_of(s, half));
+            to[0] = (uint16_t)header[half]; to[8] = (uint16_t)(header[half] >> 16);
+        }
+#pragma unroll
+        for (int e = 0; e < H; e += 4) {
+            const uint32_t *l = level + half * H + e;
+            *reinterpret_cast<uint32_t *>(&s_level[r][half * (D / 2) + s * H + e]) = l[0] | l[1] << 8 | l[2] << 16 | l[3] << 24;
         }
     }
+    __syncthreads();
+    // values' words: four components at once, a byte each, of the eight (four) positions of a word; then bytes to words
+    constexpr int WORDS = 8 / T::PER_WORD;                    // of the eight positions of g
+    for (int n = tid; n < 4 * WORDS * (D / 4); n += 256) {
+        const int c = n % (D / 4) * 4, x = n / (D / 4), g = x / WORDS, k0 = x % WORDS * T::PER_WORD;
+        uint32_t l[T::PER_WORD], keep = 0;
+#pragma unroll
+        for (int e = 0; e < T::PER_WORD; ++e) {
+            const int p = kv_value_position(g, k0 + e);
+            l[e] = *reinterpret_cast<const uint32_t *>(&s_level[p][c]);
+            if (!(fresh >> p & 1)) keep |= (uint32_t)T::L << (T::BITS == 8 ? 8 * e : (e >> 1) * 4 + (e & 1) * 16);
+        }
+        uint32_t byte[4];                                     // byte j of component c + i's word is byte i of byte[j]
+        if constexpr (T::BITS == 4) {
+            byte[0] = l[0] | l[2] << 4; byte[1] = l[4] | l[6] << 4; byte[2] = l[1] | l[3] << 4; byte[3] = l[5] | l[7] << 4;
+        } else {
+            byte[0] = l[0]; byte[1] = l[1]; byte[2] = l[2]; byte[3] = l[3];
+        }
+        const uint32_t a = __builtin_amdgcn_perm(byte[1], byte[0], 0x05010400u), d = __builtin_amdgcn_perm(byte[3], byte[2], 0x05010400u);       // bytes of components 0, 1
+        const uint32_t e = __builtin_amdgcn_perm(byte[1], byte[0], 0x07030602u), f = __builtin_amdgcn_perm(byte[3], byte[2], 0x07030602u);       // 2, 3
+        const uint32_t w[4] = {(a & 0xFFFFu) | d << 16, a >> 16 | (d & 0xFFFF0000u), (e & 0xFFFFu) | f << 16, e >> 16 | (f & 0xFFFF0000u)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t *to = s_image + T::V_AT / 4 + kv_value_word<T>(g, k0, c + i);
+            *to = keep ? (w[i] & ~keep) | (*to & keep) : w[i];
+        }
+    }
+    __syncthreads();
+    for (int n = tid; n < T::BYTES / 16; n += 256) reinterpret_cast<kv_u32x4 *>(tile)[n] = reinterpret_cast<const kv_u32x4 *>(s_image)[n];
 }
 
 // ---- read back ----------------------------------------------------------------------------------------------------------------
@@ -225,10 +415,22 @@ hipError_t launch_kv_append(int format, int head_dim, const KvView &v, const uin
 {
     const int64_t tiles = kv_tiles_touched(v), grid = tiles * v.n_seqs;
     if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    KvTurns turns;
+    turns.log2_base = log2(base);
+    turns.pair_mode = pair_mode;
+    for (int e = 0; e < 8; ++e) turns.ratio[e] = exp2(-(2.0 * e / head_dim) * turns.log2_base);
+    // query heads of a workgroup: as many as leave a thousand workgroups, up to eight
+    const int64_t per = grid * n_heads / 1024;
+    const int heads_per_group = per < 1 ? 1 : per > 8 ? 8 : (int)per;
     return for_kv_tile(format, head_dim, [&](auto tag) {
         typedef decltype(tag) T;
-        hipLaunchKernelGGL((kv_append_kernel<T>), dim3((unsigned)grid, (unsigned)(v.n_kv_heads + n_heads)), dim3(256), 0, s, v, q, k_new, v_new, n_heads, log2(base), pair_mode, q_out,
-                           (int)tiles);
+        if (v.max_tokens == 1) {
+            hipLaunchKernelGGL((kv_append_token_kernel<T>), dim3((unsigned)v.n_seqs, (unsigned)((2 * v.n_kv_heads + n_heads + 31) / 32)), dim3(256), 0, s, v, q, k_new, v_new, n_heads, turns,
+                               q_out);
+        } else {
+            hipLaunchKernelGGL((kv_append_tile_kernel<T>), dim3((unsigned)grid, (unsigned)(v.n_kv_heads + (n_heads + heads_per_group - 1) / heads_per_group)), dim3(256), 0, s, v, q, k_new,
+                               v_new, n_heads, turns, q_out, (int)tiles, heads_per_group);
+        }
         return hipGetLastError();
     });
 }
