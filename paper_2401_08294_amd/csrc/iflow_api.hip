@@ -386,13 +386,14 @@ static iflow_status_t kv_shapes(const iflow_kv_cache_t *c, const iflow_kv_batch_
     if (st != IFLOW_OK) return st;
     if (!b) return IFLOW_ERR_NULL;
     if (heads && (n_heads < 1 || n_heads > 512 || n_heads % c->n_kv_heads != 0)) return IFLOW_ERR_SHAPE;
-    if (b->n_seqs < 1 || b->n_seqs > 65536 || b->max_pages < 1) return IFLOW_ERR_SHAPE;
+    if (b->n_seqs < 1 || b->n_seqs > 65535 || b->max_pages < 1) return IFLOW_ERR_SHAPE;
     if (b->max_seq < 1 || b->max_seq > (1 << 20) || b->max_seq > (int64_t)b->max_pages * c->page_positions) return IFLOW_ERR_SHAPE;
     if (b->max_tokens < 1 || b->max_tokens > b->max_seq || b->n_tokens < 1 || b->n_tokens > (1LL << 24)) return IFLOW_ERR_SHAPE;
     if (!b->first_token && (b->max_tokens != 1 || b->n_tokens < b->n_seqs)) return IFLOW_ERR_SHAPE;
     if (!b->page_table && (int64_t)b->n_seqs * b->max_pages > c->n_pages) return IFLOW_ERR_SHAPE;
     *v = {static_cast<uint8_t *>(c->pages), b->page_table, b->seq_lens, b->first_token, c->n_pages, b->n_tokens, page_bytes,
-          b->n_seqs, b->max_pages, b->max_tokens, b->max_seq, c->n_kv_heads, c->page_positions / 32};
+          b->n_seqs, b->max_pages, b->max_tokens, b->max_seq, c->n_kv_heads, c->page_positions / 32,
+          c->page_positions == 32 ? 0u : (uint32_t)(((1ULL << 32) + c->page_positions / 32 - 1) / (uint32_t)(c->page_positions / 32))};
     return IFLOW_OK;
 }
 

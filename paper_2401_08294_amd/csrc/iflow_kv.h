@@ -43,36 +43,46 @@ struct KvView {
     const int32_t *table, *lens, *first;                      // table, first: may be null
     int64_t n_pages, n_tokens, page_bytes;
     int32_t n_seqs, max_pages, max_tokens, max_seq, n_kv_heads, tiles_per_page;
+    uint32_t page_magic;                                      // ceil(2^32 / tiles_per_page); 0 for 1
+    __device__ __forceinline__ int page_of(int t) const { return page_magic ? (int)__umulhi((uint32_t)t, page_magic) : t; }      // t / tiles_per_page, exact for t, tiles_per_page < 2^16
 };
 
 // One sequence's new tokens as the kernels take them: rows row .. row + count - 1 of the batch's tokens at positions position .. .  Whatever the arrays
-// hold, what comes out of here stays inside the call's buffers: count at most max_tokens, and every token is asked for with has().
+// hold, what comes out of here stays inside the call's buffers: count is at most max_tokens, and every token is asked for with has().  (In 32 bits: where numbers that no batch has
+// leave them, what has() sees is other numbers, and it still sees them.)
 struct KvSequence {
-    int64_t row, position, n_tokens;
-    int count, max_seq;
+    int row, position, count, n_tokens, max_seq;
     __device__ __forceinline__ KvSequence(const KvView &v, int b)
     {
-        const int64_t at = v.first ? v.first[b] : b, n = v.first ? (int64_t)v.first[b + 1] - at : 1;
-        row = at; n_tokens = v.n_tokens; max_seq = v.max_seq;
-        position = (int64_t)v.lens[b] - n;
-        count = (int)max((int64_t)0, min(n, (int64_t)v.max_tokens));
+        row = v.first ? v.first[b] : b;
+        const int n = v.first ? (int)((uint32_t)v.first[b + 1] - (uint32_t)row) : 1;
+        n_tokens = (int)v.n_tokens; max_seq = v.max_seq;
+        position = (int)((uint32_t)v.lens[b] - (uint32_t)n);
+        count = max(0, min(n, v.max_tokens));
     }
     // token i has a row, and a position that the cache has
-    __device__ __forceinline__ bool has_row(int64_t i) const { return i >= 0 && i < count && row + i >= 0 && row + i < n_tokens; }
-    __device__ __forceinline__ bool has(int64_t i) const { return has_row(i) && position + i >= 0 && position + i < max_seq; }
-    __device__ __forceinline__ int64_t first_tile() const { return position >> 5; }      // (rounded down, also below zero)
+    __device__ __forceinline__ bool has_row(int i) const { return (uint32_t)i < (uint32_t)count && (uint32_t)row + (uint32_t)i < (uint32_t)n_tokens; }
+    __device__ __forceinline__ bool has(int i) const { return has_row(i) && (uint32_t)position + (uint32_t)i < (uint32_t)max_seq; }
+    __device__ __forceinline__ int first_tile() const { return position >> 5; }          // (rounded down, also below zero)
     // positions that token i sees: its own and all before
-    __device__ __forceinline__ int sees(int i) const { return (int)max((int64_t)0, min(position + i + 1, (int64_t)max_seq)); }
+    __device__ __forceinline__ int sees(int i) const { return max(0, min((int)((uint32_t)position + (uint32_t)i + 1u), max_seq)); }
 };
 
 // The tile that holds positions 32 t .. 32 t + 31 of sequence b; null where its page is none of the cache's.  (t < max_seq / 32, rounded up: inside the table's row.)
+__device__ __forceinline__ int64_t kv_page(const KvView &v, int b, int p)
+{
+    const int64_t entry = (int64_t)b * v.max_pages + p;
+    return v.table ? (int64_t)v.table[entry] : entry;
+}
+__device__ __forceinline__ uint8_t *kv_tile_in(const KvView &v, int64_t page, int kv_head, int tile_of_page, int tile_bytes)
+{
+    if (page < 0 || page >= v.n_pages) return nullptr;
+    return v.pages + page * v.page_bytes + ((int64_t)kv_head * v.tiles_per_page + tile_of_page) * tile_bytes;
+}
 __device__ __forceinline__ uint8_t *kv_tile_at(const KvView &v, int b, int kv_head, int t, int tile_bytes)
 {
-    const int p = t / v.tiles_per_page;
-    const int64_t entry = (int64_t)b * v.max_pages + p;
-    const int64_t page = v.table ? (int64_t)v.table[entry] : entry;
-    if (page < 0 || page >= v.n_pages) return nullptr;
-    return v.pages + page * v.page_bytes + ((int64_t)kv_head * v.tiles_per_page + (t - p * v.tiles_per_page)) * tile_bytes;
+    const int p = v.page_of(t);
+    return kv_tile_in(v, kv_page(v, b, p), kv_head, t - p * v.tiles_per_page, tile_bytes);
 }
 
 // ---- where an element lies in its tile ------------------------------------------------------------------------------------
@@ -101,23 +111,27 @@ typedef float kv_float4 __attribute__((ext_vector_type(4)));
 struct KvPairs { half2_t p[4]; };                             // eight consecutive elements
 
 // the eight levels that begin at `word` (one word of nibbles, two of bytes) as fp16 numbers: or-ed into the mantissa of 1024 (64 for the nibbles four bits up), which is subtracted, exactly
+struct KvMagic {
+    uint32_t at0, at4;                                        // (in registers: v_and_or_b32 takes no literals)
+    __device__ __forceinline__ KvMagic() : at0(0x64006400u), at4(0x54005400u) { asm volatile("" : "+v"(at0), "+v"(at4)); }
+};
 template <int BITS>
-__device__ __forceinline__ KvPairs kv_levels(const uint32_t *word)
+__device__ __forceinline__ KvPairs kv_levels(const uint32_t *word, const KvMagic &magic)
 {
     KvPairs v;
+    const half2_t b0 = {(half_t)1024.f, (half_t)1024.f};
     if constexpr (BITS == 4) {
         const uint32_t w = word[0], w8 = w >> 8;
-        const half2_t b0 = {(half_t)1024.f, (half_t)1024.f}, b4 = {(half_t)64.f, (half_t)64.f};
-        v.p[0] = as_h2((w & 0x000F000Fu) | 0x64006400u) - b0;
-        v.p[1] = as_h2((w & 0x00F000F0u) | 0x54005400u) - b4;
-        v.p[2] = as_h2((w8 & 0x000F000Fu) | 0x64006400u) - b0;
-        v.p[3] = as_h2((w8 & 0x00F000F0u) | 0x54005400u) - b4;
+        const half2_t b4 = {(half_t)64.f, (half_t)64.f};
+        v.p[0] = as_h2(and_or(w, 0x000F000Fu, magic.at0)) - b0;
+        v.p[1] = as_h2(and_or(w, 0x00F000F0u, magic.at4)) - b4;
+        v.p[2] = as_h2(and_or(w8, 0x000F000Fu, magic.at0)) - b0;
+        v.p[3] = as_h2(and_or(w8, 0x00F000F0u, magic.at4)) - b4;
     } else {
-        const half2_t b0 = {(half_t)1024.f, (half_t)1024.f};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            v.p[2 * i] = as_h2(__builtin_amdgcn_perm(0x64646464u, word[i], 0x04010400u)) - b0;
-            v.p[2 * i + 1] = as_h2(__builtin_amdgcn_perm(0x64646464u, word[i], 0x04030402u)) - b0;
+            v.p[2 * i] = as_h2(__builtin_amdgcn_perm(magic.at0, word[i], 0x05010500u)) - b0;
+            v.p[2 * i + 1] = as_h2(__builtin_amdgcn_perm(magic.at0, word[i], 0x05030502u)) - b0;
         }
     }
     return v;

@@ -173,7 +173,7 @@ __global__ __launch_bounds__(256) void kv_append_token_kernel(KvView v, const ui
     const int line = blockIdx.y * 32 + r, kind = line < v.n_kv_heads ? 0 : line < 2 * v.n_kv_heads ? 1 : line < 2 * v.n_kv_heads + n_heads ? 2 : 3;
     const int head = line - (kind == 2 ? 2 : kind) * v.n_kv_heads, heads = kind == 2 ? n_heads : v.n_kv_heads;
     KvLane<T> lane;
-    if (kind < 3) lane.load((kind == 0 ? k_new : kind == 1 ? v_new : q) + (seq.row * heads + head) * D, s);
+    if (kind < 3) lane.load((kind == 0 ? k_new : kind == 1 ? v_new : q) + ((int64_t)seq.row * heads + head) * D, s);
     uint8_t *tile = kind < 2 ? kv_tile_at(v, b, head, (int)(seq.position / KV_TILE), T::BYTES) : nullptr;
     const int at = (int)(seq.position % KV_TILE), g = (at & 15) >> 2, k = (at >> 4) * 4 + (at & 3);
     // the values' pieces: a lane takes those of components s and s + 8 of every sixteen
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256) void kv_append_token_kernel(KvView v, const ui
             *sn = s_turn[0][pair]; *cs = s_turn[1][pair];
         });
     }
-    if (kind == 2) lane.store(q_out + (seq.row * heads + head) * D, s);
+    if (kind == 2) lane.store(q_out + ((int64_t)seq.row * heads + head) * D, s);
     uint32_t level[2 * H], header[2];
     if (kind < 2) {
         lane.quantize(level, header);
@@ -253,8 +253,8 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvView v, const uin
     const int tid = threadIdx.x, r = tid >> 3, s = tid & 7;
     const int b = blockIdx.x / tiles_per_seq;
     const KvSequence seq(v, b);
-    const int64_t t = seq.first_tile() + (blockIdx.x - b * tiles_per_seq);
-    const int64_t first_token = t * KV_TILE - seq.position, token = first_token + r, row = seq.row + token;
+    const int t = seq.first_tile() + (int)(blockIdx.x - b * tiles_per_seq), first_token = (int)((uint32_t)t * KV_TILE - (uint32_t)seq.position), token = first_token + r;
+    const int64_t row = (int64_t)seq.row + token;
     const uint32_t fresh = (uint32_t)__builtin_amdgcn_ballot_w64(seq.has(first_token + (tid & 31)));       // positions of the tile that are new
     if (fresh == 0) return;
     const bool mine = fresh >> r & 1;
@@ -357,26 +357,26 @@ template <typename T>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvView v, uint16_t *__restrict__ k_out, uint16_t *__restrict__ v_out, int tiles_per_seq)
 {
     constexpr int D = T::D, ROW = D + 8;
+    const KvMagic magic;
     __shared__ __align__(16) uint16_t s_value[KV_TILE][ROW];
     const int tid = threadIdx.x, head = blockIdx.y;
     const int b = blockIdx.x / tiles_per_seq;
     const KvSequence seq(v, b);
-    const int64_t t = seq.first_tile() + (blockIdx.x - b * tiles_per_seq);
-    const int64_t first_token = t * KV_TILE - seq.position;
+    const int t = seq.first_tile() + (int)(blockIdx.x - b * tiles_per_seq), first_token = (int)((uint32_t)t * KV_TILE - (uint32_t)seq.position);
     auto has = [&](int p) { return seq.has_row(first_token + p); };
     bool any = false;
     for (int i = 0; i < KV_TILE; ++i) any |= has(i);
     if (!any) return;
-    const uint8_t *tile = t >= 0 && t * KV_TILE < v.max_seq ? kv_tile_at(v, b, head, (int)t, T::BYTES) : nullptr;
+    const uint8_t *tile = t >= 0 && t <= (v.max_seq - 1) / KV_TILE ? kv_tile_at(v, b, head, (int)t, T::BYTES) : nullptr;
     auto there = [&](int p) { return tile && t * KV_TILE + p < v.max_seq; };
-    auto out_at = [&](int p, int c) { return ((seq.row + first_token + p) * v.n_kv_heads + head) * D + c; };
+    auto out_at = [&](int p, int c) { return (((int64_t)seq.row + first_token + p) * v.n_kv_heads + head) * D + c; };
     const uint16_t *kh = reinterpret_cast<const uint16_t *>(tile + T::KH_AT), *vh = reinterpret_cast<const uint16_t *>(tile + T::VH_AT);
     for (int n = tid; n < KV_TILE * D / 8; n += 256) {
         const int p = n / (D / 8), c = n % (D / 8) * 8;
         if (!has(p)) continue;
         kv_u32x4 w = {0u, 0u, 0u, 0u};
         if (there(p)) {
-            const KvPairs level = kv_levels<T::BITS>(reinterpret_cast<const uint32_t *>(tile) + kv_key_word<T>(p, c));
+            const KvPairs level = kv_levels<T::BITS>(reinterpret_cast<const uint32_t *>(tile) + kv_key_word<T>(p, c), magic);
             const int at = kv_key_header(p, c / T::BLOCK);
             const half_t sc = as_h(kh[at]), of = as_h(kh[at + 1]);
 #pragma unroll
@@ -387,7 +387,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvView v, uint16_t *__rest
     if (tile) {
         for (int n = tid; n < 4 * D; n += 256) {
             const int c = n % D, g = n / D;
-            const KvPairs level = kv_levels<T::BITS>(reinterpret_cast<const uint32_t *>(tile + T::V_AT) + kv_value_word<T>(g, 0, c));
+            const KvPairs level = kv_levels<T::BITS>(reinterpret_cast<const uint32_t *>(tile + T::V_AT) + kv_value_word<T>(g, 0, c), magic);
             const int at = kv_value_header(4 * g, c / T::BLOCK);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {

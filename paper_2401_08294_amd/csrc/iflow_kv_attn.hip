@@ -12,30 +12,89 @@
 //   - The scores' D layout, positions 4g .. 4g+3 of both halves for row i, is P^T's A operand layout of the second product when its positions are taken in that order.
 //   - Values are the B operand: lane (i, g) has components i, 16 + i, .. of just these eight positions, eight codes to a run's 32 (64) bits.
 // So codes come in with 1 KB per load instruction and become operands in registers: nothing crosses lanes or LDS.
+#include <algorithm>
+
 #include "iflow_kv.h"
 
 namespace iflow {
 
-constexpr int KVA_WAVES = 4;
 constexpr int KVA_ROWS = 16;                                  // rows of a workgroup
-constexpr int KVA_MAX_SPLITS = 128;                           // ranges a sequence is split into
-constexpr int KVA_MAX_CHUNK = 64 * KVA_WAVES * KV_TILE;       // positions of a range: a wavefront's tiles have their pages in its 64 lanes
+// workgroups that a compute unit holds at once (by their registers), and the whole device
+template <typename T> constexpr int KVA_PER_CU = T::D == 64 ? 4 : 3;
+constexpr int KVA_CUS = 256;
 constexpr float KVA_BELOW = 7.f, KVA_LAG = 15.f, KVA_SPARE = 16.f;       // in units of log2: see attn_decode_mfma_kernel
 
+// (the compiler quiets every operand of fmaxf first)
+__device__ __forceinline__ float kv_max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+// x - h.x, x - h.y in one instruction
+__device__ __forceinline__ float kv_less_low(float x, half2_t h)
+{
+    float r;
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(as_u32(h)), "v"(x));
+    return r;
+}
+__device__ __forceinline__ float kv_less_high(float x, half2_t h)
+{
+    float r;
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(as_u32(h)), "v"(x));
+    return r;
+}
 // the maximum over the four lanes i, i + 16, i + 32, i + 48
 __device__ __forceinline__ float kva_max_of_rows(float x)
 {
     const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-    x = fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+    x = kv_max3(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]), -INFINITY);
     const auto b = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-    return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+    return kv_max3(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]), -INFINITY);
 }
 
-// where the partial results of the ranges lie: O [output row][range][D], then M [output row][range], then L
+// Who does what.  The rows of a sequence's key/value head, sixteen at a time (a piece), go over all the sequence's tiles: that is a line of work.  How long the lines are only the device
+// knows: every workgroup adds up all sequences' tiles and cuts the lines into parts of at most `share` tiles, and takes the part that its number says.  A part of several
+// leaves partial results, which a second launch adds up.
+// (Tried: ranges of a fixed number of positions: a die gets the same range of every sequence, 66 us for 32 sequences of 1000 to 8001 positions, 32/8 heads, turned by head and
+// sequence 51; exactly equal shares of consecutive tiles that cross from line to line: a workgroup that crosses takes 5 us longer, and the rest wait for it, 45.)
+// (Tiles are counted in 32 bits: where all lines might have more, every line is a workgroup's.)
+struct KvLines { int tiles, lines; };                         // of each line; lines of the sequence
+__device__ __forceinline__ KvLines kv_lines_of(const KvView &v, const KvSequence &seq, int group)
+{
+    KvLines x;
+    x.lines = v.n_kv_heads * ((seq.count * group + KVA_ROWS - 1) / KVA_ROWS);
+    x.tiles = max(1, (seq.sees(seq.count - 1) + KV_TILE - 1) / KV_TILE);       // (one that sees nothing has zeros to write)
+    return x;
+}
+// work space: the partial results' slots before each sequence [n_seqs], the parts' tiles, then the partial results: M [slot][row], L [slot][row], O [slot][row][D].  (Lines of several parts have
+// more tiles than a part has, and parts have at least 1 / capacity of all tiles: there are less than two for each workgroup that the device holds.)
 struct KvPartial {
-    float *o, *m, *l;
-    int splits;
-    __device__ __host__ KvPartial(float *ws, int64_t rows, int splits_, int d) : o(ws), m(ws + rows * splits_ * d), l(m + rows * splits_), splits(splits_) {}
+    static constexpr int SLOTS = 2 * 4 * KVA_CUS;
+    int32_t *before;
+    float *m, *l, *o;
+    static __host__ __device__ __forceinline__ size_t head(int n_seqs) { return ((size_t)n_seqs + 4) / 4 * 4; }
+    __device__ __forceinline__ KvPartial(void *ws, int n_seqs)
+        : before(static_cast<int32_t *>(ws)), m(reinterpret_cast<float *>(before + head(n_seqs))), l(m + SLOTS * KVA_ROWS), o(l + SLOTS * KVA_ROWS) {}
+    static size_t bytes(int n_seqs, int d) { return head(n_seqs) * 4 + (size_t)SLOTS * KVA_ROWS * (2 + d) * 4; }
+};
+__device__ __forceinline__ int kv_parts(int tiles, int share) { return (int)((uint32_t)(tiles + share - 1) / (uint32_t)share); }
+// inclusive sum over the lanes up to this one
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);       // row_shr 1, 2, 4, 8: within rows of sixteen
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);       // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);       // row_bcast:31 into rows 2 and 3
+    return x;
+}
+// n / d of numbers whose product is below 2^32, by a multiplication
+struct KvDivide {
+    uint32_t magic;
+    KvDivide(int d) : magic(d == 1 ? 0u : (uint32_t)(((1ULL << 32) + d - 1) / (uint32_t)d)) {}
+    __device__ __forceinline__ int operator()(int n) const { return magic ? (int)__umulhi((uint32_t)n, magic) : n; }
 };
 
 // A tile as it is loaded: a lane's runs, and the headers of its positions.
@@ -46,261 +105,377 @@ struct KvTileRegs {
     kv_u32x4 vh[T::NB][2];                                    // scales, offsets of its eight positions, by block
 };
 
-template <typename T>
-__global__ __launch_bounds__(64 * KVA_WAVES) void kv_attn_kernel(KvView v, const uint16_t *__restrict__ q, int n_heads, int group, float scale_log2e, int chunk, int nsplit,
-                                                                 int pieces, uint16_t *__restrict__ out, float *__restrict__ ws)
+// DIRECT: a workgroup is a line.
+template <typename T, int WAVES, bool DIRECT>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv_attn_kernel(KvView v, const uint16_t *__restrict__ q, int n_heads, int group, KvDivide by_group,
+                                                                                           KvDivide by_heads, float scale_log2e, uint16_t *__restrict__ out, void *ws)
 {
     constexpr int D = T::D, NU = D / 32, NC = D / 16;
-    __shared__ float s_o[KVA_WAVES][KVA_ROWS][D];
-    __shared__ float s_m[KVA_WAVES][KVA_ROWS], s_l[KVA_WAVES][KVA_ROWS];
-    const int tid = threadIdx.x, lane = tid & 63;
+    constexpr int PAD = 4;                                    // floats: rows four apart in banks of their own
+    __shared__ __align__(16) float s_o[WAVES][KVA_ROWS][D + PAD];
+    __shared__ float s_m[WAVES][KVA_ROWS], s_l[WAVES][KVA_ROWS];
+    const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int li = lane & 15, g = lane >> 4;
-    // workgroup -> (sequence, key/value head, range, piece of rows)
-    int at = blockIdx.x;
-    const int piece = at % pieces; at /= pieces;
-    const int sp = at % nsplit; at /= nsplit;
-    const int head = at % v.n_kv_heads, b = at / v.n_kv_heads;
-    const KvSequence seq(v, b);
-    const int r0 = piece * KVA_ROWS, rows = min(KVA_ROWS, seq.count * group - r0);
-    if (rows <= 0) return;
-    const int longest = seq.sees((r0 + rows - 1) / group);    // the last row sees most
-    const int t_begin = sp * chunk;
-    if (t_begin >= longest && sp > 0) return;
-    const int t_end = min(longest, t_begin + chunk);
-    const int mine = longest > chunk ? (longest + chunk - 1) / chunk : 1;      // ranges that this piece's rows have
+    const KvPartial part(ws, v.n_seqs);
 
-    const int my_row = r0 + min(li, rows - 1), token = my_row / group;
-    const int64_t my_out = (seq.row + token) * n_heads + head * group + (my_row - token * group);
-    const bool real = li < rows && seq.has_row(token);
-    const int limit = seq.sees(token);
-    // queries as B operands: lane (row li, g) holds components g D/4 + 8u .. +8
-    kv_half8 qb[NU];
-#pragma unroll
-    for (int u = 0; u < NU; ++u) {
-        kv_u32x4 w = {0u, 0u, 0u, 0u};
-        if (real) w = *reinterpret_cast<const kv_u32x4 *>(q + my_out * D + g * (D / 4) + 8 * u);
-        qb[u] = __builtin_bit_cast(kv_half8, w);
-    }
-
-    // this wavefront's tiles: first + 4 n; lane n knows where tile n is
-    const int first = t_begin / KV_TILE + wave, tiles = max(0, ((t_end + KV_TILE - 1) / KV_TILE - first + KVA_WAVES - 1) / KVA_WAVES);
-    uint64_t my_tile = 0;
-    if (lane < tiles) my_tile = reinterpret_cast<uint64_t>(kv_tile_at(v, b, head, first + KVA_WAVES * lane, T::BYTES));
-    auto tile_address = [&](int n) {
-        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)my_tile, n), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(my_tile >> 32), n);
-        return (uint64_t)hi << 32 | lo;
-    };
-    // A tile is a buffer that ends with it, and is empty past the range and where its page is none: then zeros arrive, without a branch and without a request.
-    auto load = [&](KvTileRegs<T> &x, int n) {
-        const uint64_t address = n < tiles ? tile_address(n) : 0;
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(address), 0, address ? T::BYTES : 0, 0x00027000);
-        auto b128 = [&](int byte) { return __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, byte, 0, 2)); };
-#pragma unroll
-        for (int i = 0; i < T::PIECES; ++i) x.k[i] = b128(lane * 16 + i * 1024);
-        const auto h = __builtin_amdgcn_raw_buffer_load_b64(rsrc, T::KH_AT + ((g * (D / 4) / T::BLOCK) * 16 + li) * 8, 0, 2);
-        x.kh[0] = h[0]; x.kh[1] = h[1];
-#pragma unroll
-        for (int i = 0; i < T::PIECES; ++i) x.v[i] = b128(T::V_AT + lane * 16 + i * 1024);
-#pragma unroll
-        for (int i = 0; i < T::NB; ++i) {
-            x.vh[i][0] = b128(T::VH_AT + (i * 4 + g) * 32);
-            x.vh[i][1] = b128(T::VH_AT + (i * 4 + g) * 32 + 16);
+    const int lane = tid & 63, li = lane & 15, g = lane >> 4;
+    // which sequence, which line and part of it, and where the sequence's partial results begin
+    int b = 0, at = 0, slots = 0, share = 0;
+    if constexpr (DIRECT) {
+        b = blockIdx.y;
+    } else {
+        auto lines_of = [&](int s) {
+            if (s >= v.n_seqs) return KvLines{0, 0};
+            const KvSequence seq(v, s);
+            return kv_lines_of(v, seq, group);
+        };
+        auto last = [](int x) { return __builtin_amdgcn_readlane(x, 63); };
+        KvLines mine = lines_of(lane);                        // (the first 64 sequences are all in most calls)
+        int total = last(wave_scan(mine.tiles * mine.lines)), lines = last(wave_scan(mine.lines));
+        for (int s = 64; s < v.n_seqs; s += 64) {
+            const KvLines x = lines_of(s + lane);
+            total += last(wave_scan(x.tiles * x.lines)); lines += last(wave_scan(x.lines));
         }
-    };
-
-    float m = -INFINITY, l = 0.f;                             // of row li (m is the same in the row's four lanes)
-    kv_float4 oacc[NC];                                       // oacc[c][e] = O[row 4g+e][16c + li]
-#pragma unroll
-    for (int c = 0; c < NC; ++c) oacc[c] = (kv_float4){0.f, 0.f, 0.f, 0.f};
-
-    auto process = [&](KvTileRegs<T> &x, int n) {
-        const int p0 = (first + KVA_WAVES * n) * KV_TILE;
-        const bool there = tile_address(n) != 0;
-        // scores
-        kv_float4 sacc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const half2_t pair = as_h2(x.kh[h]), sc = {pair.x, pair.x}, of = {pair.y, pair.y};
-#pragma unroll
-            for (int u = 0; u < NU; ++u) {
-                constexpr int W = 8 / T::PER_WORD;            // words of eight components
-                const int word = (h * NU + u) * W;
-                uint32_t w[2] = {x.k[word / 4][word % 4], W == 2 ? x.k[word / 4][(word + W - 1) % 4] : 0u};
-                KvPairs a = kv_levels<T::BITS>(w);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) a.p[e] = kv_value(a.p[e], sc, of);
-                sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(kv_half8, a), qb[u], sacc[h], 0, 0, 0);
-            }
-        }
-        float sc[8], bm = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {                         // position p0 + 16 (e / 4) + 4g + e % 4, row li
-            sc[e] = there && p0 + 16 * (e >> 2) + 4 * g + (e & 3) < limit ? sacc[e >> 2][e & 3] * scale_log2e : -INFINITY;
-            bm = fmaxf(bm, sc[e]);
-        }
-        bm = kva_max_of_rows(bm);
-        const bool follow = bm > m + KVA_LAG;                 // (the first tile with a score above -inf: always)
-        if (__builtin_amdgcn_ballot_w64(follow) != 0) {
-            const float alpha = follow ? __builtin_amdgcn_exp2f(m - (bm - KVA_BELOW)) : 1.0f;
-            l *= alpha;
-            m = follow ? bm - KVA_BELOW : m;
-            float al[4];                                      // the accumulators hold rows 4g .. 4g+3: their factors live in lanes 4g .. 4g+3
-#pragma unroll
-            for (int e = 0; e < 4; ++e) al[e] = __shfl(alpha, 4 * g + e);
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) oacc[c][e] *= al[e];
-        }
-        const float base = (m == -INFINITY) ? 0.f : m;        // (a row that has seen nothing: no -inf - -inf)
-        kv_half8 pa, pr;                                      // the probabilities as two fp16 numbers
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float p = __builtin_amdgcn_exp2f(sc[e] - base);                     // exp2(-inf) = 0 for masked positions
-            l += p;
-            pa[e] = (_Float16)p;
-            pr[e] = (_Float16)(p - (float)pa[e]);
-        }
-        // what lies behind the last position that a row sees may be anything, also no number: its values are zeros
-        if (p0 + KV_TILE > t_end) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int p = p0 + 16 * (e >> 1) + 4 * g + 2 * (e & 1);
-                const uint32_t keep = p + 1 < t_end ? 0xFFFFFFFFu : p < t_end ? 0x0000FFFFu : 0u;
-#pragma unroll
-                for (int i = 0; i < T::NB; ++i) { x.vh[i][0][e] &= keep; x.vh[i][1][e] &= keep; }
-            }
-        }
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            constexpr int W = 8 / T::PER_WORD;
-            const int word = c * W, block = c * 16 / T::BLOCK;
-            uint32_t w[2] = {x.v[word / 4][word % 4], W == 2 ? x.v[word / 4][(word + W - 1) % 4] : 0u};
-            KvPairs a = kv_levels<T::BITS>(w);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) a.p[e] = kv_value(a.p[e], as_h2(x.vh[block][0][e]), as_h2(x.vh[block][1][e]));
-            oacc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pa, __builtin_bit_cast(kv_half8, a), oacc[c], 0, 0, 0);
-            oacc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pr, __builtin_bit_cast(kv_half8, a), oacc[c], 0, 0, 0);
-        }
-    };
-
-    KvTileRegs<T> xa, xb;
-    load(xa, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    load(xb, 1);
-    __builtin_amdgcn_sched_barrier(0);
-    for (int n = 0; n < tiles; n += 2) {
-        process(xa, n);
-        __builtin_amdgcn_sched_barrier(0);
-        load(xa, n + 2);
-        __builtin_amdgcn_sched_barrier(0);
-        if (n + 1 < tiles) process(xb, n + 1);
-        __builtin_amdgcn_sched_barrier(0);
-        load(xb, n + 3);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-
-    // ---- merge the four wavefronts' states --------------------------------------------------------------------------------
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (g == 0) { s_m[wave][li] = m; s_l[wave][li] = l; }
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s_o[wave][4 * g + e][16 * c + li] = oacc[c][e];
-    __syncthreads();
-    const KvPartial part(ws, v.n_tokens * n_heads, nsplit, D);
-#pragma unroll
-    for (int i = 0; i < KVA_ROWS * D / (64 * KVA_WAVES); ++i) {
-        const int idx = tid + i * 64 * KVA_WAVES, r = idx / D, d = idx & (D - 1);
-        const int tok = (r0 + r) / group;
-        if (r >= rows || !seq.has_row(tok)) continue;
-        float M = s_m[0][r];
-#pragma unroll
-        for (int w = 1; w < KVA_WAVES; ++w) M = fmaxf(M, s_m[w][r]);
-        const float base = M == -INFINITY ? 0.f : M - KVA_SPARE;
-        float L = 0.f, O = 0.f;
-#pragma unroll
-        for (int w = 0; w < KVA_WAVES; ++w) {
-            const float f = __builtin_amdgcn_exp2f(s_m[w][r] - base);                 // (nothing seen: zero)
-            L = __builtin_fmaf(s_l[w][r], f, L);
-            O = __builtin_fmaf(s_o[w][r][d], f, O);
-        }
-        const int64_t to = (seq.row + tok) * n_heads + head * group + (r0 + r - tok * group);
-        if (mine == 1) {
-            out[to * D + d] = as_u16((half_t)(L > 0.f ? O / L : 0.f));
+        // The parts' tiles: one for each wavefront where all are few, else at least two (a part costs about as much as four tiles besides).  The fewest that leave no more parts than the device
+        // holds at once, for what does not fit waits for a whole part; where there are half as many lines already, 1 / capacity of all tiles: parts are then about as many again as lines.
+        constexpr int UNIT = WAVES, CAPACITY = KVA_PER_CU<T> * KVA_CUS;
+        if (lines > CAPACITY / 2) {
+            share = max(2 * UNIT, (total / CAPACITY + UNIT) / UNIT * UNIT);
+        } else if (v.n_seqs > 64) {
+            share = max(2 * UNIT, (total / (CAPACITY - lines) + UNIT) / UNIT * UNIT);      // (a line has less than one part more than its tiles over a part's)
         } else {
-            part.o[(to * nsplit + sp) * D + d] = O;
-            if (d == 0) { part.m[to * nsplit + sp] = M == -INFINITY ? M : base; part.l[to * nsplit + sp] = L; }
+            share = total <= KVA_CUS * UNIT ? UNIT : max(2 * UNIT, (total / (CAPACITY - lines / 2) + UNIT - 1) / UNIT * UNIT);
+            while (last(wave_scan(mine.lines * kv_parts(mine.tiles, share))) > CAPACITY) share += UNIT;
+        }
+        const bool clerk = blockIdx.x == gridDim.x - 1;       // the last workgroup writes down what the merge wants to know
+        if (clerk && wave > 0) return;
+        at = blockIdx.x;
+        for (;;) {
+            const int parts = kv_parts(mine.tiles, share), work = mine.lines * parts, upto = wave_scan(work), held = parts > 1 ? work : 0, held_upto = wave_scan(held);
+            if (clerk) {
+                if (b + lane < v.n_seqs) part.before[b + lane] = slots + held_upto - held;
+                if (b == 0 && lane == 0) part.before[v.n_seqs] = share;
+            } else {
+                const uint64_t mask = __builtin_amdgcn_ballot_w64(upto > at);
+                if (mask != 0) {
+                    const int skip = __builtin_ctzll(mask);
+                    b += skip;
+                    at -= __builtin_amdgcn_readlane(upto - work, skip);
+                    slots += __builtin_amdgcn_readlane(held_upto - held, skip);
+                    break;
+                }
+                at -= last(upto);
+            }
+            slots += last(held_upto);
+            b += 64;
+            if (b >= v.n_seqs) return;                        // (there are more workgroups than parts)
+            mine = lines_of(b + lane);
+        }
+    }
+    const KvSequence seq(v, b);
+    const KvLines x = kv_lines_of(v, seq, group);
+    if (DIRECT && (int)blockIdx.x >= x.lines) return;
+    const int parts = DIRECT ? 1 : kv_parts(x.tiles, share);
+    const int line = DIRECT ? blockIdx.x : __builtin_amdgcn_readfirstlane((int)((uint32_t)at / (uint32_t)parts)), my_part = at - line * parts;
+    // (parts as long as one another, in whole tiles for each wavefront)
+    const int per = DIRECT ? x.tiles : min(share, (kv_parts(x.tiles, parts) + WAVES - 1) / WAVES * WAVES), t0 = DIRECT ? 0 : my_part * per, n_tiles = min(per, x.tiles - t0);
+    const int piece = by_heads(line), head = line - piece * v.n_kv_heads;
+    const KvMagic magic;
+    {
+        const int r0 = piece * KVA_ROWS, rows = min(KVA_ROWS, seq.count * group - r0);
+        const int longest = seq.sees(by_group(r0 + rows - 1)), shortest = seq.sees(by_group(r0));      // the last row sees most
+        const int my_row = r0 + min(li, rows - 1), token = by_group(my_row);
+        const int64_t my_out = (int64_t)(seq.row + token) * n_heads + head * group + (my_row - token * group);
+        const int limit = seq.sees(token);
+        // queries as B operands: lane (row li, g) holds components g D/4 + 8u .. +8
+        kv_half8 qb[NU];
+        const bool real = li < rows && seq.has_row(token);
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+            kv_u32x4 w = {0u, 0u, 0u, 0u};
+            if (real) w = *reinterpret_cast<const kv_u32x4 *>(q + my_out * D + g * (D / 4) + 8 * u);
+            qb[u] = __builtin_bit_cast(kv_half8, w);
+        }
+        float m = -INFINITY, l = 0.f;                         // of row li (m is the same in the row's four lanes)
+        kv_float4 oacc[NC];                                   // oacc[c][e] = O[row 4g+e][16c + li]
+#pragma unroll
+        for (int c = 0; c < NC; ++c) oacc[c] = (kv_float4){0.f, 0.f, 0.f, 0.f};
+
+        // 256 tiles at a time; this wavefront's: first + 4 n, and lane n knows where tile n is
+        for (int done = 0; done < n_tiles; done += 64 * WAVES) {
+            const int first = t0 + done + wave, last = min(t0 + min(n_tiles, done + 64 * WAVES), (longest + KV_TILE - 1) / KV_TILE);
+            const int tiles = __builtin_amdgcn_readfirstlane(max(0, (last - first + WAVES - 1) / WAVES));       // (the same for the wavefront, as the compiler is told)
+            uint64_t my_tile = 0;
+            if (lane < tiles) my_tile = reinterpret_cast<uint64_t>(kv_tile_at(v, b, head, first + WAVES * lane, T::BYTES));
+            auto tile_address = [&](int n) {
+                const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)my_tile, n), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(my_tile >> 32), n);
+                return (uint64_t)hi << 32 | lo;
+            };
+            // A tile is a buffer that ends with it, and is empty past the range and where its page is none: then zeros arrive, without a branch and without a request.
+            auto tile_buffer = [&](int n) {
+                const uint64_t address = n < tiles ? tile_address(n) : 0;
+                return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(address), 0, address ? T::BYTES : 0, 0x00027000);
+            };
+            auto load_keys = [&](KvTileRegs<T> &y, int n) {
+                const auto rsrc = tile_buffer(n);
+#pragma unroll
+                for (int i = 0; i < T::PIECES; ++i) y.k[i] = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane * 16 + i * 1024, 0, 2));
+                const auto h = __builtin_amdgcn_raw_buffer_load_b64(rsrc, T::KH_AT + ((g * (D / 4) / T::BLOCK) * 16 + li) * 8, 0, 2);
+                y.kh[0] = h[0]; y.kh[1] = h[1];
+            };
+            auto load_values = [&](KvTileRegs<T> &y, int n) {
+                const auto rsrc = tile_buffer(n);
+#pragma unroll
+                for (int i = 0; i < T::PIECES; ++i) y.v[i] = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, T::V_AT + lane * 16 + i * 1024, 0, 2));
+#pragma unroll
+                for (int i = 0; i < T::NB; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) y.vh[i][j] = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, T::VH_AT + (i * 4 + g) * 32 + 16 * j, 0, 2));
+            };
+
+            KvTileRegs<T> y;
+            // (Scheduling barriers: the waits count requests, so keys and values have to be requested in the same order in front of the loop and in it, or a wait becomes one for everything.)
+            __builtin_amdgcn_sched_barrier(0);
+            load_keys(y, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            load_values(y, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            for (int n = 0; n < tiles; ++n) {
+                const int p0 = (first + WAVES * n) * KV_TILE;
+                // scores
+                kv_float4 sacc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const half2_t pair = as_h2(y.kh[h]), sc = {pair.x, pair.x}, of = {pair.y, pair.y};
+#pragma unroll
+                    for (int u = 0; u < NU; ++u) {
+                        constexpr int W = 8 / T::PER_WORD;    // words of eight components
+                        const int word = (h * NU + u) * W;
+                        uint32_t w[2] = {y.k[word / 4][word % 4], W == 2 ? y.k[word / 4][(word + W - 1) % 4] : 0u};
+                        KvPairs a = kv_levels<T::BITS>(w, magic);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) a.p[e] = kv_value(a.p[e], sc, of);
+                        sacc[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(kv_half8, a), qb[u], sacc[h], 0, 0, 0);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                load_keys(y, n + 1);                          // (into the registers that have just been read)
+                __builtin_amdgcn_sched_barrier(0);
+                // position p0 + 16 (e / 4) + 4g + e % 4, row li: not seen from the row's limit on, nor on a page that is not there
+                const bool there = tile_address(n) != 0;
+                if (!there || p0 + KV_TILE > shortest) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (!there || p0 + 16 * (e >> 2) + 4 * g + (e & 3) >= limit) sacc[e >> 2][e & 3] = -INFINITY;
+                }
+                float bm = kv_max3(kv_max3(kv_max3(sacc[0][0], sacc[0][1], sacc[0][2]), sacc[0][3], sacc[1][0]), kv_max3(sacc[1][1], sacc[1][2], sacc[1][3]), -INFINITY);
+                bm = kva_max_of_rows(bm) * scale_log2e;
+                const bool follow = bm > m + KVA_LAG;         // (the first tile with a score above -inf: always)
+                if (__builtin_amdgcn_ballot_w64(follow) != 0) {
+                    const float alpha = follow ? __builtin_amdgcn_exp2f(m - (bm - KVA_BELOW)) : 1.0f;
+                    const bool nothing = __builtin_amdgcn_ballot_w64(m != -INFINITY) == 0;
+                    l *= alpha;
+                    m = follow ? bm - KVA_BELOW : m;
+                    if (!nothing) {                           // the accumulators hold rows 4g .. 4g+3: their factors live in lanes 4g .. 4g+3
+                        float al[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) al[e] = __shfl(alpha, 4 * g + e);
+#pragma unroll
+                        for (int c = 0; c < NC; ++c)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) oacc[c][e] *= al[e];
+                    }
+                }
+                const float below = (m == -INFINITY) ? 0.f : -m;       // (a row that has seen nothing: no -inf - -inf)
+                // the probabilities as two fp16 numbers, the first cut off so that both are positive: together within 2^-21 of them
+                KvPairs pa, pr;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p0e = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e >> 1][2 * (e & 1)], scale_log2e, below));          // exp2(-inf) = 0 for masked positions
+                    const float p1e = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e >> 1][2 * (e & 1) + 1], scale_log2e, below));
+                    l += p0e; l += p1e;
+                    pa.p[e] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(p0e, p1e));
+                    pr.p[e] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(kv_less_low(p0e, pa.p[e]), kv_less_high(p1e, pa.p[e])));
+                }
+                // what lies behind the last position that a row sees may be anything, also no number: its values are zeros
+                if (p0 + KV_TILE > longest) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int p = p0 + 16 * (e >> 1) + 4 * g + 2 * (e & 1);
+                        const uint32_t keep = p + 1 < longest ? 0xFFFFFFFFu : p < longest ? 0x0000FFFFu : 0u;
+#pragma unroll
+                        for (int i = 0; i < T::NB; ++i) { y.vh[i][0][e] &= keep; y.vh[i][1][e] &= keep; }
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    constexpr int W = 8 / T::PER_WORD;
+                    const int word = c * W, block = c * 16 / T::BLOCK;
+                    uint32_t w[2] = {y.v[word / 4][word % 4], W == 2 ? y.v[word / 4][(word + W - 1) % 4] : 0u};
+                    KvPairs a = kv_levels<T::BITS>(w, magic);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a.p[e] = kv_value(a.p[e], as_h2(y.vh[block][0][e]), as_h2(y.vh[block][1][e]));
+                    oacc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(kv_half8, pa), __builtin_bit_cast(kv_half8, a), oacc[c], 0, 0, 0);
+                    oacc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(kv_half8, pr), __builtin_bit_cast(kv_half8, a), oacc[c], 0, 0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                load_values(y, n + 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+
+        // ---- merge the four wavefronts' states ----------------------------------------------------------------------------
+        int id = tid;
+        asm volatile("" : "+v"(id));                          // (the addresses below are made here, not kept in registers through the tiles)
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if ((id & 48) == 0) { s_m[wave][id & 15] = m; s_l[wave][id & 15] = l; }
+        float *my_o = &s_o[wave][4 * (id >> 4 & 3)][id & 15];
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) my_o[e * (D + PAD) + 16 * c] = oacc[c][e];
+        __syncthreads();
+        const int slot = min(slots + at, KvPartial::SLOTS - 1);      // (below that; also where another stream changes the lengths meanwhile)
+        constexpr int QUADS = D / 4;                          // a thread takes four components of a row
+#pragma unroll
+        for (int i = 0; i < (KVA_ROWS * QUADS + 64 * WAVES - 1) / (64 * WAVES); ++i) {
+            const int r = id / QUADS + i * (64 * WAVES / QUADS), d = id % QUADS * 4, tok = by_group(r0 + r);
+            if (KVA_ROWS * QUADS < 64 * WAVES && r >= KVA_ROWS) break;        // (64 components, eight wavefronts: half the threads)
+            float M = s_m[0][r];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) M = fmaxf(M, s_m[w][r]);
+            const float to_base = M == -INFINITY ? 0.f : M - KVA_SPARE;
+            float L = 0.f;
+            kv_float4 O = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const float f = __builtin_amdgcn_exp2f(s_m[w][r] - to_base);          // (nothing seen: zero)
+                const kv_float4 o = *reinterpret_cast<const kv_float4 *>(&s_o[w][r][d]);
+                L = __builtin_fmaf(s_l[w][r], f, L);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[e] = __builtin_fmaf(o[e], f, O[e]);
+            }
+            if (parts == 1) {
+                if (r < rows && seq.has_row(tok)) {
+                    const float div = L > 0.f ? L : 1.f;      // (nothing seen: zeros)
+                    const half2_t a = {(half_t)(O[0] / div), (half_t)(O[1] / div)}, c = {(half_t)(O[2] / div), (half_t)(O[3] / div)};
+                    const int64_t to = (int64_t)(seq.row + tok) * n_heads + head * group + (r0 + r - tok * group);
+                    *reinterpret_cast<kv_u32x2 *>(out + to * D + d) = (kv_u32x2){as_u32(a), as_u32(c)};
+                }
+            } else {
+                *reinterpret_cast<kv_float4 *>(part.o + (slot * KVA_ROWS + r) * D + d) = O;
+                if (d == 0) { part.m[slot * KVA_ROWS + r] = M == -INFINITY ? M : to_base; part.l[slot * KVA_ROWS + r] = L; }
+            }
         }
     }
 }
 
-// Merge of the ranges: one workgroup of D threads per (sequence, token, query head).
-__global__ void kv_attn_merge_kernel(KvView v, int n_heads, int group, int d_head, int chunk, int nsplit, const float *__restrict__ ws, uint16_t *__restrict__ out)
+// Merge of a line's partial results: one workgroup per (sequence, token, query head), thread (d, u) for component d of results 8u .. 8u + 7, then 8 (u + groups) ..: a group's eight are requested
+// at once, and the groups' states meet in LDS and are added in order.
+constexpr int KVA_MERGE = 8;
+__global__ __launch_bounds__(1024) void kv_attn_merge_kernel(KvView v, int n_heads, int group, void *ws, uint16_t *__restrict__ out)
 {
-    const int h = blockIdx.x % n_heads, i = blockIdx.x / n_heads % v.max_tokens, b = blockIdx.x / n_heads / v.max_tokens, d = threadIdx.x;
+    __shared__ float s_o[8][128], s_m[8], s_l[8];
+    const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z, D = blockDim.x, d = threadIdx.x, groups = blockDim.y, u = threadIdx.y;
+    const KvPartial part(ws, v.n_seqs);
+    const int before = part.before[b], share = part.before[v.n_seqs];
     const KvSequence seq(v, b);
     if (!seq.has_row(i)) return;
-    const int piece = (i * group + h % group) / KVA_ROWS, last = min(seq.count * group, (piece + 1) * KVA_ROWS) - 1;
-    const int longest = seq.sees(last / group), mine = longest > chunk ? (longest + chunk - 1) / chunk : 1;
+    const KvLines x = kv_lines_of(v, seq, group);
+    const int row = i * group + h % group, piece = row / KVA_ROWS, r = row % KVA_ROWS, line = piece * v.n_kv_heads + h / group;
+    const int mine = kv_parts(x.tiles, share);
     if (mine == 1) return;                                    // (written by the first launch)
-    const KvPartial part(const_cast<float *>(ws), v.n_tokens * n_heads, nsplit, d_head);
-    const int64_t to = (seq.row + i) * n_heads + h;
-    float M = -INFINITY;
-    for (int s = 0; s < mine; ++s) M = fmaxf(M, part.m[to * nsplit + s]);
-    const float base = M == -INFINITY ? 0.f : M - KVA_SPARE;
-    float L = 0.f, O = 0.f;
-    for (int s = 0; s < mine; ++s) {
-        const float f = __builtin_amdgcn_exp2f(part.m[to * nsplit + s] - base);
-        L = __builtin_fmaf(part.l[to * nsplit + s], f, L);
-        O = __builtin_fmaf(part.o[(to * nsplit + s) * d_head + d], f, O);
+    auto slot = [&](int s) { return min(before + line * mine + s, KvPartial::SLOTS - 1) * KVA_ROWS + r; };
+    float M = -INFINITY, L = 0.f, O = 0.f;                    // relative to to_base(M)
+    auto to_base = [](float m) { return m == -INFINITY ? 0.f : m - KVA_SPARE; };
+    for (int s0 = u * KVA_MERGE; s0 < mine; s0 += groups * KVA_MERGE) {
+        float m[KVA_MERGE], l[KVA_MERGE], o[KVA_MERGE], top = M;
+#pragma unroll
+        for (int e = 0; e < KVA_MERGE; ++e) {
+            const int s = slot(min(s0 + e, mine - 1));    // past the end: the last one again, with no weight
+            m[e] = part.m[s]; l[e] = part.l[s]; o[e] = part.o[s * D + d];
+        }
+#pragma unroll
+        for (int e = 0; e < KVA_MERGE; ++e) top = fmaxf(top, m[e]);
+        const float now = to_base(top), again = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to_base(M) - now);
+        L *= again; O *= again;
+        M = top;
+#pragma unroll
+        for (int e = 0; e < KVA_MERGE; ++e) {
+            const float f = s0 + e < mine ? __builtin_amdgcn_exp2f(m[e] - now) : 0.f;
+            L = __builtin_fmaf(l[e], f, L);
+            O = __builtin_fmaf(o[e], f, O);
+        }
     }
-    out[to * d_head + d] = as_u16((half_t)(L > 0.f ? O / L : 0.f));
+    if (groups > 1) {
+        s_o[u][d] = O;
+        if (d == 0) { s_m[u] = M; s_l[u] = L; }
+        __syncthreads();
+        if (u > 0) return;
+        for (int e = 1; e < groups; ++e) M = fmaxf(M, s_m[e]);
+        L = 0.f; O = 0.f;
+        for (int e = 0; e < groups; ++e) {
+            const float f = s_m[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to_base(s_m[e]) - to_base(M));
+            L = __builtin_fmaf(s_l[e], f, L);
+            O = __builtin_fmaf(s_o[e][d], f, O);
+        }
+    }
+    out[((int64_t)(seq.row + i) * n_heads + h) * D + d] = as_u16((half_t)(L > 0.f ? O / L : 0.f));
 }
 
-// Positions of a range and the number of ranges: about two workgroups per compute unit (of the 256 that a whole device has), none of fewer than 256 positions.
-struct KvAttnGeometry { int chunk, nsplit, pieces; };
-static KvAttnGeometry kv_attn_geometry(const KvView &v, int n_heads)
+// Whether a line is a workgroup's, without a second launch, and of how many wavefronts then (0: lines are cut).  Us (graph replay; one page table, lengths an eighth to the whole), cut / direct with four
+// wavefronts / with eight, for the longest sequence's positions:
+//                                        512               768               1024              2048
+//   32/8 heads x 128, 4 bits,  8 lines   8.0 / 6.5 / 6.0   8.3 / 8.5 / 7.6   8.4 / 10.2 / 9.1  8.7 / 16.9 / 14.4
+//                             64 lines   8.6 / 7.0 / 6.5   8.6 / 8.7 / 7.9   9.6 / 10.5 / 9.4  12.2 / 17.2 / 14.7
+//                            512 lines   18.6 / 10.1 / 12  20.9 / 13.1 / 15  22.8 / 15.6 / 18  31.0 / 26.6 / 27.8
+//   32/32 heads x 128, 8 bits, 256       12.6 / 8.7 / 8.3  15.0 / 10.3 / 9.8 16.6 / 12.9 / 12  24.9 / 21.7 / 20.4
+//   71/1 heads x 64, 4 bits,   5         7.3 / 5.5 / 5.2   7.3 / 6.6 / 6.0   7.3 / 7.7 / 6.9   7.8 / 12.2 / 11
+//                            320         11.9 / 7.8 / 7.8  14.0 / 9.6 / 9.4  15.5 / 10.9 / 10.4 18.3 / 16.9 / 15.9
+// The boundaries lie where the longest line alone takes as long as the parts and their merge, and later where there is a line for every compute unit.
+constexpr int KVA_SPLIT_WAVES = 4;
+static int64_t kv_attn_lines(const KvView &v, int n_heads)    // of a sequence, at most
 {
-    const int group = n_heads / v.n_kv_heads;
-    KvAttnGeometry r;
-    r.pieces = (int)(((int64_t)v.max_tokens * group + KVA_ROWS - 1) / KVA_ROWS);
-    const int64_t workgroups = (int64_t)v.n_seqs * v.n_kv_heads * r.pieces;
-    int64_t want = (512 + workgroups - 1) / workgroups;
-    int64_t chunk = (v.max_seq + want - 1) / want;
-    const int64_t unit = KV_TILE * KVA_WAVES;
-    chunk = (chunk + unit - 1) / unit * unit;
-    if (chunk < 2 * unit) chunk = 2 * unit;
-    if (chunk > KVA_MAX_CHUNK) chunk = KVA_MAX_CHUNK;
-    r.chunk = (int)chunk;
-    r.nsplit = (int)((v.max_seq + chunk - 1) / chunk);
-    return r;
+    return v.n_kv_heads * (((int64_t)v.max_tokens * (n_heads / v.n_kv_heads) + KVA_ROWS - 1) / KVA_ROWS);
+}
+static int kv_attn_direct(const KvView &v, int head_dim, int n_heads)
+{
+    const int64_t tiles = (v.max_seq + KV_TILE - 1) / KV_TILE, lines = v.n_seqs * kv_attn_lines(v, n_heads);
+    const int waves = head_dim == 64 || lines < 256 ? 8 : 4;
+    if (lines * tiles > (1LL << 30)) return waves;            // (more tiles than the cut counts in 32 bits)
+    return v.max_seq <= (lines >= 256 ? 2560 : head_dim == 64 ? 1024 : 768) ? waves : 0;
 }
 
 size_t kv_attn_workspace_bytes(const KvView &v, int head_dim, int n_heads)
 {
-    const KvAttnGeometry geo = kv_attn_geometry(v, n_heads);
-    return geo.nsplit == 1 ? 0 : (size_t)v.n_tokens * n_heads * geo.nsplit * (head_dim + 2) * sizeof(float);
+    return kv_attn_direct(v, head_dim, n_heads) ? 0 : KvPartial::bytes(v.n_seqs, head_dim);
 }
 
 hipError_t launch_kv_attn(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace, hipStream_t s)
 {
-    const KvAttnGeometry geo = kv_attn_geometry(v, n_heads);
     const int group = n_heads / v.n_kv_heads;
-    const int64_t grid = (int64_t)v.n_seqs * v.n_kv_heads * geo.nsplit * geo.pieces;
-    const int64_t merge = (int64_t)v.n_seqs * v.max_tokens * n_heads;
-    if (geo.nsplit > KVA_MAX_SPLITS || grid > 0x7fffffff || merge > 0x7fffffff) return hipErrorInvalidValue;
+    const int64_t lines = kv_attn_lines(v, n_heads);
+    const float scale_log2e = scale * 1.4426950408889634f;
+    const int direct = kv_attn_direct(v, head_dim, n_heads);
+    if (v.max_tokens > 65535) return hipErrorInvalidValue;
+    const KvDivide by_group(group), by_heads(v.n_kv_heads);
     hipError_t e = for_kv_tile(format, head_dim, [&](auto tag) {
         typedef decltype(tag) T;
-        hipLaunchKernelGGL((kv_attn_kernel<T>), dim3((unsigned)grid), dim3(64 * KVA_WAVES), 0, s, v, q, n_heads, group, scale * 1.4426950408889634f, geo.chunk, geo.nsplit, geo.pieces,
-                           out, static_cast<float *>(workspace));
+#define IFLOW_KVA_GO(W, DIRECT, GRID) hipLaunchKernelGGL((kv_attn_kernel<T, W, DIRECT>), GRID, dim3(64 * W), 0, s, v, q, n_heads, group, by_group, by_heads, scale_log2e, out, workspace)
+        if (direct == 8) IFLOW_KVA_GO(8, true, dim3((unsigned)lines, (unsigned)v.n_seqs));
+        else if (direct) IFLOW_KVA_GO(4, true, dim3((unsigned)lines, (unsigned)v.n_seqs));
+        else IFLOW_KVA_GO(KVA_SPLIT_WAVES, false, dim3((unsigned)(KVA_PER_CU<T> * KVA_CUS + v.n_seqs * lines + 1)));
+#undef IFLOW_KVA_GO
         return hipGetLastError();
     });
-    if (e != hipSuccess || geo.nsplit == 1) return e;
-    hipLaunchKernelGGL(kv_attn_merge_kernel, dim3((unsigned)merge), dim3((unsigned)head_dim), 0, s, v, n_heads, group, head_dim, geo.chunk, geo.nsplit,
-                       static_cast<const float *>(workspace), out);
+    if (e != hipSuccess || direct) return e;
+    // Groups of threads for the results that a long line is likely to have: sequences as long as max_seq, or of several, half of it in the mean.
+    const int tiles = (v.max_seq + KV_TILE - 1) / KV_TILE;
+    const int64_t part = std::max<int64_t>(2 * KVA_SPLIT_WAVES, v.n_seqs * lines * tiles / (v.n_seqs > 1 ? 2 : 1) / (4 * KVA_CUS));
+    const int groups = (int)((tiles / part + 2 + KVA_MERGE - 1) / KVA_MERGE);
+    hipLaunchKernelGGL(kv_attn_merge_kernel, dim3((unsigned)n_heads, (unsigned)v.max_tokens, (unsigned)v.n_seqs), dim3((unsigned)head_dim, (unsigned)(groups > 8 ? 8 : groups)), 0, s, v,
+                       n_heads, group, workspace, out);
     return hipGetLastError();
 }
 

@@ -200,6 +200,17 @@ def test_attention_of_several_tokens(gpu, name, n_heads, n_kv, d, lens, counts):
     s.check_attend(s.queries(), d ** -0.5)
 
 
+@pytest.mark.parametrize("name,n_heads,n_kv,d,lens,counts", [("Q4_B64", 8, 2, 128, [2100, 5, 900, 0, 1024], None), ("Q8_B64", 4, 4, 128, [1300], None), ("Q4_B32", 40, 2, 64, [3000, 1, 700], [2, 1, 2]),
+                                                            ("Q8_B32", 3, 1, 64, [1500, 1281], None), ("Q4_B32", 5, 1, 128, [40] * 66 + [1500, 33], None), ("Q4_B64", 16, 1, 128, [9000], None)])
+def test_attention_over_parts_of_long_lines(gpu, name, n_heads, n_kv, d, lens, counts):  # noqa: F811
+    """Sequences that are cut and merged, among short ones that are not and ones of no length; more sequences than a wavefront has lanes."""
+    say(f"[case] kv attention in parts {name} {n_heads}/{n_kv} heads of {d}, {len(lens)} sequences to {max(lens)}")
+    s = Setup(gpu, name, n_kv, d, 64, lens, counts, 4200 + n_heads, n_heads)
+    s.fill()
+    s.describe()
+    s.check_attend(s.queries(), d ** -0.5)
+
+
 @pytest.mark.parametrize("counts", [None, [3], [150]])
 def test_attention_peaked_and_climbing_scores(gpu, counts):  # noqa: F811
     """Large scores: one position outweighs the rest, wherever it is, and scores that climb by up to 40 (log2) from tile to tile, each head by another step: the reference follows in some
@@ -342,11 +353,12 @@ def test_pages_beyond_32_bits(gpu):  # noqa: F811
 def test_refusals_name_themselves(gpu):  # noqa: F811
     torch, it = gpu
     say("[case] kv refusals")
-    s = Setup(gpu, "Q4_B64", 2, 64, 32, [700, 40], None, 4100, 4)
+    s = Setup(gpu, "Q4_B64", 2, 64, 32, [3000, 40], None, 4100, 4)      # (long enough for a workspace)
     s.describe()
     q = s.dev(s.queries())
     out = torch.zeros((2, 4, 64), dtype=torch.float16, device="cuda")
     need = it.kv_attn_workspace_bytes(s.d_cache, s.d_batch, 4)
+    assert need > 0
     ws = torch.zeros((need,), dtype=torch.uint8, device="cuda")
     for call, status in ((lambda: it.kv_attn(s.d_cache, s.d_batch, q, 4, 0.1, out, ws, need - 1), it.ERR_SIZE), (lambda: it.kv_attn(s.d_cache, s.d_batch, q, 3, 0.1, out, ws, need), it.ERR_SHAPE),
                          (lambda: it.kv_attn(s.d_cache, s.d_batch, q, 4, 0.1, q, ws, need), it.ERR_SHAPE), (lambda: it.kv_append(s.d_cache, s.d_batch, q, out, q, 4, BASE, 1, out), it.ERR_SHAPE)):

@@ -100,7 +100,7 @@ def test_refusals_before_any_launch(iflow):  # noqa: F811
     for bad in (dict(head_dim=96), dict(head_dim=256), dict(n_kv_heads=0), dict(n_kv_heads=65), dict(page_positions=0), dict(page_positions=48), dict(page_positions=(1 << 20) + 32),
                 dict(n_pages=0), dict(n_pages=1 << 31), dict(n_pages=(1 << 31) - 1, page_positions=1 << 20)):
         refused(iflow.ERR_SHAPE, cache=bad)
-    for bad in (dict(n_seqs=0), dict(n_seqs=65537), dict(max_pages=0), dict(max_seq=0), dict(max_seq=1281), dict(max_seq=(1 << 20) + 1, max_pages=1 << 20), dict(max_tokens=0),
+    for bad in (dict(n_seqs=0), dict(n_seqs=65536), dict(max_pages=0), dict(max_seq=0), dict(max_seq=1281), dict(max_seq=(1 << 20) + 1, max_pages=1 << 20), dict(max_tokens=0),
                 dict(max_tokens=1281), dict(n_tokens=0), dict(n_tokens=(1 << 24) + 1), dict(first_token=None), dict(first_token=None, max_tokens=1, n_tokens=3), dict(page_table=None, max_pages=26)):
         refused(iflow.ERR_SHAPE, batch=bad)
     for heads in (0, 12, 520, -8):
