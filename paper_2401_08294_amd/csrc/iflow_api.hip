@@ -453,6 +453,7 @@ iflow_status_t iflow_kv_attn_workspace_bytes(const iflow_kv_cache_t *cache, cons
     if (!bytes) return IFLOW_ERR_NULL;
     const iflow_status_t st = kv_shapes(cache, batch, true, n_heads, &v);
     if (st != IFLOW_OK) return st;
+    if ((int64_t)v.max_tokens * (n_heads / v.n_kv_heads) > (1 << 22)) return IFLOW_ERR_SHAPE;
     *bytes = iflow::kv_attn_workspace_bytes(v, cache->head_dim, n_heads);
     return IFLOW_OK;
 }
@@ -464,6 +465,7 @@ iflow_status_t iflow_kv_attn(const iflow_kv_cache_t *cache, const iflow_kv_batch
     iflow_status_t st = kv_shapes(cache, batch, true, n_heads, &v);
     if (st != IFLOW_OK) return st;
     if (!(scale > 0.0f && scale < 3.0e38f)) return IFLOW_ERR_SHAPE;
+    if ((int64_t)v.max_tokens * (n_heads / v.n_kv_heads) > (1 << 22)) return IFLOW_ERR_SHAPE;
     const size_t need = iflow::kv_attn_workspace_bytes(v, cache->head_dim, n_heads);
     if (!q || !out || (need && !workspace)) return IFLOW_ERR_NULL;
     st = kv_pointers(v);

@@ -424,6 +424,257 @@ __global__ __launch_bounds__(1024) void kv_attn_merge_kernel(KvView v, int n_hea
     out[((int64_t)(seq.row + i) * n_heads + h) * D + d] = as_u16((half_t)(L > 0.f ? O / L : 0.f));
 }
 
+// ---- many rows: prompts -----------------------------------------------------------------------------------------------------
+// With dozens of rows a tile is decoded once for all of them: RG wavefronts of 32 rows each share 64 positions, which they decode into LDS together, in the order in which
+// v_mfma_f32_32x32x16_f16 takes its operands (A: lane i + 32 h holds A[i][8h..8h+7], B alike, D: element e of lane j + 32 h is D[8 (e / 4) + 4h + e % 4][j]):
+//   S[position][row] = K Q^T with the queries in registers; a lane has one row's scores, sixteen of every 32 positions, and its half of the row's maximum and sum;
+//   O[component][row] = V^T P^T: element e of a tile's scores is position 4g + e % 4 or 16 + 4g + e % 4 of g = 2 (e / 8) + h where row i of S is position i with bits 3 and 4 changed
+//   over, so a lane's probabilities are its own operand, and a value's eight positions are a word of the cache's.  The sums' factors are the lane's own too.
+// Keys in LDS: [tile][component / 8][i: 32][8 components], values: [tile][g][component][8 positions]: 16-byte pieces that 32 lanes read side by side.
+// PG groups of wavefronts take every PG-th 64 positions and add up in LDS: where there are too few rows to fill the device.  The probabilities are rounded to fp16 once (and summed as rounded):
+// as large an error as the output's own rounding, where a second product for the rest would be half as much work again for the matrix cores.
+typedef float kv_float16 __attribute__((ext_vector_type(16)));
+
+template <typename T, int RG, int PG>
+__global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_rows_kernel(KvView v, const uint16_t *__restrict__ q, int n_heads, int group, KvDivide by_group, float scale_log2e,
+                                                                                          uint16_t *__restrict__ out)
+{
+    constexpr int D = T::D, NU = D / 16, NC = D / 32, STEP = 2 * KV_TILE;      // NU: steps of 16 components; NC: groups of 32
+    constexpr int UNITS = 2 * T::PIECES;                      // 1 KB of key codes (and of value codes) of a step
+    constexpr bool SPLIT = UNITS < RG;                        // half the wavefronts decode keys, half values
+    constexpr int MINE = SPLIT ? 1 : UNITS / RG;
+    constexpr int KEYS = STEP * D * 2, GROUP = 2 * KEYS;      // bytes
+    constexpr int ROWS = 32 * RG;
+    static_assert(SPLIT ? 2 * UNITS == RG : UNITS % RG == 0, "the wavefronts share the decoding evenly");
+    constexpr int MERGE = (PG > 1 ? PG * ROWS * (D + 4) * 4 : 0), LDS = GROUP * PG > MERGE ? GROUP * PG : MERGE;
+    __shared__ __align__(16) uint8_t s_mem[LDS];
+    __shared__ float s_m[PG][ROWS], s_l[PG][ROWS];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wave % RG, pg = wave / RG;
+    const int li = lane & 31, hf = lane >> 5;
+    const int head = blockIdx.x, b = blockIdx.z;
+    const KvSequence seq(v, b);
+    const int n_rows = seq.count * group;
+    const int r0 = ((int)gridDim.y - 1 - (int)blockIdx.y) * ROWS;      // (the last rows, which see most, first)
+    if (r0 >= n_rows) return;
+    const int longest = seq.sees(by_group(min(n_rows, r0 + ROWS) - 1));
+    const int my_row = min(n_rows - 1, r0 + rg * 32 + li), token = by_group(my_row), limit = seq.sees(token);
+    const bool real = r0 + rg * 32 + li < n_rows && seq.has_row(token);
+    const int64_t my_out = ((int64_t)(seq.row + token) * n_heads + head * group + (my_row - token * group)) * D;
+    // of the wavefront's rows: what the first sees, and the last
+    const int shortest = seq.sees(by_group(min(n_rows - 1, r0 + rg * 32))), limit_of_wave = seq.sees(by_group(min(n_rows - 1, r0 + rg * 32 + 31)));
+    uint8_t *stage = s_mem + pg * GROUP;
+
+    // queries as B operands: lane (row li, hf) holds components 16u + 8 hf .. +8
+    kv_half8 qb[NU];
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+        kv_u32x4 w = {0u, 0u, 0u, 0u};
+        if (real) w = *reinterpret_cast<const kv_u32x4 *>(q + my_out + 16 * u + 8 * hf);
+        qb[u] = __builtin_bit_cast(kv_half8, w);
+    }
+    float m = -INFINITY, l = 0.f;
+    kv_float16 oacc[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) oacc[c][e] = 0.f;
+
+    const KvMagic magic;
+    const int tiles = (longest + KV_TILE - 1) / KV_TILE, steps = (tiles + 1) / 2;
+    const int trips = (steps + PG - 1) / PG;                  // the same for all groups: they meet at the barriers
+    uint64_t my_tile = 0;                                     // where tile 64 n + lane is
+    auto find_tiles = [&](int t0) { my_tile = t0 + lane < tiles ? reinterpret_cast<uint64_t>(kv_tile_at(v, b, head, t0 + lane, T::BYTES)) : 0; };
+    auto tile_address = [&](int t) {
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)my_tile, t & 63), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(my_tile >> 32), t & 63);
+        return (uint64_t)hi << 32 | lo;
+    };
+    // What this wavefront decodes of a step: units of 1 KB, a piece of a tile's key codes or value codes.
+    constexpr int W = 8 / T::PER_WORD, CH = 4 / W;            // words of eight elements; eights of a lane's 16 bytes
+    constexpr int VB = CH * 16 > T::BLOCK ? CH * 16 / T::BLOCK : 1;    // blocks that a value piece's components lie in
+    struct Codes { kv_u32x4 k[MINE], v[MINE], vh[MINE][VB][2]; uint32_t kh[MINE][2]; } x;
+    const int g = lane >> 4, i = lane & 15;                   // the cache's (g, i)
+    const bool keys = !SPLIT || rg < UNITS, values = !SPLIT || rg >= UNITS;
+    auto unit_of = [&](int j) { return SPLIT ? rg % UNITS : rg + RG * j; };
+    auto load = [&](int t0) {                                 // t0: the step's first tile
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+            const int unit = unit_of(j), t = t0 + unit / T::PIECES, n = unit % T::PIECES;
+            const uint64_t address = t < tiles ? tile_address(t) : 0;
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(address), 0, address ? T::BYTES : 0, 0x00027000);
+            if (keys) {
+                x.k[j] = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane * 16 + n * 1024, 0, 0));
+                const auto h = __builtin_amdgcn_raw_buffer_load_b64(rsrc, T::KH_AT + ((g * (D / 4) / T::BLOCK) * 16 + i) * 8, 0, 0);
+                x.kh[j][0] = h[0]; x.kh[j][1] = h[1];
+            }
+            if (values) {
+                x.v[j] = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, T::V_AT + lane * 16 + n * 1024, 0, 0));
+#pragma unroll
+                for (int y = 0; y < VB; ++y)
+#pragma unroll
+                    for (int z = 0; z < 2; ++z)
+                        x.vh[j][y][z] = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, T::VH_AT + (y * 4 + g) * 32 + 16 * z + n * CH * 16 / T::BLOCK * 128, 0, 0));
+            }
+        }
+    };
+    auto decode = [&](int t0) {
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+            const int unit = unit_of(j), tile = unit / T::PIECES, n = unit % T::PIECES;
+            if (keys) {
+#pragma unroll
+                for (int y = 0; y < CH; ++y) {                // word 4 n + y W of the run: half h of the tile, components c ..
+                    const int h = T::RUN / 2 < 4 ? y * W / (T::RUN / 2) : n / (T::RUN / 2 < 4 ? 1 : T::RUN / 8), c = g * (D / 4) + (T::RUN / 2 < 4 ? y * W % (T::RUN / 2) : (4 * n + y * W) % (T::RUN / 2)) * T::PER_WORD;
+                    const half2_t pair = as_h2(h ? x.kh[j][1] : x.kh[j][0]), sc = {pair.x, pair.x}, of = {pair.y, pair.y};
+                    uint32_t w[2] = {x.k[j][y * W], W == 2 ? x.k[j][(y * W + W - 1) % 4] : 0u};
+                    KvPairs a = kv_levels<T::BITS>(w, magic);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a.p[e] = kv_value(a.p[e], sc, of);
+                    const int at = (i & 7) | h << 3 | (i >> 3) << 4;
+                    *reinterpret_cast<kv_u32x4 *>(stage + ((tile * (D / 8) + c / 8) * 32 + at) * 16) = __builtin_bit_cast(kv_u32x4, a);
+                }
+            }
+            if (values) {
+                // what lies behind the last position that a row sees may be anything, also no number: its values are zeros
+                const int p0 = (t0 + tile) * KV_TILE;
+                if (p0 + KV_TILE > longest) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int p = p0 + 16 * (e >> 1) + 4 * g + 2 * (e & 1);
+                        const uint32_t keep = p + 1 < longest ? 0xFFFFFFFFu : p < longest ? 0x0000FFFFu : 0u;
+#pragma unroll
+                        for (int y = 0; y < VB; ++y) { x.vh[j][y][0][e] &= keep; x.vh[j][y][1][e] &= keep; }
+                    }
+                }
+#pragma unroll
+                for (int y = 0; y < CH; ++y) {
+                    uint32_t w[2] = {x.v[j][y * W], W == 2 ? x.v[j][(y * W + W - 1) % 4] : 0u};
+                    KvPairs a = kv_levels<T::BITS>(w, magic);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a.p[e] = kv_value(a.p[e], as_h2(x.vh[j][y * VB / CH][0][e]), as_h2(x.vh[j][y * VB / CH][1][e]));
+                    *reinterpret_cast<kv_u32x4 *>(stage + KEYS + ((tile * 4 + g) * D + (n * CH + y) * 16 + i) * 16) = __builtin_bit_cast(kv_u32x4, a);
+                }
+            }
+        }
+    };
+
+    find_tiles(0);
+    load(2 * pg);
+    for (int trip = 0; trip < trips; ++trip) {
+        const int step = trip * PG + pg, t0 = 2 * step;
+        const bool there0 = t0 < tiles && tile_address(t0) != 0, there1 = t0 + 1 < tiles && tile_address(t0 + 1) != 0;
+        if (trip > 0) __syncthreads();                        // (the last step's operands have been read)
+        if (step < steps) decode(t0);
+        if (((t0 + 2 * PG) & 63) < 2 * PG) find_tiles((t0 + 2 * PG) & ~63);
+        load(t0 + 2 * PG);
+        __syncthreads();
+        if (step >= steps || t0 * KV_TILE >= limit_of_wave) continue;
+        kv_float16 sacc[2];
+#pragma unroll
+        for (int tl = 0; tl < 2; ++tl) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sacc[tl][e] = 0.f;
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                const kv_half8 a = *reinterpret_cast<const kv_half8 *>(stage + ((tl * (D / 8) + 2 * u + hf) * 32 + li) * 16);
+                sacc[tl] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, qb[u], sacc[tl], 0, 0, 0);
+            }
+        }
+        if (!there0 || !there1 || t0 * KV_TILE + STEP > shortest) {
+#pragma unroll
+            for (int tl = 0; tl < 2; ++tl)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (!(tl ? there1 : there0) || (t0 + tl) * KV_TILE + 16 * ((e >> 2) & 1) + 8 * (e >> 3) + 4 * hf + (e & 3) >= limit) sacc[tl][e] = -INFINITY;
+        }
+        float bm = kv_max3(sacc[0][0], sacc[0][1], sacc[1][0]);
+        bm = kv_max3(bm, sacc[1][1], sacc[0][2]);
+#pragma unroll
+        for (int e = 3; e < 15; e += 2) { bm = kv_max3(bm, sacc[0][e], sacc[0][e + 1]); bm = kv_max3(bm, sacc[1][e - 1], sacc[1][e]); }
+        bm = kv_max3(bm, sacc[0][15], sacc[1][14]);
+        bm = kv_max3(bm, sacc[1][15], -INFINITY);
+        const auto other = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, bm), __builtin_bit_cast(uint32_t, bm), false, false);
+        bm = kv_max3(__builtin_bit_cast(float, (uint32_t)other[0]), __builtin_bit_cast(float, (uint32_t)other[1]), -INFINITY) * scale_log2e;
+        const bool follow = bm > m + KVA_LAG;                 // (the first step with a score above -inf: always)
+        if (__builtin_amdgcn_ballot_w64(follow) != 0) {
+            const float alpha = follow ? __builtin_amdgcn_exp2f(m - (bm - KVA_BELOW)) : 1.0f;
+            l *= alpha;
+            m = follow ? bm - KVA_BELOW : m;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) oacc[c][e] *= alpha;
+        }
+        const float below = (m == -INFINITY) ? 0.f : -m;      // (a row that has seen nothing: no -inf - -inf)
+        const half2_t ones = {(half_t)1.f, (half_t)1.f};
+#pragma unroll
+        for (int tl = 0; tl < 2; ++tl)
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                KvPairs pb;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tl][8 * z + 2 * e], scale_log2e, below));
+                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tl][8 * z + 2 * e + 1], scale_log2e, below));
+                    pb.p[e] = (half2_t){(half_t)p0, (half_t)p1};
+                    l = __builtin_amdgcn_fdot2(pb.p[e], ones, l, false);
+                }
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const kv_half8 a = *reinterpret_cast<const kv_half8 *>(stage + KEYS + ((tl * 4 + 2 * z + hf) * D + 32 * c + li) * 16);
+                    oacc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, __builtin_bit_cast(kv_half8, pb), oacc[c], 0, 0, 0);
+                }
+            }
+    }
+
+    // element 4 y + e of oacc[c] is component 32 c + 8 y + 4 hf + e of row li
+    l += __shfl_xor(l, 32);
+    if constexpr (PG == 1) {
+        if (!real) return;
+        const float div = l > 0.f ? l : 1.f;                  // (nothing seen: zeros)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const half2_t a = {(half_t)(oacc[c][4 * y] / div), (half_t)(oacc[c][4 * y + 1] / div)}, d = {(half_t)(oacc[c][4 * y + 2] / div), (half_t)(oacc[c][4 * y + 3] / div)};
+                *reinterpret_cast<kv_u32x2 *>(out + my_out + 32 * c + 8 * y + 4 * hf) = (kv_u32x2){as_u32(a), as_u32(d)};
+            }
+    } else {
+        constexpr int PITCH = D + 4;
+        __syncthreads();
+        float *mine = reinterpret_cast<float *>(s_mem) + (pg * ROWS + rg * 32 + li) * PITCH + 4 * hf;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) *reinterpret_cast<kv_float4 *>(mine + 32 * c + 8 * y) = (kv_float4){oacc[c][4 * y], oacc[c][4 * y + 1], oacc[c][4 * y + 2], oacc[c][4 * y + 3]};
+        if (hf == 0) { s_m[pg][rg * 32 + li] = m; s_l[pg][rg * 32 + li] = l; }
+        __syncthreads();
+        constexpr int QUADS = D / 4;
+        for (int n = tid; n < ROWS * QUADS; n += 64 * RG * PG) {
+            const int r = n / QUADS, d = n % QUADS * 4, tok = by_group(min(n_rows - 1, r0 + r));
+            float M = s_m[0][r];
+#pragma unroll
+            for (int w = 1; w < PG; ++w) M = fmaxf(M, s_m[w][r]);
+            const float to_base = M == -INFINITY ? 0.f : M - KVA_SPARE;
+            float L = 0.f;
+            kv_float4 O = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < PG; ++w) {
+                const float f = __builtin_amdgcn_exp2f(s_m[w][r] - to_base);
+                const kv_float4 o = *reinterpret_cast<const kv_float4 *>(reinterpret_cast<const float *>(s_mem) + (w * ROWS + r) * PITCH + d);
+                L = __builtin_fmaf(s_l[w][r], f, L);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[e] = __builtin_fmaf(o[e], f, O[e]);
+            }
+            if (r0 + r >= n_rows || !seq.has_row(tok)) continue;
+            const float div = L > 0.f ? L : 1.f;
+            const half2_t a = {(half_t)(O[0] / div), (half_t)(O[1] / div)}, c = {(half_t)(O[2] / div), (half_t)(O[3] / div)};
+            const int64_t to = (int64_t)(seq.row + tok) * n_heads + head * group + (r0 + r - tok * group);
+            *reinterpret_cast<kv_u32x2 *>(out + to * D + d) = (kv_u32x2){as_u32(a), as_u32(c)};
+        }
+    }
+}
+
 // Whether a line is a workgroup's, without a second launch, and of how many wavefronts then (0: lines are cut).  Us (graph replay; one page table, lengths an eighth to the whole), cut / direct with four
 // wavefronts / with eight, for the longest sequence's positions:
 //                                        512               768               1024              2048
@@ -439,6 +690,19 @@ static int64_t kv_attn_lines(const KvView &v, int n_heads)    // of a sequence, 
 {
     return v.n_kv_heads * (((int64_t)v.max_tokens * (n_heads / v.n_kv_heads) + KVA_ROWS - 1) / KVA_ROWS);
 }
+#ifndef KVA_ROWS_FROM
+#define KVA_ROWS_FROM 64
+#endif
+#ifndef KVA_ROWS_WG
+#define KVA_ROWS_WG 512
+#endif
+// Rows of a workgroup that decodes for many (0: the rows are few).
+static int kv_attn_rows(const KvView &v, int n_heads)
+{
+    const int64_t rows = (int64_t)v.max_tokens * (n_heads / v.n_kv_heads);
+    if (rows < KVA_ROWS_FROM) return 0;
+    return v.n_seqs * v.n_kv_heads * ((rows + 127) / 128) >= KVA_ROWS_WG ? 128 : 64;
+}
 static int kv_attn_direct(const KvView &v, int head_dim, int n_heads)
 {
     const int64_t tiles = (v.max_seq + KV_TILE - 1) / KV_TILE, lines = v.n_seqs * kv_attn_lines(v, n_heads);
@@ -449,7 +713,7 @@ static int kv_attn_direct(const KvView &v, int head_dim, int n_heads)
 
 size_t kv_attn_workspace_bytes(const KvView &v, int head_dim, int n_heads)
 {
-    return kv_attn_direct(v, head_dim, n_heads) ? 0 : KvPartial::bytes(v.n_seqs, head_dim);
+    return kv_attn_rows(v, n_heads) || kv_attn_direct(v, head_dim, n_heads) ? 0 : KvPartial::bytes(v.n_seqs, head_dim);
 }
 
 hipError_t launch_kv_attn(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace, hipStream_t s)
@@ -458,8 +722,18 @@ hipError_t launch_kv_attn(int format, int head_dim, const KvView &v, const uint1
     const int64_t lines = kv_attn_lines(v, n_heads);
     const float scale_log2e = scale * 1.4426950408889634f;
     const int direct = kv_attn_direct(v, head_dim, n_heads);
-    if (v.max_tokens > 65535) return hipErrorInvalidValue;
     const KvDivide by_group(group), by_heads(v.n_kv_heads);
+    if (const int rows = kv_attn_rows(v, n_heads)) {
+        const int64_t blocks = ((int64_t)v.max_tokens * group + rows - 1) / rows;
+        if (blocks > 65535) return hipErrorInvalidValue;
+        return for_kv_tile(format, head_dim, [&](auto tag) {
+            typedef decltype(tag) T;
+            const dim3 grid((unsigned)v.n_kv_heads, (unsigned)blocks, (unsigned)v.n_seqs);
+            if (rows == 64) hipLaunchKernelGGL((kv_attn_rows_kernel<T, 2, 4>), grid, dim3(512), 0, s, v, q, n_heads, group, by_group, scale_log2e, out);
+            else hipLaunchKernelGGL((kv_attn_rows_kernel<T, 4, 1>), grid, dim3(256), 0, s, v, q, n_heads, group, by_group, scale_log2e, out);
+            return hipGetLastError();
+        });
+    }
     hipError_t e = for_kv_tile(format, head_dim, [&](auto tag) {
         typedef decltype(tag) T;
 #define IFLOW_KVA_GO(W, DIRECT, GRID) hipLaunchKernelGGL((kv_attn_kernel<T, W, DIRECT>), GRID, dim3(64 * W), 0, s, v, q, n_heads, group, by_group, by_heads, scale_log2e, out, workspace)

@@ -131,6 +131,8 @@ def test_refusals_before_any_launch(iflow):  # noqa: F811
     assert L.iflow_kv_append(None, b, at, at, at, 32, 10000.0, 1, at, None) == iflow.ERR_NULL and L.iflow_kv_append(c, None, at, at, at, 32, 10000.0, 1, at, None) == iflow.ERR_NULL
     assert L.iflow_kv_cache_bytes(c, None) == iflow.ERR_NULL and L.iflow_kv_cache_bytes(None, C.byref(C.c_size_t(0))) == iflow.ERR_NULL
     assert L.iflow_kv_attn_workspace_bytes(c, b, 32, None) == iflow.ERR_NULL
+    many = made(iflow.KvBatch, good_batch, dict(max_tokens=1 << 20, max_seq=1 << 20, max_pages=1 << 14))
+    assert L.iflow_kv_attn(c, many, 2 * at, 64, 0.1, 3 * at, 8 * at, 1 << 40, None) == iflow.ERR_SHAPE
     # through the binding: the same, as an error
     with pytest.raises(iflow.IflowError) as info:
         iflow.kv_attn(iflow.kv_cache(iflow.Q4_B64, 8, 128, 64, 10, at), iflow.kv_batch(2, 4, None, at + 4, 200), 2 * at, 32, 0.1, 3 * at, 4 * at, 1 << 30, stream=0)
