@@ -435,7 +435,7 @@ __global__ __launch_bounds__(1024) void kv_attn_merge_kernel(KvView v, int n_hea
 // as large an error as the output's own rounding, where a second product for the rest would be half as much work again for the matrix cores.
 typedef float kv_float16 __attribute__((ext_vector_type(16)));
 
-template <typename T, int RG, int PG>
+template <typename T, int RG, int PG, int STAGES>
 __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_rows_kernel(KvView v, const uint16_t *__restrict__ q, int n_heads, int group, KvDivide by_group, float scale_log2e,
                                                                                           uint16_t *__restrict__ out)
 {
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     constexpr int UNITS = 2 * T::PIECES;                      // 1 KB of key codes (and of value codes) of a step
     constexpr bool SPLIT = UNITS < RG;                        // half the wavefronts decode keys, half values
     constexpr int MINE = SPLIT ? 1 : UNITS / RG;
-    constexpr int KEYS = STEP * D * 2, GROUP = 2 * KEYS;      // bytes
+    constexpr int KEYS = STEP * D * 2, GROUP = 2 * STAGES * KEYS;      // bytes of a step's keys (its values are as many), of what a group of wavefronts stages
     constexpr int ROWS = 32 * RG;
     static_assert(SPLIT ? 2 * UNITS == RG : UNITS % RG == 0, "the wavefronts share the decoding evenly");
     constexpr int MERGE = (PG > 1 ? PG * ROWS * (D + 4) * 4 : 0), LDS = GROUP * PG > MERGE ? GROUP * PG : MERGE;
@@ -453,16 +453,22 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wave % RG, pg = wave / RG;
     const int li = lane & 31, hf = lane >> 5;
     const int head = blockIdx.x, b = blockIdx.z;
+    // where tile 64 n + lane is: the first 64 are asked for before the sequence's length is known
+    uint64_t my_tile = 0;
+    auto find_tiles = [&](int t0) { my_tile = (t0 + lane) * KV_TILE < v.max_seq ? reinterpret_cast<uint64_t>(kv_tile_at(v, b, head, t0 + lane, T::BYTES)) : 0; };
+    find_tiles(0);
     const KvSequence seq(v, b);
     const int n_rows = seq.count * group;
     const int r0 = ((int)gridDim.y - 1 - (int)blockIdx.y) * ROWS;      // (the last rows, which see most, first)
     if (r0 >= n_rows) return;
-    const int longest = seq.sees(by_group(min(n_rows, r0 + ROWS) - 1));
+    // (the same for the wavefront, as the compiler is told: what it takes for different in the lanes costs a loop around every load)
+    auto same = [](int n) { return __builtin_amdgcn_readfirstlane(n); };
+    const int longest = same(seq.sees(by_group(min(n_rows, r0 + ROWS) - 1)));
     const int my_row = min(n_rows - 1, r0 + rg * 32 + li), token = by_group(my_row), limit = seq.sees(token);
     const bool real = r0 + rg * 32 + li < n_rows && seq.has_row(token);
     const int64_t my_out = ((int64_t)(seq.row + token) * n_heads + head * group + (my_row - token * group)) * D;
     // of the wavefront's rows: what the first sees, and the last
-    const int shortest = seq.sees(by_group(min(n_rows - 1, r0 + rg * 32))), limit_of_wave = seq.sees(by_group(min(n_rows - 1, r0 + rg * 32 + 31)));
+    const int shortest = same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32)))), limit_of_wave = same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32 + 31))));
     uint8_t *stage = s_mem + pg * GROUP;
 
     // queries as B operands: lane (row li, hf) holds components 16u + 8 hf .. +8
@@ -483,8 +489,6 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     const KvMagic magic;
     const int tiles = (longest + KV_TILE - 1) / KV_TILE, steps = (tiles + 1) / 2;
     const int trips = (steps + PG - 1) / PG;                  // the same for all groups: they meet at the barriers
-    uint64_t my_tile = 0;                                     // where tile 64 n + lane is
-    auto find_tiles = [&](int t0) { my_tile = t0 + lane < tiles ? reinterpret_cast<uint64_t>(kv_tile_at(v, b, head, t0 + lane, T::BYTES)) : 0; };
     auto tile_address = [&](int t) {
         const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)my_tile, t & 63), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(my_tile >> 32), t & 63);
         return (uint64_t)hi << 32 | lo;
@@ -492,94 +496,104 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     // What this wavefront decodes of a step: units of 1 KB, a piece of a tile's key codes or value codes.
     constexpr int W = 8 / T::PER_WORD, CH = 4 / W;            // words of eight elements; eights of a lane's 16 bytes
     constexpr int VB = CH * 16 > T::BLOCK ? CH * 16 / T::BLOCK : 1;    // blocks that a value piece's components lie in
-    struct Codes { kv_u32x4 k[MINE], v[MINE], vh[MINE][VB][2]; uint32_t kh[MINE][2]; } x;
+    struct Keys { kv_u32x4 k[MINE]; uint32_t kh[MINE][2]; };
+    struct Codes : Keys { kv_u32x4 v[MINE], vh[MINE][VB][2]; } x;
     const int g = lane >> 4, i = lane & 15;                   // the cache's (g, i)
     const bool keys = !SPLIT || rg < UNITS, values = !SPLIT || rg >= UNITS;
     auto unit_of = [&](int j) { return SPLIT ? rg % UNITS : rg + RG * j; };
-    auto load = [&](int t0) {                                 // t0: the step's first tile
+    auto buffer_of = [&](int t) {                             // (empty where there is none: zeros arrive)
+        const uint64_t address = t < tiles ? tile_address(t) : 0;
+        return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(address), 0, address ? T::BYTES : 0, 0x00027000);
+    };
+    auto load_keys = [&](int t0) {                            // t0: the step's first tile
+        if (!keys) return;
 #pragma unroll
         for (int j = 0; j < MINE; ++j) {
-            const int unit = unit_of(j), t = t0 + unit / T::PIECES, n = unit % T::PIECES;
-            const uint64_t address = t < tiles ? tile_address(t) : 0;
-            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(address), 0, address ? T::BYTES : 0, 0x00027000);
-            if (keys) {
-                x.k[j] = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane * 16 + n * 1024, 0, 0));
-                const auto h = __builtin_amdgcn_raw_buffer_load_b64(rsrc, T::KH_AT + ((g * (D / 4) / T::BLOCK) * 16 + i) * 8, 0, 0);
-                x.kh[j][0] = h[0]; x.kh[j][1] = h[1];
-            }
-            if (values) {
-                x.v[j] = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, T::V_AT + lane * 16 + n * 1024, 0, 0));
+            const int unit = unit_of(j), n = unit % T::PIECES;
+            const auto rsrc = buffer_of(t0 + unit / T::PIECES);
+            x.k[j] = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane * 16 + n * 1024, 0, 0));
+            const auto h = __builtin_amdgcn_raw_buffer_load_b64(rsrc, T::KH_AT + ((g * (D / 4) / T::BLOCK) * 16 + i) * 8, 0, 0);
+            x.kh[j][0] = h[0]; x.kh[j][1] = h[1];
+        }
+    };
+    auto load_values = [&](int t0) {
+        if (!values) return;
 #pragma unroll
-                for (int y = 0; y < VB; ++y)
+        for (int j = 0; j < MINE; ++j) {
+            const int unit = unit_of(j), n = unit % T::PIECES;
+            const auto rsrc = buffer_of(t0 + unit / T::PIECES);
+            x.v[j] = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, T::V_AT + lane * 16 + n * 1024, 0, 0));
 #pragma unroll
-                    for (int z = 0; z < 2; ++z)
-                        x.vh[j][y][z] = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, T::VH_AT + (y * 4 + g) * 32 + 16 * z + n * CH * 16 / T::BLOCK * 128, 0, 0));
+            for (int y = 0; y < VB; ++y)
+#pragma unroll
+                for (int z = 0; z < 2; ++z)
+                    x.vh[j][y][z] = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, T::VH_AT + (y * 4 + g) * 32 + 16 * z + n * CH * 16 / T::BLOCK * 128, 0, 0));
+        }
+    };
+    auto decode_key = [&](uint8_t *to, int j, int y) {         // word 4 n + y W of the run: half h of the tile, components c ..
+        const int unit = unit_of(j), tile = unit / T::PIECES, n = unit % T::PIECES;
+        constexpr bool SHORT = T::RUN / 2 < 4;
+        const int h = SHORT ? y * W / (T::RUN / 2) : n / (SHORT ? 1 : T::RUN / 8), c = g * (D / 4) + (SHORT ? y * W % (T::RUN / 2) : (4 * n + y * W) % (T::RUN / 2)) * T::PER_WORD;
+        const half2_t pair = as_h2(h ? x.kh[j][1] : x.kh[j][0]), sc = {pair.x, pair.x}, of = {pair.y, pair.y};
+        uint32_t w[2] = {x.k[j][y * W], W == 2 ? x.k[j][(y * W + W - 1) % 4] : 0u};
+        KvPairs a = kv_levels<T::BITS>(w, magic);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a.p[e] = kv_value(a.p[e], sc, of);
+        const int at = (i & 7) | h << 3 | (i >> 3) << 4;
+        *reinterpret_cast<kv_u32x4 *>(to + ((tile * (D / 8) + c / 8) * 32 + at) * 16) = __builtin_bit_cast(kv_u32x4, a);
+    };
+    auto decode_value = [&](uint8_t *to, int j, int y) {
+        const int unit = unit_of(j), tile = unit / T::PIECES, n = unit % T::PIECES;
+        uint32_t w[2] = {x.v[j][y * W], W == 2 ? x.v[j][(y * W + W - 1) % 4] : 0u};
+        KvPairs a = kv_levels<T::BITS>(w, magic);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a.p[e] = kv_value(a.p[e], as_h2(x.vh[j][y * VB / CH][0][e]), as_h2(x.vh[j][y * VB / CH][1][e]));
+        *reinterpret_cast<kv_u32x4 *>(to + ((tile * 4 + g) * D + (n * CH + y) * 16 + i) * 16) = __builtin_bit_cast(kv_u32x4, a);
+    };
+    constexpr int CHUNKS = MINE * CH;                         // eights of a lane: of keys, and of values
+    auto decode_keys = [&](uint8_t *to) {
+        if (!keys) return;
+#pragma unroll
+        for (int n = 0; n < CHUNKS; ++n) decode_key(to, n / CH, n % CH);
+    };
+    auto decode_values = [&](uint8_t *to) {
+        if (!values) return;
+#pragma unroll
+        for (int n = 0; n < CHUNKS; ++n) decode_value(to, n / CH, n % CH);
+    };
+    // what lies behind the last position that a row sees may be anything, also no number: its values are zeros
+    auto cut_values = [&](int t0) {
+        if (!values || t0 * KV_TILE + STEP <= longest) return;
+#pragma unroll
+        for (int j = 0; j < MINE; ++j) {
+            const int p0 = (t0 + unit_of(j) / T::PIECES) * KV_TILE;
+            {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int p = p0 + 16 * (e >> 1) + 4 * g + 2 * (e & 1);
+                    const uint32_t keep = p + 1 < longest ? 0xFFFFFFFFu : p < longest ? 0x0000FFFFu : 0u;
+#pragma unroll
+                    for (int y = 0; y < VB; ++y) { x.vh[j][y][0][e] &= keep; x.vh[j][y][1][e] &= keep; }
+                }
             }
         }
     };
-    auto decode = [&](int t0) {
+    // scores of a step from its keys in LDS: product n of 2 NU is components 16 (n / 2) .. of tile n % 2
+    kv_float16 sacc[2];
+    auto key_operand = [&](const uint8_t *from, int n) { return *reinterpret_cast<const kv_half8 *>(from + ((n % 2 * (D / 8) + 2 * (n / 2) + hf) * 32 + li) * 16); };
+    auto clear = [&](kv_float16 (&to)[2]) {
 #pragma unroll
-        for (int j = 0; j < MINE; ++j) {
-            const int unit = unit_of(j), tile = unit / T::PIECES, n = unit % T::PIECES;
-            if (keys) {
+        for (int tl = 0; tl < 2; ++tl)
 #pragma unroll
-                for (int y = 0; y < CH; ++y) {                // word 4 n + y W of the run: half h of the tile, components c ..
-                    const int h = T::RUN / 2 < 4 ? y * W / (T::RUN / 2) : n / (T::RUN / 2 < 4 ? 1 : T::RUN / 8), c = g * (D / 4) + (T::RUN / 2 < 4 ? y * W % (T::RUN / 2) : (4 * n + y * W) % (T::RUN / 2)) * T::PER_WORD;
-                    const half2_t pair = as_h2(h ? x.kh[j][1] : x.kh[j][0]), sc = {pair.x, pair.x}, of = {pair.y, pair.y};
-                    uint32_t w[2] = {x.k[j][y * W], W == 2 ? x.k[j][(y * W + W - 1) % 4] : 0u};
-                    KvPairs a = kv_levels<T::BITS>(w, magic);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) a.p[e] = kv_value(a.p[e], sc, of);
-                    const int at = (i & 7) | h << 3 | (i >> 3) << 4;
-                    *reinterpret_cast<kv_u32x4 *>(stage + ((tile * (D / 8) + c / 8) * 32 + at) * 16) = __builtin_bit_cast(kv_u32x4, a);
-                }
-            }
-            if (values) {
-                // what lies behind the last position that a row sees may be anything, also no number: its values are zeros
-                const int p0 = (t0 + tile) * KV_TILE;
-                if (p0 + KV_TILE > longest) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int p = p0 + 16 * (e >> 1) + 4 * g + 2 * (e & 1);
-                        const uint32_t keep = p + 1 < longest ? 0xFFFFFFFFu : p < longest ? 0x0000FFFFu : 0u;
-#pragma unroll
-                        for (int y = 0; y < VB; ++y) { x.vh[j][y][0][e] &= keep; x.vh[j][y][1][e] &= keep; }
-                    }
-                }
-#pragma unroll
-                for (int y = 0; y < CH; ++y) {
-                    uint32_t w[2] = {x.v[j][y * W], W == 2 ? x.v[j][(y * W + W - 1) % 4] : 0u};
-                    KvPairs a = kv_levels<T::BITS>(w, magic);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) a.p[e] = kv_value(a.p[e], as_h2(x.vh[j][y * VB / CH][0][e]), as_h2(x.vh[j][y * VB / CH][1][e]));
-                    *reinterpret_cast<kv_u32x4 *>(stage + KEYS + ((tile * 4 + g) * D + (n * CH + y) * 16 + i) * 16) = __builtin_bit_cast(kv_u32x4, a);
-                }
-            }
-        }
+            for (int e = 0; e < 16; ++e) to[tl][e] = 0.f;
     };
-
-    find_tiles(0);
-    load(2 * pg);
-    for (int trip = 0; trip < trips; ++trip) {
-        const int step = trip * PG + pg, t0 = 2 * step;
-        const bool there0 = t0 < tiles && tile_address(t0) != 0, there1 = t0 + 1 < tiles && tile_address(t0 + 1) != 0;
-        if (trip > 0) __syncthreads();                        // (the last step's operands have been read)
-        if (step < steps) decode(t0);
-        if (((t0 + 2 * PG) & 63) < 2 * PG) find_tiles((t0 + 2 * PG) & ~63);
-        load(t0 + 2 * PG);
-        __syncthreads();
-        if (step >= steps || t0 * KV_TILE >= limit_of_wave) continue;
-        kv_float16 sacc[2];
+    auto score = [&](const uint8_t *from, kv_float16 (&to)[2]) {
+        clear(to);
 #pragma unroll
-        for (int tl = 0; tl < 2; ++tl) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) sacc[tl][e] = 0.f;
-#pragma unroll
-            for (int u = 0; u < NU; ++u) {
-                const kv_half8 a = *reinterpret_cast<const kv_half8 *>(stage + ((tl * (D / 8) + 2 * u + hf) * 32 + li) * 16);
-                sacc[tl] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, qb[u], sacc[tl], 0, 0, 0);
-            }
-        }
+        for (int n = 0; n < 2 * NU; ++n) to[n % 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_operand(from, n), qb[n / 2], to[n % 2], 0, 0, 0);
+    };
+    // what a row does not see goes, and the reference and the sums follow where a score is far above
+    auto settle = [&](int t0, bool there0, bool there1) {
         if (!there0 || !there1 || t0 * KV_TILE + STEP > shortest) {
 #pragma unroll
             for (int tl = 0; tl < 2; ++tl)
@@ -605,38 +619,137 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
 #pragma unroll
                 for (int e = 0; e < 16; ++e) oacc[c][e] *= alpha;
         }
-        const float below = (m == -INFINITY) ? 0.f : -m;      // (a row that has seen nothing: no -inf - -inf)
-        const half2_t ones = {(half_t)1.f, (half_t)1.f};
+    };
+    const half2_t ones = {(half_t)1.f, (half_t)1.f};
+    KvPairs pb[2][2];
+    float below = 0.f;                                        // what is added to a score (a row that has seen nothing: no -inf - -inf)
+    auto weigh_pair = [&](int n) {                            // scores 2 n, 2 n + 1 of 32 to probabilities, in place of operands
+        const int tl = n / 8, z = n / 4 % 2, e = n % 4;
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tl][8 * z + 2 * e], scale_log2e, below));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tl][8 * z + 2 * e + 1], scale_log2e, below));
+        pb[tl][z].p[e] = (half2_t){(half_t)p0, (half_t)p1};
+        l = __builtin_amdgcn_fdot2(pb[tl][z].p[e], ones, l, false);
+    };
+    // product n of 4 NC: positions of operand n / NC, components 32 (n % NC) ..
+    auto value_operand = [&](const uint8_t *from, int n) { return *reinterpret_cast<const kv_half8 *>(from + ((n / (2 * NC) * 4 + 2 * (n / NC % 2) + hf) * D + 32 * (n % NC) + li) * 16); };
+    auto add = [&](kv_half8 a, int n) {
+        oacc[n % NC] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, __builtin_bit_cast(kv_half8, pb[n / (2 * NC)][n / NC % 2]), oacc[n % NC], 0, 0, 0);
+    };
+    // which tiles are there, of the 64 that lanes know and of the 64 before
+    uint64_t known = 0, before = 0;
+    int window = 0;
+    auto there = [&](int t) { return t < tiles && ((t >> 6 == window ? known : before) >> (t & 63) & 1) != 0; };
+    auto first_of = [&](int trip) { return 2 * (trip * PG + pg); };
+    auto advance = [&](int t0) {
+        if (t0 >> 6 != window) {
+            window = t0 >> 6;
+            find_tiles(t0 & ~63);
+            before = known;
+            known = __builtin_amdgcn_ballot_w64(my_tile != 0);
+        }
+    };
+    known = __builtin_amdgcn_ballot_w64(my_tile != 0);
+
+    if constexpr (STAGES == 1) {
+        uint8_t *k_at = stage, *v_at = stage + KEYS;
+        load_keys(first_of(0)); load_values(first_of(0));
+        for (int trip = 0; trip < trips; ++trip) {
+            const int t0 = first_of(trip);
+            if (trip > 0) __syncthreads();                    // (the last step's operands have been read)
+            cut_values(t0);
+            decode_keys(k_at); decode_values(v_at);
+            advance(first_of(trip + 1));
+            load_keys(first_of(trip + 1)); load_values(first_of(trip + 1));
+            __syncthreads();
+            if (t0 * KV_TILE >= limit_of_wave) continue;
+            score(k_at, sacc);
+            settle(t0, there(t0), there(t0 + 1));
+            below = (m == -INFINITY) ? 0.f : -m;
 #pragma unroll
-        for (int tl = 0; tl < 2; ++tl)
+            for (int n = 0; n < 16; ++n) weigh_pair(n);
 #pragma unroll
-            for (int z = 0; z < 2; ++z) {
-                KvPairs pb;
+            for (int n = 0; n < 4 * NC; ++n) add(value_operand(v_at, n), n);
+        }
+    } else {
+        // Step n's probabilities are made while step n + 1 is scored, and its values added while step n + 2's keys and n + 1's values are decoded: matrix and vector instructions of one
+        // wavefront do not wait for one another.  Two places for keys and for values, one barrier a step.
+        auto k_at = [&](int trip) { return stage + (trip & 1) * KEYS; };
+        auto v_at = [&](int trip) { return stage + (2 + (trip & 1)) * KEYS; };
+        load_keys(first_of(0));
+        const Keys keys0 = x;
+        load_keys(first_of(1));
+        load_values(first_of(0));
+        const Keys keys1 = x;
+        static_cast<Keys &>(x) = keys0;
+        decode_keys(k_at(0));
+        static_cast<Keys &>(x) = keys1;
+        decode_keys(k_at(1));
+        load_keys(first_of(2));
+        cut_values(first_of(0));
+        decode_values(v_at(0));
+        load_values(first_of(1));
+        __syncthreads();
+        score(k_at(0), sacc);
+        settle(first_of(0), there(first_of(0)), there(first_of(0) + 1));
+        for (int trip = 0; trip < trips; ++trip) {
+            kv_float16 next[2];
+            clear(next);
+            below = (m == -INFINITY) ? 0.f : -m;
+            cut_values(first_of(trip + 1));
+            // (Operands are read AHEAD products before theirs; the barriers hold the order, which the scheduler takes apart into matrix and vector instructions.)
+            constexpr int AHEAD = 4;
+            kv_half8 a[AHEAD];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tl][8 * z + 2 * e], scale_log2e, below));
-                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tl][8 * z + 2 * e + 1], scale_log2e, below));
-                    pb.p[e] = (half2_t){(half_t)p0, (half_t)p1};
-                    l = __builtin_amdgcn_fdot2(pb.p[e], ones, l, false);
-                }
+            for (int n = 0; n < AHEAD; ++n) a[n] = key_operand(k_at(trip + 1), n);
 #pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    const kv_half8 a = *reinterpret_cast<const kv_half8 *>(stage + KEYS + ((tl * 4 + 2 * z + hf) * D + 32 * c + li) * 16);
-                    oacc[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, __builtin_bit_cast(kv_half8, pb), oacc[c], 0, 0, 0);
+            for (int n = 0; n < 2 * NU; ++n) {
+                __builtin_amdgcn_sched_barrier(0);
+                next[n % 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[n % AHEAD], qb[n / 2], next[n % 2], 0, 0, 0);
+                a[n % AHEAD] = n + AHEAD < 2 * NU ? key_operand(k_at(trip + 1), n + AHEAD) : value_operand(v_at(trip), n + AHEAD - 2 * NU);
+#pragma unroll
+                for (int y = 0; y < 8 / NU; ++y) { weigh_pair(n * (8 / NU) + y); }
+            }
+#pragma unroll
+            for (int n = 0; n < 4 * NC; ++n) {
+                __builtin_amdgcn_sched_barrier(0);
+                add(a[n % AHEAD], n);
+                if (n + AHEAD < 4 * NC) a[n % AHEAD] = value_operand(v_at(trip), n + AHEAD);
+                if (n % 2 == 0) {
+                    constexpr int EACH = 2 * CHUNKS / (2 * NC) > 0 ? 2 * CHUNKS / (2 * NC) : 1;
+#pragma unroll
+                    for (int y = 0; y < EACH; ++y) {
+                        const int c = n / 2 * EACH + y;
+                        if (SPLIT) {
+                            if (keys && c < CHUNKS) decode_key(k_at(trip), c / CH, c % CH);
+                            if (values && c < CHUNKS) decode_value(v_at(trip + 1), c / CH, c % CH);
+                        } else if (c < CHUNKS) {
+                            decode_key(k_at(trip), c / CH, c % CH);
+                        } else if (c < 2 * CHUNKS) {
+                            decode_value(v_at(trip + 1), (c - CHUNKS) / CH, c % CH);
+                        }
+                    }
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
+            load_values(first_of(trip + 2));
+            advance(first_of(trip + 3));
+            load_keys(first_of(trip + 3));
+            __syncthreads();
+            sacc[0] = next[0]; sacc[1] = next[1];
+            if (trip + 1 < trips) settle(first_of(trip + 1), there(first_of(trip + 1)), there(first_of(trip + 1) + 1));
+        }
     }
 
     // element 4 y + e of oacc[c] is component 32 c + 8 y + 4 hf + e of row li
     l += __shfl_xor(l, 32);
     if constexpr (PG == 1) {
         if (!real) return;
-        const float div = l > 0.f ? l : 1.f;                  // (nothing seen: zeros)
+        const float f = l > 0.f ? 1.f / l : 0.f;              // (nothing seen: zeros; 64 divisions would take as long as two steps)
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-                const half2_t a = {(half_t)(oacc[c][4 * y] / div), (half_t)(oacc[c][4 * y + 1] / div)}, d = {(half_t)(oacc[c][4 * y + 2] / div), (half_t)(oacc[c][4 * y + 3] / div)};
+                const half2_t a = {(half_t)(oacc[c][4 * y] * f), (half_t)(oacc[c][4 * y + 1] * f)}, d = {(half_t)(oacc[c][4 * y + 2] * f), (half_t)(oacc[c][4 * y + 3] * f)};
                 *reinterpret_cast<kv_u32x2 *>(out + my_out + 32 * c + 8 * y + 4 * hf) = (kv_u32x2){as_u32(a), as_u32(d)};
             }
     } else {
@@ -690,18 +803,17 @@ static int64_t kv_attn_lines(const KvView &v, int n_heads)    // of a sequence, 
 {
     return v.n_kv_heads * (((int64_t)v.max_tokens * (n_heads / v.n_kv_heads) + KVA_ROWS - 1) / KVA_ROWS);
 }
-#ifndef KVA_ROWS_FROM
-#define KVA_ROWS_FROM 64
-#endif
-#ifndef KVA_ROWS_WG
-#define KVA_ROWS_WG 512
-#endif
-// Rows of a workgroup that decodes for many (0: the rows are few).
+// Rows of a workgroup that decodes for many (0: by sixteens, as above).  Us, by sixteens / 64 rows / 128 rows, for so many blocks of 64 rows (graph replay):
+//   32/8 heads x 128, 4 bits, one sequence of 4000                   64: 39 / 51 / 92    128: 66 / 54 / 94    256: 100 / 61 / 96   512: 181 / 109 / 104  1024: 298 / 184 / 139
+//   ... eight of 250 to 2000 (blocks: if all had as many as most)    128: 24 / 30 / 51   256: 30 / 31 / 52    512: 49 / 46 / 55    1024: 82 / 62 / 60
+//   64/8 heads x 128, 8 bits, one of 1000                            64: 13 / 24 / 38    128: 19 / 25 / 41    256: 30 / 27 / 45    512: 48 / 48 / 51
+//   71/1 heads x 64, 4 bits, one of 2000                             71: 19 / 21 / 44    142: 26 / 22 / 44
+// Blocks of 64 rows take as long for one as for 256; those of 128 take two for each compute unit to hide one another's waits.
 static int kv_attn_rows(const KvView &v, int n_heads)
 {
-    const int64_t rows = (int64_t)v.max_tokens * (n_heads / v.n_kv_heads);
-    if (rows < KVA_ROWS_FROM) return 0;
-    return v.n_seqs * v.n_kv_heads * ((rows + 127) / 128) >= KVA_ROWS_WG ? 128 : 64;
+    const int64_t rows = (int64_t)v.max_tokens * (n_heads / v.n_kv_heads), lines = v.n_seqs * v.n_kv_heads;
+    if (rows < 64 || lines * ((rows + 63) / 64) < (v.n_seqs == 1 ? 128 : 256)) return 0;
+    return lines * ((rows + 127) / 128) >= 512 ? 128 : 64;
 }
 static int kv_attn_direct(const KvView &v, int head_dim, int n_heads)
 {
@@ -724,13 +836,12 @@ hipError_t launch_kv_attn(int format, int head_dim, const KvView &v, const uint1
     const int direct = kv_attn_direct(v, head_dim, n_heads);
     const KvDivide by_group(group), by_heads(v.n_kv_heads);
     if (const int rows = kv_attn_rows(v, n_heads)) {
-        const int64_t blocks = ((int64_t)v.max_tokens * group + rows - 1) / rows;
-        if (blocks > 65535) return hipErrorInvalidValue;
+        const int64_t blocks = ((int64_t)v.max_tokens * group + rows - 1) / rows;      // (at most 2^22 rows: 32768)
         return for_kv_tile(format, head_dim, [&](auto tag) {
             typedef decltype(tag) T;
             const dim3 grid((unsigned)v.n_kv_heads, (unsigned)blocks, (unsigned)v.n_seqs);
-            if (rows == 64) hipLaunchKernelGGL((kv_attn_rows_kernel<T, 2, 4>), grid, dim3(512), 0, s, v, q, n_heads, group, by_group, scale_log2e, out);
-            else hipLaunchKernelGGL((kv_attn_rows_kernel<T, 4, 1>), grid, dim3(256), 0, s, v, q, n_heads, group, by_group, scale_log2e, out);
+            if (rows == 64) hipLaunchKernelGGL((kv_attn_rows_kernel<T, 2, 4, 1>), grid, dim3(512), 0, s, v, q, n_heads, group, by_group, scale_log2e, out);
+            else hipLaunchKernelGGL((kv_attn_rows_kernel<T, 4, 1, 2>), grid, dim3(256), 0, s, v, q, n_heads, group, by_group, scale_log2e, out);
             return hipGetLastError();
         });
     }

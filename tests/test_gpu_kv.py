@@ -211,6 +211,30 @@ def test_attention_over_parts_of_long_lines(gpu, name, n_heads, n_kv, d, lens, c
     s.check_attend(s.queries(), d ** -0.5)
 
 
+@pytest.mark.parametrize("name,n_heads,d,lens,counts", [("Q4_B64", 64, 64, [150, 333, 200, 260], [150, 150, 140, 129]), ("Q4_B32", 64, 64, [129, 70, 300, 64], [129, 2, 130, 64]),
+                                                       ("Q8_B32", 128, 64, [90, 200, 80, 65], [65, 66, 80, 0]), ("Q4_B64", 64, 128, [140, 131, 180, 129], [140, 129, 130, 1]),
+                                                       ("Q4_B32", 64, 128, [140, 0, 180, 129], [140, 0, 130, 129]), ("Q8_B64", 64, 128, [130, 150, 131, 129], [129, 130, 131, 129])])
+def test_attention_of_prompts_that_fill_the_device(gpu, name, n_heads, d, lens, counts):  # noqa: F811
+    """As many heads and tokens as give every compute unit two blocks of 128 rows."""
+    say(f"[case] kv attention of prompts {name} {n_heads}/64 heads of {d}, lengths {lens}, tokens {counts}")
+    s = Setup(gpu, name, 64, d, 64, lens, counts, 4300 + n_heads + d, n_heads)
+    s.fill()
+    s.table[1, 0] = -1                                         # (a page that is not there)
+    s.describe()
+    s.check_attend(s.queries(), d ** -0.5)
+
+
+@pytest.mark.parametrize("name,n_heads,d,lens,counts", [("Q4_B64", 64, 64, [400], [129]), ("Q4_B32", 64, 64, [129], [129]), ("Q8_B32", 128, 64, [700], [70]), ("Q8_B64", 64, 64, [330, 65], [65, 65]),
+                                                       ("Q4_B64", 64, 128, [300], [130]), ("Q4_B32", 128, 128, [90], [90]), ("Q8_B32", 64, 128, [600], [65]), ("Q8_B64", 64, 128, [200, 1], [129, 1])])
+def test_attention_of_prompts_in_blocks_of_64(gpu, name, n_heads, d, lens, counts):  # noqa: F811
+    """Fewer blocks than fill the device twice: 64 rows, whose positions four groups of wavefronts share."""
+    say(f"[case] kv attention of prompts {name} {n_heads}/64 heads of {d}, lengths {lens}, tokens {counts}")
+    s = Setup(gpu, name, 64, d, 96, lens, counts, 4400 + n_heads + d, n_heads)
+    s.fill()
+    s.describe()
+    s.check_attend(s.queries(), d ** -0.5)
+
+
 @pytest.mark.parametrize("counts", [None, [3], [150]])
 def test_attention_peaked_and_climbing_scores(gpu, counts):  # noqa: F811
     """Large scores: one position outweighs the rest, wherever it is, and scores that climb by up to 40 (log2) from tile to tile, each head by another step: the reference follows in some
@@ -232,6 +256,29 @@ def test_attention_peaked_and_climbing_scores(gpu, counts):  # noqa: F811
         for p in range(n):
             s.cache.store(s.table[0], p, k[p].view(np.uint16), v[p])
         s.d_pages.copy_(s.dev(s.pages))
+        s.check_attend(q.view(np.uint16), 0.125)
+
+
+@pytest.mark.parametrize("n_seqs", [1, 8])
+def test_attention_of_prompts_with_climbing_scores(gpu, n_seqs):  # noqa: F811
+    """Blocks of 64 rows (one sequence) and of 128 (eight): scores that climb along the positions, by another step for every head, so that the reference follows in some rows and not in others, and
+    groups of wavefronts are added from references far apart."""
+    n_kv, d, n = 64, 64, 200
+    s = Setup(gpu, "Q8_B32", n_kv, d, 64, [n] * n_seqs, [129 if n_seqs == 1 else 65] * n_seqs, 4500, 64, spare_pages=0)
+    s.fill()
+    if n_seqs > 1:
+        s.table[1:] = s.table[0]                               # (pages that are only read may be shared)
+    for name, climb in (("tiles", np.arange(n) // 32), ("positions", np.arange(n) / 8.0), ("down", -(np.arange(n) // 16))):
+        say(f"[case] kv attention of prompts, climbing scores: {name}, {n_seqs} sequences")
+        k, v = s.values(n)
+        k, q = k.view(np.float16), s.queries().view(np.float16)
+        k[:, :, :32] = 0.0
+        k[:, :, 0] = climb[:, None]
+        q[..., 1:32] = 0.0
+        q[..., 0] = np.resize([0.0, 6.0, 7.9, 8.0, 10.0, 14.9, 20.0, 40.0, -6.0, -20.0, 3.0], 64) * np.log(2.0) / 0.125 / max(1.0, np.abs(climb).max() / 30.0)
+        for p in range(n):
+            s.cache.store(s.table[0], p, k[p].view(np.uint16), v[p])
+        s.describe()
         s.check_attend(q.view(np.uint16), 0.125)
 
 
