@@ -53,23 +53,27 @@ __device__ __forceinline__ half_t kv_half_once(double x)
 
 template <typename T> struct KvLane {
     static constexpr int H = KV_PART<T>, D = T::D;
-    typedef half_t Components __attribute__((ext_vector_type(2 * H)));
-    Components x;                                             // of both halves (a vector: of an array, where the pairing is chosen, components are picked by address)
+    float x[2 * H];                                           // components of both halves: fp16 values, a register each (of 16-bit ones, picked by the pairing, the compiler made an array in memory)
 
     static __device__ __forceinline__ int pair_of(int s, int e, int pair_mode)
     {
         return pair_mode == IFLOW_ROPE_HALVES ? s * H + e : e < H / 2 ? s * H / 2 + e : D / 4 + s * H / 2 + e - H / 2;
     }
-    __device__ __forceinline__ void load(const uint16_t *row, int s)
+    // what is loaded ahead of its use waits packed
+    struct Words { uint32_t w[H]; };
+    static __device__ __forceinline__ Words load(const uint16_t *row, int s)
+    {
+        Words n;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+            if constexpr (H == 8) *reinterpret_cast<kv_u32x4 *>(n.w + half * (H / 2)) = *reinterpret_cast<const kv_u32x4 *>(row + half * (D / 2) + s * H);
+            else *reinterpret_cast<kv_u32x2 *>(n.w + half * (H / 2)) = *reinterpret_cast<const kv_u32x2 *>(row + half * (D / 2) + s * H);
+        return n;
+    }
+    __device__ __forceinline__ explicit KvLane(const Words &n)
     {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            uint32_t w[H / 2];
-            if constexpr (H == 8) *reinterpret_cast<kv_u32x4 *>(w) = *reinterpret_cast<const kv_u32x4 *>(row + half * (D / 2) + s * H);
-            else *reinterpret_cast<kv_u32x2 *>(w) = *reinterpret_cast<const kv_u32x2 *>(row + half * (D / 2) + s * H);
-#pragma unroll
-            for (int e = 0; e < H / 2; ++e) { const half2_t p = as_h2(w[e]); x[half * H + 2 * e] = p.x; x[half * H + 2 * e + 1] = p.y; }
-        }
+        for (int e = 0; e < H; ++e) { const half2_t p = as_h2(n.w[e]); x[2 * e] = (float)p.x; x[2 * e + 1] = (float)p.y; }
     }
     __device__ __forceinline__ void store(uint16_t *row, int s) const
     {
@@ -77,27 +81,26 @@ template <typename T> struct KvLane {
         for (int half = 0; half < 2; ++half) {
             uint32_t w[H / 2];
 #pragma unroll
-            for (int e = 0; e < H / 2; ++e) w[e] = as_u32((half2_t){x[half * H + 2 * e], x[half * H + 2 * e + 1]});
+            for (int e = 0; e < H / 2; ++e) w[e] = as_u32((half2_t){(half_t)x[half * H + 2 * e], (half_t)x[half * H + 2 * e + 1]});
             if constexpr (H == 8) kv_store(row + half * (D / 2) + s * H, *reinterpret_cast<kv_u32x4 *>(w));
             else kv_store(row + half * (D / 2) + s * H, *reinterpret_cast<kv_u32x2 *>(w));
         }
     }
     template <typename Turn> __device__ __forceinline__ void rotate(int pair_mode, Turn turn)
     {
-        half_t first[H], second[H];                           // the pairs' numbers, turned
-#pragma unroll
-        for (int e = 0; e < H; ++e) {
+        auto pair = [&](int i, int j, int e) {
             double sn, cs;
             turn(e, &sn, &cs);
-            const bool halves = pair_mode == IFLOW_ROPE_HALVES;
-            const double a = (double)(float)(halves ? x[e] : x[2 * e]), b = (double)(float)(halves ? x[H + e] : x[2 * e + 1]);
-            const half_t ra = kv_half_once(__builtin_fma(a, cs, -(b * sn))), rb = kv_half_once(__builtin_fma(a, sn, b * cs));
-            first[e] = ra; second[e] = rb;
-        }
+            const double a = (double)x[i], b = (double)x[j];
+            x[i] = (float)kv_half_once(__builtin_fma(a, cs, -(b * sn)));
+            x[j] = (float)kv_half_once(__builtin_fma(a, sn, b * cs));
+        };
+        if (pair_mode == IFLOW_ROPE_HALVES) {
 #pragma unroll
-        for (int e = 0; e < H; ++e) {
-            x[e] = pair_mode == IFLOW_ROPE_HALVES ? first[e] : e % 2 ? second[e / 2] : first[e / 2];
-            x[H + e] = pair_mode == IFLOW_ROPE_HALVES ? second[e] : e % 2 ? second[(H + e) / 2] : first[(H + e) / 2];
+            for (int e = 0; e < H; ++e) pair(e, H + e, e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < H; ++e) pair(2 * e, 2 * e + 1, e);
         }
     }
     // The lane's levels, as iflow_quantize_'s kernel finds them (multiplied by the reciprocal, divided where that could decide differently), and the headers of its blocks, by half of the head.
@@ -106,9 +109,9 @@ template <typename T> struct KvLane {
         float mn[2], mx[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            mn[half] = mx[half] = (float)x[half * H];
+            mn[half] = mx[half] = x[half * H];
 #pragma unroll
-            for (int e = 1; e < H; ++e) { mn[half] = fminf(mn[half], (float)x[half * H + e]); mx[half] = fmaxf(mx[half], (float)x[half * H + e]); }
+            for (int e = 1; e < H; ++e) { mn[half] = fminf(mn[half], x[half * H + e]); mx[half] = fmaxf(mx[half], x[half * H + e]); }
         }
         if (T::NB == 1) { mn[0] = mn[1] = fminf(mn[0], mn[1]); mx[0] = mx[1] = fmaxf(mx[0], mx[1]); }
 #pragma unroll
@@ -131,7 +134,7 @@ template <typename T> struct KvLane {
             float edge = 0.f;
 #pragma unroll
             for (int e = 0; e < H; ++e) {
-                const float f = __builtin_amdgcn_fmed3f(((float)x[half * H + e] - of) * rs, -1.0f, (float)T::L + 1.0f) + 0.5f;
+                const float f = __builtin_amdgcn_fmed3f((x[half * H + e] - of) * rs, -1.0f, (float)T::L + 1.0f) + 0.5f;
                 const float r = floorf(f);
                 edge = fmaxf(edge, fabsf((f - r) - 0.5f));
                 level[half * H + e] = (uint32_t)__builtin_amdgcn_fmed3f(r, 0.0f, (float)T::L);
@@ -139,7 +142,7 @@ template <typename T> struct KvLane {
             if (edge > 0.5f - 0.0001220703125f) {
 #pragma unroll
                 for (int e = 0; e < H; ++e) {
-                    const float t = ((float)x[half * H + e] - of) / sc;
+                    const float t = (x[half * H + e] - of) / sc;
                     float r = floorf(t);
                     r = t - r >= 0.5f ? r + 1.0f : r;
                     r = r >= 0.0f ? r : 0.0f;
@@ -183,9 +186,8 @@ __global__ __launch_bounds__(256) void kv_append_token_kernel(KvView v, const ui
     if (!seq.has(0)) return;
     const int line = blockIdx.y * 32 + r, kind = line < v.n_kv_heads ? 0 : line < 2 * v.n_kv_heads ? 1 : line < 2 * v.n_kv_heads + n_heads ? 2 : 3;
     const int head = line - min(kind, 2) * v.n_kv_heads, heads = kind >= 2 ? n_heads : v.n_kv_heads;
-    KvLane<T> lane;
     // (lines past the last: the last query head again, not stored)
-    lane.load((kind == 0 ? k_new : kind == 1 ? v_new : q) + ((int64_t)seq.row * heads + (kind == 3 ? n_heads - 1 : head)) * D, s);
+    const typename KvLane<T>::Words words = KvLane<T>::load((kind == 0 ? k_new : kind == 1 ? v_new : q) + ((int64_t)seq.row * heads + (kind == 3 ? n_heads - 1 : head)) * D, s);
     uint8_t *tile = kind < 2 ? kv_tile_at(v, b, head, (int)(seq.position / KV_TILE), T::BYTES) : nullptr;
     const int at = (int)(seq.position % KV_TILE), g = (at & 15) >> 2, k = (at >> 4) * 4 + (at & 3);
     // the values' pieces: a lane takes those of components s and s + 8 of every sixteen
@@ -198,6 +200,7 @@ __global__ __launch_bounds__(256) void kv_append_token_kernel(KvView v, const ui
     }
     if (tid < D / 2) kv_sincos((double)seq.position * exp2(-(2.0 * tid / D) * turns.log2_base), &s_turn[0][tid], &s_turn[1][tid]);
     __syncthreads();
+    KvLane<T> lane(words);
     if (kind != 1) {
         lane.rotate(turns.pair_mode, [&](int e, double *sn, double *cs) {
             const int pair = KvLane<T>::pair_of(s, e, turns.pair_mode);
@@ -271,28 +274,23 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvView v, const uin
     if (fresh == 0) return;
     const bool mine = fresh >> r & 1;
 
-    double sn[H], cs[H];
-    auto take_turns = [&] {
-        const double position = (double)(seq.position + token);
-        const double f0 = exp2(-(2.0 * KvLane<T>::pair_of(s, 0, turns.pair_mode) / D) * turns.log2_base);
-        const double f1 = turns.pair_mode == IFLOW_ROPE_HALVES ? f0 * turns.ratio[H / 2] : exp2(-(2.0 * KvLane<T>::pair_of(s, H / 2, turns.pair_mode) / D) * turns.log2_base);
-#pragma unroll
-        for (int e = 0; e < H; ++e) kv_sincos(position * ((e < H / 2 ? f0 : f1) * turns.ratio[e % (H / 2)]), &sn[e], &cs[e]);
-    };
-    auto turn = [&](int e, double *a, double *c) { *a = sn[e]; *c = cs[e]; };
+    const double position = (double)(seq.position + token), f0 = exp2(-(2.0 * KvLane<T>::pair_of(s, 0, turns.pair_mode) / D) * turns.log2_base);
+    const double f1 = turns.pair_mode == IFLOW_ROPE_HALVES ? f0 * turns.ratio[H / 2] : exp2(-(2.0 * KvLane<T>::pair_of(s, H / 2, turns.pair_mode) / D) * turns.log2_base);
+    auto turn = [&](int e, double *sn, double *cs) { kv_sincos(position * ((e < H / 2 ? f0 : f1) * turns.ratio[e % (H / 2)]), sn, cs); };
 
     // Query heads' workgroups stand evenly among the keys' and values': those wait for memory, these for instructions.
     const int groups = gridDim.y - v.n_kv_heads, group = blockIdx.y * groups / gridDim.y, next_group = (blockIdx.y + 1) * groups / gridDim.y;
     if (next_group > group) {                                 // query heads
         const int h0 = group * heads_per_group, h1 = min(n_heads, h0 + heads_per_group);
         if (!mine) return;
-        KvLane<T> next;
-        next.load(q + (row * n_heads + h0) * D, s);
-        take_turns();
+        typename KvLane<T>::Words next = KvLane<T>::load(q + (row * n_heads + h0) * D, s);
+        double sn[H], cs[H];
+#pragma unroll
+        for (int e = 0; e < H; ++e) turn(e, &sn[e], &cs[e]);
         for (int h = h0; h < h1; ++h) {
-            KvLane<T> lane = next;
-            if (h + 1 < h1) next.load(q + (row * n_heads + h + 1) * D, s);
-            lane.rotate(turns.pair_mode, turn);
+            KvLane<T> lane(next);
+            if (h + 1 < h1) next = KvLane<T>::load(q + (row * n_heads + h + 1) * D, s);
+            lane.rotate(turns.pair_mode, [&](int e, double *a, double *c) { *a = sn[e]; *c = cs[e]; });
             lane.store(q_out + (row * n_heads + h) * D, s);
         }
         return;
@@ -301,19 +299,16 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvView v, const uin
     // (a position that is new is in 0 .. max_seq - 1: no other tile is looked up)
     uint8_t *tile = kv_tile_at(v, b, head, (int)t, T::BYTES);
     if (!tile) return;
-    KvLane<T> key, value;
+    typename KvLane<T>::Words key_words = {}, value_words = {};
     if (mine) {
-        key.load(k_new + (row * v.n_kv_heads + head) * D, s);
-        value.load(v_new + (row * v.n_kv_heads + head) * D, s);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 2 * H; ++e) { key.x[e] = (half_t)0.f; value.x[e] = (half_t)0.f; }
+        key_words = KvLane<T>::load(k_new + (row * v.n_kv_heads + head) * D, s);
+        value_words = KvLane<T>::load(v_new + (row * v.n_kv_heads + head) * D, s);
     }
     if (fresh != 0xFFFFFFFFu) {
         for (int n = tid; n < T::BYTES / 16; n += 256) reinterpret_cast<kv_u32x4 *>(s_image)[n] = reinterpret_cast<const kv_u32x4 *>(tile)[n];
         __syncthreads();
     }
-    take_turns();
+    KvLane<T> key(key_words);
     key.rotate(turns.pair_mode, turn);
     uint32_t level[2 * H], header[2];
     key.quantize(level, header);
@@ -322,7 +317,7 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvView v, const uin
         if (mine && KvLane<T>::has_header(s, half)) s_image[T::KH_AT / 4 + kv_key_header(r, KvLane<T>::block_of(s, half)) / 2] = header[half];
         KvLane<T>::key_words(level + half * H, s, half, [&](int c, uint32_t w) { if (mine) s_image[kv_key_word<T>(r, c)] = w; });
     }
-    value.quantize(level, header);
+    KvLane<T>(value_words).quantize(level, header);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         if (mine && KvLane<T>::has_header(s, half)) {
