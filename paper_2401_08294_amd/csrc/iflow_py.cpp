@@ -2,13 +2,16 @@
 //
 // These kernels take a few microseconds each, as long as it takes to call them: through ctypes a product costs 1.5 us of marshalling and the
 // three-matrix call of a decoder layer 4, next to the 2.3 or more of the launch itself.  Here an address is one method call (data_ptr) and an array lives
-// on the stack.  Measured, us to enqueue, ctypes -> here: a product with one vector 5.2 -> 4.6, a decoder layer's six calls 43 -> 32.
+// on the stack.  Measured, us to enqueue, ctypes -> here: a product with one vector 5.2 -> 4.6, a decoder layer's six calls 43 -> 32, a token into the paged cache 4.9 -> 4.0.
 // The functions are the library's own, bound by address (bind), so the library is loaded once and in one place.  An address is an integer, None
-// (null) or an object with data_ptr(), a number what has __index__ or __float__, matrices and outputs are lists or tuples; a call returns the library's
+// (null) or an object with data_ptr(), a number what has __index__ or __float__, matrices and outputs are lists or tuples, a description an object of the class
+// that descriptions() was given; a call returns the library's
 // status and runs without the interpreter's lock, as a ctypes call does.  A call with anything else among its arguments (ctypes' own numbers, an iterator,
 // a text) is handed on as it is to the function that otherwise() was given, which takes or refuses it.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+
+#include <cstring>
 
 #include "../../include/iflow.h"
 
@@ -25,7 +28,11 @@ decltype(&iflow_qgemv_gated) p_qgemv_gated;
 decltype(&iflow_qgemm_fused) p_qgemm_fused;
 decltype(&iflow_attn_decode) p_attn_decode;
 decltype(&iflow_rope_append) p_rope_append;
+decltype(&iflow_kv_append) p_kv_append;
+decltype(&iflow_kv_read) p_kv_read;
+decltype(&iflow_kv_attn) p_kv_attn;
 PyObject *s_data_ptr, *general;                                // general(name, arguments ...): the call that takes every form of argument
+PyTypeObject *cache_type, *batch_type;                         // the classes of iflow_kv_cache_t and iflow_kv_batch_t
 
 // One call's arguments in order; the first that does not fit ends the reading (bad; perhaps a Python exception) and turns the rest into zeros.
 struct Args {
@@ -84,6 +91,19 @@ struct Args {
         const double v = PyFloat_AsDouble(o);
         if (v == -1.0 && PyErr_Occurred()) bad = true;
         return (float)v;
+    }
+    // a description: an object of its class, whose memory it is (copied: another thread may write to it meanwhile)
+    template <typename T> T description(PyTypeObject *type)
+    {
+        PyObject *o = next();
+        T d = {};
+        if (!o) return d;
+        Py_buffer memory;
+        if (!type || !PyObject_TypeCheck(o, type) || PyObject_GetBuffer(o, &memory, PyBUF_SIMPLE) != 0) { bad = true; return d; }
+        if (memory.len >= (Py_ssize_t)sizeof(T)) memcpy(&d, memory.buf, sizeof(T));
+        else bad = true;
+        PyBuffer_Release(&memory);
+        return d;
     }
     // a list of addresses or of whole numbers, its first MAX_ARRAY entries; its length, or -1 for None
     template <typename Put> Py_ssize_t each(Put put)
@@ -282,13 +302,52 @@ PyObject *rope_append(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     });
 }
 
-// bind(addresses of the nine functions, in this order)
+PyObject *kv_append(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a("kv_append", args, nargs, 10);
+    const iflow_kv_cache_t cache = a.description<iflow_kv_cache_t>(cache_type);
+    const iflow_kv_batch_t batch = a.description<iflow_kv_batch_t>(batch_type);
+    const uint16_t *q = a.ptr<const uint16_t>(), *k = a.ptr<const uint16_t>(), *v = a.ptr<const uint16_t>();
+    const int heads = a.word();
+    const float base = a.real();
+    const int pairing = a.word();
+    uint16_t *q_out = a.ptr<uint16_t>();
+    void *stream = a.handle();
+    return run(a, [&] { return p_kv_append(&cache, &batch, q, k, v, heads, base, (iflow_rope_pairing_t)pairing, q_out, stream); });
+}
+
+PyObject *kv_read(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a("kv_read", args, nargs, 5);
+    const iflow_kv_cache_t cache = a.description<iflow_kv_cache_t>(cache_type);
+    const iflow_kv_batch_t batch = a.description<iflow_kv_batch_t>(batch_type);
+    uint16_t *k = a.ptr<uint16_t>(), *v = a.ptr<uint16_t>();
+    void *stream = a.handle();
+    return run(a, [&] { return p_kv_read(&cache, &batch, k, v, stream); });
+}
+
+PyObject *kv_attn(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a("kv_attn", args, nargs, 9);
+    const iflow_kv_cache_t cache = a.description<iflow_kv_cache_t>(cache_type);
+    const iflow_kv_batch_t batch = a.description<iflow_kv_batch_t>(batch_type);
+    const uint16_t *q = a.ptr<const uint16_t>();
+    const int heads = a.word();
+    const float scale = a.real();
+    uint16_t *out = a.ptr<uint16_t>();
+    void *workspace = a.ptr<void>();
+    const int64_t bytes = a.num();
+    void *stream = a.handle();
+    return run(a, [&] { return p_kv_attn(&cache, &batch, q, heads, scale, out, workspace, (size_t)bytes, stream); });
+}
+
+// bind(addresses of the twelve functions, in this order)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    Args a("bind", args, nargs, 9);
-    void *f[9];
+    Args a("bind", args, nargs, 12);
+    void *f[12];
     for (void *&p : f) p = a.handle();
-    if (a.bad) { PyErr_SetString(PyExc_TypeError, "nine addresses are wanted"); return nullptr; }
+    if (a.bad) { PyErr_SetString(PyExc_TypeError, "twelve addresses are wanted"); return nullptr; }
     p_quantize = reinterpret_cast<decltype(p_quantize)>(f[0]);
     p_dequant = reinterpret_cast<decltype(p_dequant)>(f[1]);
     p_qgemv = reinterpret_cast<decltype(p_qgemv)>(f[2]);
@@ -298,6 +357,9 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     p_qgemm_fused = reinterpret_cast<decltype(p_qgemm_fused)>(f[6]);
     p_attn_decode = reinterpret_cast<decltype(p_attn_decode)>(f[7]);
     p_rope_append = reinterpret_cast<decltype(p_rope_append)>(f[8]);
+    p_kv_append = reinterpret_cast<decltype(p_kv_append)>(f[9]);
+    p_kv_read = reinterpret_cast<decltype(p_kv_read)>(f[10]);
+    p_kv_attn = reinterpret_cast<decltype(p_kv_attn)>(f[11]);
     Py_RETURN_NONE;
 }
 
@@ -311,10 +373,22 @@ PyObject *otherwise(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     Py_RETURN_NONE;
 }
 
+// descriptions(class of iflow_kv_cache_t, class of iflow_kv_batch_t)
+PyObject *descriptions(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    if (nargs != 2 || !PyType_Check(args[0]) || !PyType_Check(args[1])) { PyErr_SetString(PyExc_TypeError, "two classes are wanted"); return nullptr; }
+    PyTypeObject *was[2] = {cache_type, batch_type};
+    cache_type = reinterpret_cast<PyTypeObject *>(Py_NewRef(args[0]));
+    batch_type = reinterpret_cast<PyTypeObject *>(Py_NewRef(args[1]));
+    Py_XDECREF(was[0]);
+    Py_XDECREF(was[1]);
+    Py_RETURN_NONE;
+}
+
 #define IFLOW_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {IFLOW_METHOD(bind), IFLOW_METHOD(otherwise), IFLOW_METHOD(quantize), IFLOW_METHOD(dequant), IFLOW_METHOD(qgemv), IFLOW_METHOD(qgemm),
                          IFLOW_METHOD(qgemv_fused), IFLOW_METHOD(qgemv_gated), IFLOW_METHOD(qgemm_fused), IFLOW_METHOD(attn_decode),
-                         IFLOW_METHOD(rope_append), {nullptr, nullptr, 0, nullptr}};
+                         IFLOW_METHOD(rope_append), IFLOW_METHOD(kv_append), IFLOW_METHOD(kv_read), IFLOW_METHOD(kv_attn), IFLOW_METHOD(descriptions), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

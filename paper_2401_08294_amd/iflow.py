@@ -70,7 +70,7 @@ _lib = None
 _native = None                 # the extension, bound to the library's functions (without one: the same calls through ctypes)
 # Enqueueing from Python, us, ctypes / here: a product with one vector 5.2 / 4.6, the attention's two launches 8.6 / 7.7, a decoder layer's six calls (seven
 # launches) 43 / 32 (on another host 4.4 / 3.7, 7.1 / 6.1, 35.0 / 24.6) - of which 2.3 and more a launch are the launch itself.
-_NATIVE_CALLS = ("quantize", "dequant", "qgemv", "qgemm", "qgemv_fused", "qgemv_gated", "qgemm_fused", "attn_decode", "rope_append")
+_NATIVE_CALLS = ("quantize", "dequant", "qgemv", "qgemm", "qgemv_fused", "qgemv_gated", "qgemm_fused", "attn_decode", "rope_append", "kv_append", "kv_read", "kv_attn")
 
 
 class ArgumentError(C.ArgumentError, TypeError):
@@ -126,6 +126,18 @@ class _Ctypes:
     def rope_append(q, k_new, v_new, n_heads, n_kv_heads, head_dim, position, max_seq, base, pair_mode, k_cache, v_cache, stream):
         return _lib.iflow_rope_append(_ptr(q), _ptr(k_new), _ptr(v_new), n_heads, n_kv_heads, head_dim, position, max_seq, base, pair_mode,
                                       _ptr(k_cache), _ptr(v_cache), stream)
+
+    @staticmethod
+    def kv_append(cache, batch, q, k_new, v_new, n_heads, base, pair_mode, q_out, stream):
+        return _lib.iflow_kv_append(cache, batch, _ptr(q), _ptr(k_new), _ptr(v_new), n_heads, base, pair_mode, _ptr(q_out), stream)
+
+    @staticmethod
+    def kv_read(cache, batch, k_out, v_out, stream):
+        return _lib.iflow_kv_read(cache, batch, _ptr(k_out), _ptr(v_out), stream)
+
+    @staticmethod
+    def kv_attn(cache, batch, q, n_heads, scale, out, workspace, workspace_bytes, stream):
+        return _lib.iflow_kv_attn(cache, batch, _ptr(q), n_heads, scale, _ptr(out), _ptr(workspace), workspace_bytes, stream)
 
 
 def _through_ctypes(name, *args):
@@ -202,6 +214,7 @@ def lib():
         L.iflow_decode_stack_plan.argtypes = [C.POINTER(DecodeStack), p, sz, p, sz, p, C.POINTER(Chain)]
         L.iflow_decode_stack_launch.argtypes = [C.POINTER(Chain), i64, p]
         if native is not None:
+            native.descriptions(KvCache, KvBatch)
             native.bind(*[C.cast(getattr(L, "iflow_" + name), p).value for name in _NATIVE_CALLS])
             native.otherwise(_through_ctypes)
         else:
@@ -399,12 +412,12 @@ def kv_cache_bytes(cache: KvCache) -> int:
 def kv_append(cache: KvCache, batch: KvBatch, q, k_new, v_new, n_heads: int, base: float, pair_mode: int, q_out, stream=None) -> None:
     """Rotary position embedding of the batch's tokens: q [n_tokens][n_heads][head_dim] rotated into q_out (or q itself), rotated k_new and v_new [n_tokens][n_kv_heads][head_dim]
     quantized into the cache."""
-    _check(lib().iflow_kv_append(C.byref(cache), C.byref(batch), _ptr(q), _ptr(k_new), _ptr(v_new), n_heads, base, pair_mode, _ptr(q_out), _stream(stream)), "iflow_kv_append")
+    _check((_native or _calls()).kv_append(cache, batch, q, k_new, v_new, n_heads, base, pair_mode, q_out, _stream(stream)), "iflow_kv_append")
 
 
 def kv_read(cache: KvCache, batch: KvBatch, k_out, v_out, stream=None) -> None:
     """The keys and values of the batch's tokens as the cache holds them, fp16 [n_tokens][n_kv_heads][head_dim]."""
-    _check(lib().iflow_kv_read(C.byref(cache), C.byref(batch), _ptr(k_out), _ptr(v_out), _stream(stream)), "iflow_kv_read")
+    _check((_native or _calls()).kv_read(cache, batch, k_out, v_out, _stream(stream)), "iflow_kv_read")
 
 
 def kv_attn_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int) -> int:
@@ -415,7 +428,7 @@ def kv_attn_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int) -> int
 
 def kv_attn(cache: KvCache, batch: KvBatch, q, n_heads: int, scale: float, out, workspace, workspace_bytes: int, stream=None) -> None:
     """Causal grouped-query attention of the batch's tokens, q [n_tokens][n_heads][head_dim], over their sequences' cached positions."""
-    _check(lib().iflow_kv_attn(C.byref(cache), C.byref(batch), _ptr(q), n_heads, scale, _ptr(out), _ptr(workspace), workspace_bytes, _stream(stream)), "iflow_kv_attn")
+    _check((_native or _calls()).kv_attn(cache, batch, q, n_heads, scale, out, workspace, workspace_bytes, _stream(stream)), "iflow_kv_attn")
 
 
 def qgemv_chain_workspace_bytes(rows_list) -> int:

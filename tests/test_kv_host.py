@@ -137,3 +137,57 @@ def test_refusals_before_any_launch(iflow):  # noqa: F811
     with pytest.raises(iflow.IflowError) as info:
         iflow.kv_attn(iflow.kv_cache(iflow.Q4_B64, 8, 128, 64, 10, at), iflow.kv_batch(2, 4, None, at + 4, 200), 2 * at, 32, 0.1, 3 * at, 4 * at, 1 << 30, stream=0)
     assert info.value.status == iflow.ERR_ALIGN
+
+
+def test_extension_hands_the_cache_calls_on(iflow):  # noqa: F811
+    """The three calls through the Python extension: every argument in its place, the descriptions by their contents, wrong types refused before anything is called."""
+    L = iflow.lib()
+    native = iflow._native
+    names = ("kv_append", "kv_read", "kv_attn")
+    seen = {}
+
+    class Tensor:
+        def __init__(self, address):
+            self.address = address
+
+        def data_ptr(self):
+            return self.address
+
+    def fields(d):
+        return tuple(getattr(d, name) for name, _ in d._fields_)
+
+    def recorder(name):
+        def record(cache, batch, *args):
+            seen[name] = (fields(cache.contents), fields(batch.contents)) + args
+            return iflow.ERR_SHAPE
+        return C.CFUNCTYPE(C.c_int, *getattr(L, "iflow_" + name).argtypes)(record)
+    fakes = {name: recorder(name) for name in names}
+    real = [C.cast(getattr(L, "iflow_" + name), C.c_void_p).value for name in iflow._NATIVE_CALLS]
+    native.bind(*[C.cast(fakes[name], C.c_void_p).value if name in fakes else at for name, at in zip(iflow._NATIVE_CALLS, real)])
+    cache, batch = iflow.kv_cache(4, 5, 6, 7, 8 << 40, Tensor(9 << 40)), iflow.kv_batch(2, 3, Tensor(4 << 40), 5, 6, first_token=7, n_tokens=8 << 33, max_tokens=9)
+    c, b = (4, 5, 6, 7, 8 << 40, 9 << 40), (2, 3, 4 << 40, 5, 7, 8 << 33, 9, 6)
+    try:
+        def call(f, *args, **kw):
+            with pytest.raises(iflow.IflowError) as info:
+                f(*args, **kw)
+            assert info.value.status == iflow.ERR_SHAPE
+        call(iflow.kv_append, cache, batch, 11, Tensor(12), 13, 14, 0.5, 1, 15, stream=16)
+        assert seen["kv_append"] == (c, b, 11, 12, 13, 14, 0.5, 1, 15, 16)
+        call(iflow.kv_read, cache, batch, 11, Tensor(12), stream=16)
+        assert seen["kv_read"] == (c, b, 11, 12, 16)
+        call(iflow.kv_attn, cache, batch, Tensor(11), 12, 0.25, 13, None, 14 << 40, stream=16)
+        assert seen["kv_attn"] == (c, b, 11, 12, 0.25, 13, None, 14 << 40, 16)
+        seen.clear()
+        for wrong in (lambda: iflow.kv_read(batch, cache, 1, 2, stream=3), lambda: iflow.kv_read(bytes(32), batch, 1, 2, stream=3), lambda: iflow.kv_read(cache, 1, 2, 3, stream=4),
+                      lambda: iflow.kv_attn(cache, batch, "q", 1, 0.5, 2, 3, 4, stream=5), lambda: iflow.kv_append(cache, batch, 1, 2, 3, 4.5, 0.5, 1, 6, stream=7)):
+            with pytest.raises((TypeError, ValueError, AttributeError)):
+                wrong()
+        assert not seen
+    finally:
+        native.bind(*real)
+    cache, batch = iflow.kv_cache(iflow.Q4_B64, 8, 128, 64, 8, 64), iflow.kv_batch(2, 4, None, 64, 200)
+    for f in (lambda c, b: iflow.kv_append(c, b, 64, 128, 192, 32, 1e4, 1, 64, stream=0), lambda c, b: iflow.kv_read(c, b, 64, 128, stream=0), lambda c, b: iflow.kv_attn(c, b, 64, 32, 1.0, 128, 192, 64, stream=0)):
+        for given in ((None, batch), (cache, None)):           # (no description: the library's own answer)
+            with pytest.raises(iflow.IflowError) as info:
+                f(*given)
+            assert info.value.status == iflow.ERR_NULL
