@@ -389,6 +389,7 @@ static iflow_status_t kv_shapes(const iflow_kv_cache_t *c, const iflow_kv_batch_
     if (b->n_seqs < 1 || b->n_seqs > 65535 || b->max_pages < 1) return IFLOW_ERR_SHAPE;
     if (b->max_seq < 1 || b->max_seq > (1 << 20) || b->max_seq > (int64_t)b->max_pages * c->page_positions) return IFLOW_ERR_SHAPE;
     if (b->max_tokens < 1 || b->max_tokens > b->max_seq || b->n_tokens < 1 || b->n_tokens > (1LL << 24)) return IFLOW_ERR_SHAPE;
+    if ((int64_t)b->n_seqs * b->max_tokens > (1LL << 24)) return IFLOW_ERR_SHAPE;
     if (!b->first_token && (b->max_tokens != 1 || b->n_tokens < b->n_seqs)) return IFLOW_ERR_SHAPE;
     if (!b->page_table && (int64_t)b->n_seqs * b->max_pages > c->n_pages) return IFLOW_ERR_SHAPE;
     *v = {static_cast<uint8_t *>(c->pages), b->page_table, b->seq_lens, b->first_token, c->n_pages, b->n_tokens, page_bytes,
@@ -400,9 +401,11 @@ static iflow_status_t kv_shapes(const iflow_kv_cache_t *c, const iflow_kv_batch_
 static iflow_status_t kv_pointers(const iflow::KvView &v)
 {
     if (!v.pages || !v.lens) return IFLOW_ERR_NULL;
-    if (!aligned16(v.pages) || !aligned16(v.lens) || !aligned16(v.table) || !aligned16(v.first)) return IFLOW_ERR_ALIGN;
+    if (!aligned16(v.pages) || ((reinterpret_cast<uintptr_t>(v.lens) | reinterpret_cast<uintptr_t>(v.table) | reinterpret_cast<uintptr_t>(v.first)) & 3) != 0) return IFLOW_ERR_ALIGN;
     return IFLOW_OK;
 }
+
+static bool overlaps_pages(const iflow::KvView &v, const void *p, int64_t n) { return overlaps(p, n, v.pages, v.n_pages * v.page_bytes); }
 
 iflow_status_t iflow_kv_cache_bytes(const iflow_kv_cache_t *cache, size_t *bytes)
 {
@@ -429,7 +432,7 @@ iflow_status_t iflow_kv_append(const iflow_kv_cache_t *cache, const iflow_kv_bat
     const int64_t q_bytes = v.n_tokens * n_heads * cache->head_dim * 2, kv_bytes = v.n_tokens * v.n_kv_heads * cache->head_dim * 2;
     // rows are read and written by different workgroups: only a row in its own place is read before it is written
     if (q_out != q && overlaps(q_out, q_bytes, q, q_bytes)) return IFLOW_ERR_SHAPE;
-    if (overlaps(q_out, q_bytes, k_new, kv_bytes) || overlaps(q_out, q_bytes, v_new, kv_bytes)) return IFLOW_ERR_SHAPE;
+    if (overlaps(q_out, q_bytes, k_new, kv_bytes) || overlaps(q_out, q_bytes, v_new, kv_bytes) || overlaps_pages(v, q_out, q_bytes)) return IFLOW_ERR_SHAPE;
     return device_status(iflow::launch_kv_append((int)cache->format, cache->head_dim, v, q, k_new, v_new, n_heads, (double)base, (int)pair_mode, q_out, (hipStream_t)stream));
 }
 
@@ -443,7 +446,7 @@ iflow_status_t iflow_kv_read(const iflow_kv_cache_t *cache, const iflow_kv_batch
     if (st != IFLOW_OK) return st;
     if (!aligned16(k_out) || !aligned16(v_out)) return IFLOW_ERR_ALIGN;
     const int64_t bytes = v.n_tokens * v.n_kv_heads * cache->head_dim * 2;
-    if (overlaps(k_out, bytes, v_out, bytes)) return IFLOW_ERR_SHAPE;
+    if (overlaps(k_out, bytes, v_out, bytes) || overlaps_pages(v, k_out, bytes) || overlaps_pages(v, v_out, bytes)) return IFLOW_ERR_SHAPE;
     return device_status(iflow::launch_kv_read((int)cache->format, cache->head_dim, v, k_out, v_out, (hipStream_t)stream));
 }
 
@@ -473,7 +476,8 @@ iflow_status_t iflow_kv_attn(const iflow_kv_cache_t *cache, const iflow_kv_batch
     if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return IFLOW_ERR_ALIGN;
     if (workspace_bytes < need) return IFLOW_ERR_SIZE;
     const int64_t bytes = v.n_tokens * n_heads * cache->head_dim * 2;
-    if (overlaps(out, bytes, q, bytes)) return IFLOW_ERR_SHAPE;
+    if (overlaps(out, bytes, q, bytes) || overlaps_pages(v, out, bytes)) return IFLOW_ERR_SHAPE;
+    if (need && (overlaps(workspace, (int64_t)need, q, bytes) || overlaps(workspace, (int64_t)need, out, bytes) || overlaps_pages(v, workspace, (int64_t)need))) return IFLOW_ERR_SHAPE;
     return device_status(iflow::launch_kv_attn((int)cache->format, cache->head_dim, v, q, n_heads, scale, out, workspace, (hipStream_t)stream));
 }
 

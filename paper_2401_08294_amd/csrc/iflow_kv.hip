@@ -423,7 +423,6 @@ hipError_t launch_kv_append(int format, int head_dim, const KvView &v, const uin
                             uint16_t *q_out, hipStream_t s)
 {
     const int64_t tiles = kv_tiles_touched(v), grid = tiles * v.n_seqs;
-    if (grid > 0x7fffffff) return hipErrorInvalidValue;
     KvTurns turns;
     turns.log2_base = log2(base);
     turns.pair_mode = pair_mode;
@@ -447,7 +446,6 @@ hipError_t launch_kv_append(int format, int head_dim, const KvView &v, const uin
 hipError_t launch_kv_read(int format, int head_dim, const KvView &v, uint16_t *k_out, uint16_t *v_out, hipStream_t s)
 {
     const int64_t tiles = kv_tiles_touched(v), grid = tiles * v.n_seqs;
-    if (grid > 0x7fffffff) return hipErrorInvalidValue;
     return for_kv_tile(format, head_dim, [&](auto tag) {
         typedef decltype(tag) T;
         hipLaunchKernelGGL((kv_read_kernel<T>), dim3((unsigned)grid, (unsigned)v.n_kv_heads), dim3(256), 0, s, v, k_out, v_out, (int)tiles);

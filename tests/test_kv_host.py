@@ -101,7 +101,7 @@ def test_refusals_before_any_launch(iflow):  # noqa: F811
                 dict(n_pages=0), dict(n_pages=1 << 31), dict(n_pages=(1 << 31) - 1, page_positions=1 << 20)):
         refused(iflow.ERR_SHAPE, cache=bad)
     for bad in (dict(n_seqs=0), dict(n_seqs=65536), dict(max_pages=0), dict(max_seq=0), dict(max_seq=1281), dict(max_seq=(1 << 20) + 1, max_pages=1 << 20), dict(max_tokens=0),
-                dict(max_tokens=1281), dict(n_tokens=0), dict(n_tokens=(1 << 24) + 1), dict(first_token=None), dict(first_token=None, max_tokens=1, n_tokens=3), dict(page_table=None, max_pages=26)):
+                dict(max_tokens=1281), dict(n_tokens=0), dict(n_tokens=(1 << 24) + 1), dict(n_seqs=(1 << 14) + 1, max_tokens=1 << 10), dict(first_token=None), dict(first_token=None, max_tokens=1, n_tokens=3), dict(page_table=None, max_pages=26)):
         refused(iflow.ERR_SHAPE, batch=bad)
     for heads in (0, 12, 520, -8):
         refused(iflow.ERR_SHAPE, heads=heads)
@@ -109,7 +109,7 @@ def test_refusals_before_any_launch(iflow):  # noqa: F811
     refused(iflow.ERR_NULL, batch=dict(seq_lens=None))
     refused(iflow.ERR_ALIGN, cache=dict(pages=at + 8))
     for name in ("page_table", "seq_lens", "first_token"):
-        refused(iflow.ERR_ALIGN, batch={name: at + 4})
+        refused(iflow.ERR_ALIGN, batch={name: at + 2})
     c, b = made(iflow.KvCache, good_cache, {}), made(iflow.KvBatch, good_batch, {})
     n = 9 * 32 * 128 * 2
     for args, status in (((None, 4 * at, 5 * at, 32, 10000.0, 1, 3 * at), iflow.ERR_NULL), ((2 * at, None, 5 * at, 32, 10000.0, 1, 3 * at), iflow.ERR_NULL),
@@ -131,11 +131,22 @@ def test_refusals_before_any_launch(iflow):  # noqa: F811
     assert L.iflow_kv_append(None, b, at, at, at, 32, 10000.0, 1, at, None) == iflow.ERR_NULL and L.iflow_kv_append(c, None, at, at, at, 32, 10000.0, 1, at, None) == iflow.ERR_NULL
     assert L.iflow_kv_cache_bytes(c, None) == iflow.ERR_NULL and L.iflow_kv_cache_bytes(None, C.byref(C.c_size_t(0))) == iflow.ERR_NULL
     assert L.iflow_kv_attn_workspace_bytes(c, b, 32, None) == iflow.ERR_NULL
+    # the pool and the workspace, each begun in front of and ended behind
+    pool, far = 100 * 8 * 2 * 4608, 0x10000000
+    c = made(iflow.KvCache, good_cache, dict(pages=far))
+    assert iflow.kv_cache_bytes(c) == pool and need % 16 == 0 and need < far // 4
+    for near in (far + pool - 16, far + 16 - 9 * 8 * 128 * 2):
+        assert L.iflow_kv_read(c, b, near, at, None) == iflow.ERR_SHAPE and L.iflow_kv_read(c, b, at, near, None) == iflow.ERR_SHAPE
+    for near in (far + pool - 16, far + 16 - n):
+        assert L.iflow_kv_append(c, b, 20 * at, 21 * at, 22 * at, 32, 10000.0, 1, near, None) == iflow.ERR_SHAPE
+        assert L.iflow_kv_attn(c, b, 20 * at, 32, 0.1, near, 30 * at, need, None) == iflow.ERR_SHAPE
+    for ws in (2 * far + n - 16, 2 * far + 16 - need, 3 * far + n - 16, 3 * far + 16 - need, far + pool - 16, far + 16 - need):
+        assert L.iflow_kv_attn(c, b, 2 * far, 32, 0.1, 3 * far, ws, need, None) == iflow.ERR_SHAPE, ws
     many = made(iflow.KvBatch, good_batch, dict(max_tokens=1 << 20, max_seq=1 << 20, max_pages=1 << 14))
     assert L.iflow_kv_attn(c, many, 2 * at, 64, 0.1, 3 * at, 8 * at, 1 << 40, None) == iflow.ERR_SHAPE
     # through the binding: the same, as an error
     with pytest.raises(iflow.IflowError) as info:
-        iflow.kv_attn(iflow.kv_cache(iflow.Q4_B64, 8, 128, 64, 10, at), iflow.kv_batch(2, 4, None, at + 4, 200), 2 * at, 32, 0.1, 3 * at, 4 * at, 1 << 30, stream=0)
+        iflow.kv_attn(iflow.kv_cache(iflow.Q4_B64, 8, 128, 64, 10, at), iflow.kv_batch(2, 4, None, at + 2, 200), 2 * at, 32, 0.1, 3 * at, 4 * at, 1 << 30, stream=0)
     assert info.value.status == iflow.ERR_ALIGN
 
 
