@@ -64,9 +64,40 @@ struct KvSequence {
     __device__ __forceinline__ bool has_row(int i) const { return (uint32_t)i < (uint32_t)count && (uint32_t)row + (uint32_t)i < (uint32_t)n_tokens; }
     __device__ __forceinline__ bool has(int i) const { return has_row(i) && (uint32_t)position + (uint32_t)i < (uint32_t)max_seq; }
     __device__ __forceinline__ int first_tile() const { return position >> 5; }          // (rounded down, also below zero)
+    __device__ __forceinline__ int tiles() const { return count > 0 ? ((position & (KV_TILE - 1)) + count + KV_TILE - 1) >> 5 : 0; }       // that its tokens lie in
     // positions that token i sees: its own and all before
     __device__ __forceinline__ int sees(int i) const { return max(0, min((int)((uint32_t)position + (uint32_t)i + 1u), max_seq)); }
 };
+
+// inclusive sum over the lanes up to this one
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);       // row_shr 1, 2, 4, 8: within rows of sixteen
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);       // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);       // row_bcast:31 into rows 2 and 3
+    return x;
+}
+// Number w of all sequences' units, units(b) of each, in order: whose it is (b), and which of that sequence's (w); false past the last.  By every wavefront alike, 64 sequences at a time.
+// For batches whose longest sequence has many more tokens than most, where a grid of max_tokens for each would be workgroups with nothing to do.
+template <typename Units> __device__ __forceinline__ bool kv_find(const KvView &v, int &w, int &b, Units units)
+{
+    const int lane = threadIdx.x & 63;
+    for (b = 0; b < v.n_seqs; b += 64) {
+        const int mine = b + lane < v.n_seqs ? units(KvSequence(v, b + lane)) : 0, upto = wave_scan(mine);
+        const uint64_t mask = __builtin_amdgcn_ballot_w64(upto > w);
+        if (mask != 0) {
+            const int skip = __builtin_ctzll(mask);
+            b += skip;
+            w -= __builtin_amdgcn_readlane(upto - mine, skip);
+            return true;
+        }
+        w -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
 
 // The tile that holds positions 32 t .. 32 t + 31 of sequence b; null where its page is none of the cache's.  (t < max_seq / 32, rounded up: inside the table's row.)
 __device__ __forceinline__ int64_t kv_page(const KvView &v, int b, int p)

@@ -172,6 +172,22 @@ template <typename T> struct KvLane {
     }
 };
 
+// Workgroup x of a head runs for tile x % tiles_per_seq of sequence x / tiles_per_seq, or, FIND, for the x-th, the x + grid-th, .. of the tiles that there are.
+template <bool FIND, typename Do> __device__ __forceinline__ void kv_each_tile(const KvView &v, int tiles_per_seq, Do run)
+{
+    if constexpr (FIND) {
+        for (int x = blockIdx.x, b, nth; nth = x, kv_find(v, nth, b, [](const KvSequence &seq) { return seq.tiles(); }); x += gridDim.x) {
+            int tid = threadIdx.x;
+            asm volatile("" : "+v"(tid));                     // (made anew for every tile: what follows from it is not kept in registers from one to the next)
+            run(b, nth, tid);
+            __syncthreads();                                  // (what run() has in LDS has been read)
+        }
+    } else {
+        const int b = blockIdx.x / (unsigned)tiles_per_seq;
+        run(b, (int)blockIdx.x - b * tiles_per_seq, (int)threadIdx.x);
+    }
+}
+
 // One token per sequence: a workgroup takes 32 rows of one token, keys' heads first, then values', then queries'.  Bound by the latency of what follows on one another: the sequence's length, its page, the
 // row, and for values the words that eight positions share (read, changed, written by one lane; requested as soon as the page is known).
 template <typename T>
@@ -259,16 +275,15 @@ __global__ __launch_bounds__(256) void kv_append_token_kernel(KvView v, const ui
 // Any number of tokens: a workgroup takes the new positions of one tile, of one key/value head or of several query heads.  A tile is put together in LDS, over what it held where
 // positions of it are older, and leaves in 16-byte pieces; nobody else writes it in this call.
 template <typename T>
-__global__ __launch_bounds__(256) void kv_append_tile_kernel(KvView v, const uint16_t *q, const uint16_t *__restrict__ k_new, const uint16_t *__restrict__ v_new, int n_heads, KvTurns turns,
-                                                             uint16_t *q_out, int tiles_per_seq, int heads_per_group)
+__device__ __forceinline__ void kv_append_tile(const KvView &v, int b, int nth, int tid, const uint16_t *q, const uint16_t *__restrict__ k_new, const uint16_t *__restrict__ v_new, int n_heads,
+                                               const KvTurns &turns, uint16_t *q_out, int heads_per_group)
 {
     constexpr int D = T::D, H = KV_PART<T>;
     __shared__ __align__(16) uint32_t s_image[T::BYTES / 4];
     __shared__ __align__(16) uint8_t s_level[KV_TILE][D];
-    const int tid = threadIdx.x, r = tid >> 3, s = tid & 7;
-    const int b = blockIdx.x / tiles_per_seq;
+    const int r = tid >> 3, s = tid & 7;
     const KvSequence seq(v, b);
-    const int t = seq.first_tile() + (int)(blockIdx.x - b * tiles_per_seq), first_token = (int)((uint32_t)t * KV_TILE - (uint32_t)seq.position), token = first_token + r;
+    const int t = seq.first_tile() + nth, first_token = (int)((uint32_t)t * KV_TILE - (uint32_t)seq.position), token = first_token + r;
     const int64_t row = (int64_t)seq.row + token;
     const uint32_t fresh = (uint32_t)__builtin_amdgcn_ballot_w64(seq.has(first_token + (tid & 31)));       // positions of the tile that are new
     if (fresh == 0) return;
@@ -361,17 +376,23 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvView v, const uin
     for (int n = tid; n < T::BYTES / 16; n += 256) reinterpret_cast<kv_u32x4 *>(tile)[n] = reinterpret_cast<const kv_u32x4 *>(s_image)[n];
 }
 
+template <typename T, bool FIND>
+__global__ __launch_bounds__(256) void kv_append_tile_kernel(KvView v, const uint16_t *q, const uint16_t *__restrict__ k_new, const uint16_t *__restrict__ v_new, int n_heads, KvTurns turns,
+                                                             uint16_t *q_out, int tiles_per_seq, int heads_per_group)
+{
+    kv_each_tile<FIND>(v, tiles_per_seq, [&](int b, int nth, int tid) { kv_append_tile<T>(v, b, nth, tid, q, k_new, v_new, n_heads, turns, q_out, heads_per_group); });
+}
+
 // ---- read back ----------------------------------------------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(256) void kv_read_kernel(KvView v, uint16_t *__restrict__ k_out, uint16_t *__restrict__ v_out, int tiles_per_seq)
+__device__ __forceinline__ void kv_read_tile(const KvView &v, int b, int nth, int tid, uint16_t *__restrict__ k_out, uint16_t *__restrict__ v_out)
 {
     constexpr int D = T::D, ROW = D + 8;
     const KvMagic magic;
     __shared__ __align__(16) uint16_t s_value[KV_TILE][ROW];
-    const int tid = threadIdx.x, head = blockIdx.y;
-    const int b = blockIdx.x / tiles_per_seq;
+    const int head = blockIdx.y;
     const KvSequence seq(v, b);
-    const int t = seq.first_tile() + (int)(blockIdx.x - b * tiles_per_seq), first_token = (int)((uint32_t)t * KV_TILE - (uint32_t)seq.position);
+    const int t = seq.first_tile() + nth, first_token = (int)((uint32_t)t * KV_TILE - (uint32_t)seq.position);
     auto has = [&](int p) { return seq.has_row(first_token + p); };
     bool any = false;
     for (int i = 0; i < KV_TILE; ++i) any |= has(i);
@@ -416,19 +437,32 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvView v, uint16_t *__rest
     }
 }
 
-// tiles that a sequence's new tokens can touch, wherever they begin
-static int64_t kv_tiles_touched(const KvView &v) { return (v.max_tokens + 2 * KV_TILE - 2) / KV_TILE; }
+template <typename T, bool FIND>
+__global__ __launch_bounds__(256) void kv_read_kernel(KvView v, uint16_t *__restrict__ k_out, uint16_t *__restrict__ v_out, int tiles_per_seq)
+{
+    kv_each_tile<FIND>(v, tiles_per_seq, [&](int b, int nth, int tid) { kv_read_tile<T>(v, b, nth, tid, k_out, v_out); });
+}
+
+// The tiles of a call: as many for each sequence as max_tokens can touch, wherever they begin, or, if the batch's rows touch fewer together, as many as those, to be found by the kernel.
+// (Us, one way / the other: 2000 tokens of one sequence and one each of 63 others appended 193 / 27, of 255 others 693 / 58: 196 thousand workgroups, the few with work of the others all on one die; prompts of
+// 5400 tokens, the longest 2000 of four, 37.5 / 34; 12 sequences of up to 777 positions read back 9.9 / 9.2.)
+struct KvGrid { int64_t all; int per_seq; };
+static KvGrid kv_grid(const KvView &v)
+{
+    const int64_t per_seq = (v.max_tokens + 2 * KV_TILE - 2) / KV_TILE, all = per_seq * v.n_seqs, rows = v.n_tokens / KV_TILE + 2 * v.n_seqs;
+    return v.n_seqs > 1 && all > rows ? KvGrid{rows, 0} : KvGrid{all, (int)per_seq};
+}
 
 hipError_t launch_kv_append(int format, int head_dim, const KvView &v, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new, int n_heads, double base, int pair_mode,
                             uint16_t *q_out, hipStream_t s)
 {
-    const int64_t tiles = kv_tiles_touched(v), grid = tiles * v.n_seqs;
+    const KvGrid grid = kv_grid(v);
     KvTurns turns;
     turns.log2_base = log2(base);
     turns.pair_mode = pair_mode;
     for (int e = 0; e < 8; ++e) turns.ratio[e] = exp2(-(2.0 * e / head_dim) * turns.log2_base);
     // query heads of a workgroup: as many as leave a thousand workgroups, up to eight
-    const int64_t per = grid * n_heads / 1024;
+    const int64_t per = grid.all * n_heads / 1024;
     const int heads_per_group = per < 1 ? 1 : per > 8 ? 8 : (int)per;
     return for_kv_tile(format, head_dim, [&](auto tag) {
         typedef decltype(tag) T;
@@ -436,8 +470,11 @@ hipError_t launch_kv_append(int format, int head_dim, const KvView &v, const uin
             hipLaunchKernelGGL((kv_append_token_kernel<T>), dim3((unsigned)v.n_seqs, (unsigned)((2 * v.n_kv_heads + n_heads + 31) / 32)), dim3(256), 0, s, v, q, k_new, v_new, n_heads, turns,
                                q_out);
         } else {
-            hipLaunchKernelGGL((kv_append_tile_kernel<T>), dim3((unsigned)grid, (unsigned)(v.n_kv_heads + (n_heads + heads_per_group - 1) / heads_per_group)), dim3(256), 0, s, v, q, k_new,
-                               v_new, n_heads, turns, q_out, (int)tiles, heads_per_group);
+            const dim3 blocks((unsigned)grid.all, (unsigned)(v.n_kv_heads + (n_heads + heads_per_group - 1) / heads_per_group));
+#define IFLOW_KV_GO(FIND) hipLaunchKernelGGL((kv_append_tile_kernel<T, FIND>), blocks, dim3(256), 0, s, v, q, k_new, v_new, n_heads, turns, q_out, grid.per_seq, heads_per_group)
+            if (grid.per_seq) IFLOW_KV_GO(false);
+            else IFLOW_KV_GO(true);
+#undef IFLOW_KV_GO
         }
         return hipGetLastError();
     });
@@ -445,10 +482,12 @@ hipError_t launch_kv_append(int format, int head_dim, const KvView &v, const uin
 
 hipError_t launch_kv_read(int format, int head_dim, const KvView &v, uint16_t *k_out, uint16_t *v_out, hipStream_t s)
 {
-    const int64_t tiles = kv_tiles_touched(v), grid = tiles * v.n_seqs;
+    const KvGrid grid = kv_grid(v);
     return for_kv_tile(format, head_dim, [&](auto tag) {
         typedef decltype(tag) T;
-        hipLaunchKernelGGL((kv_read_kernel<T>), dim3((unsigned)grid, (unsigned)v.n_kv_heads), dim3(256), 0, s, v, k_out, v_out, (int)tiles);
+        const dim3 blocks((unsigned)grid.all, (unsigned)v.n_kv_heads);
+        if (grid.per_seq) hipLaunchKernelGGL((kv_read_kernel<T, false>), blocks, dim3(256), 0, s, v, k_out, v_out, grid.per_seq);
+        else hipLaunchKernelGGL((kv_read_kernel<T, true>), blocks, dim3(256), 0, s, v, k_out, v_out, 0);
         return hipGetLastError();
     });
 }

@@ -60,10 +60,11 @@ __device__ __forceinline__ float kva_max_of_rows(float x)
 // sequence 51; exactly equal shares of consecutive tiles that cross from line to line: a workgroup that crosses takes 5 us longer, and the rest wait for it, 45.)
 // (Tiles are counted in 32 bits: where all lines might have more, every line is a workgroup's.)
 struct KvLines { int tiles, lines; };                         // of each line; lines of the sequence
-__device__ __forceinline__ KvLines kv_lines_of(const KvView &v, const KvSequence &seq, int group)
+// (sequences of `few` rows and more are not served by sixteens)
+__device__ __forceinline__ KvLines kv_lines_of(const KvView &v, const KvSequence &seq, int group, int few)
 {
     KvLines x;
-    x.lines = v.n_kv_heads * ((seq.count * group + KVA_ROWS - 1) / KVA_ROWS);
+    x.lines = seq.count * group < few ? v.n_kv_heads * ((seq.count * group + KVA_ROWS - 1) / KVA_ROWS) : 0;
     x.tiles = max(1, (seq.sees(seq.count - 1) + KV_TILE - 1) / KV_TILE);       // (one that sees nothing has zeros to write)
     return x;
 }
@@ -79,17 +80,6 @@ struct KvPartial {
     static size_t bytes(int n_seqs, int d) { return head(n_seqs) * 4 + (size_t)SLOTS * KVA_ROWS * (2 + d) * 4; }
 };
 __device__ __forceinline__ int kv_parts(int tiles, int share) { return (int)((uint32_t)(tiles + share - 1) / (uint32_t)share); }
-// inclusive sum over the lanes up to this one
-__device__ __forceinline__ int wave_scan(int x)
-{
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);       // row_shr 1, 2, 4, 8: within rows of sixteen
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);       // row_bcast:15 into rows 1 and 3
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);       // row_bcast:31 into rows 2 and 3
-    return x;
-}
 // n / d of numbers whose product is below 2^32, by a multiplication
 struct KvDivide {
     uint32_t magic;
@@ -107,7 +97,7 @@ struct KvTileRegs {
 
 // DIRECT: a workgroup is a line.
 template <typename T, int WAVES, bool DIRECT>
-__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv_attn_kernel(KvView v, const uint16_t *__restrict__ q, int n_heads, int group, KvDivide by_group,
+__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv_attn_kernel(KvView v, const uint16_t *__restrict__ q, int n_heads, int group, int few, KvDivide by_group,
                                                                                            KvDivide by_heads, float scale_log2e, uint16_t *__restrict__ out, void *ws)
 {
     constexpr int D = T::D, NU = D / 32, NC = D / 16;
@@ -122,12 +112,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
     // which sequence, which line and part of it, and where the sequence's partial results begin
     int b = 0, at = 0, slots = 0, share = 0;
     if constexpr (DIRECT) {
-        b = blockIdx.y;
+        at = blockIdx.x;
+        if ((int)gridDim.y == v.n_seqs) b = blockIdx.y;
+        else if (!kv_find(v, at, b, [&](const KvSequence &seq) { return kv_lines_of(v, seq, group, few).lines; })) return;
     } else {
         auto lines_of = [&](int s) {
             if (s >= v.n_seqs) return KvLines{0, 0};
             const KvSequence seq(v, s);
-            return kv_lines_of(v, seq, group);
+            return kv_lines_of(v, seq, group, few);
         };
         auto last = [](int x) { return __builtin_amdgcn_readlane(x, 63); };
         KvLines mine = lines_of(lane);                        // (the first 64 sequences are all in most calls)
@@ -173,10 +165,10 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
         }
     }
     const KvSequence seq(v, b);
-    const KvLines x = kv_lines_of(v, seq, group);
-    if (DIRECT && (int)blockIdx.x >= x.lines) return;
+    const KvLines x = kv_lines_of(v, seq, group, few);
+    if (DIRECT && at >= x.lines) return;
     const int parts = DIRECT ? 1 : kv_parts(x.tiles, share);
-    const int line = DIRECT ? blockIdx.x : __builtin_amdgcn_readfirstlane((int)((uint32_t)at / (uint32_t)parts)), my_part = at - line * parts;
+    const int line = DIRECT ? at : __builtin_amdgcn_readfirstlane((int)((uint32_t)at / (uint32_t)parts)), my_part = at - line * parts;
     // (parts as long as one another, in whole tiles for each wavefront)
     const int per = DIRECT ? x.tiles : min(share, (kv_parts(x.tiles, parts) + WAVES - 1) / WAVES * WAVES), t0 = DIRECT ? 0 : my_part * per, n_tiles = min(per, x.tiles - t0);
     const int piece = by_heads(line), head = line - piece * v.n_kv_heads;
@@ -374,15 +366,18 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
 // Merge of a line's partial results: one workgroup per (sequence, token, query head), thread (d, u) for component d of results 8u .. 8u + 7, then 8 (u + groups) ..: a group's eight are requested
 // at once, and the groups' states meet in LDS and are added in order.
 constexpr int KVA_MERGE = 8;
-__global__ __launch_bounds__(1024) void kv_attn_merge_kernel(KvView v, int n_heads, int group, void *ws, uint16_t *__restrict__ out)
+__global__ __launch_bounds__(1024) void kv_attn_merge_kernel(KvView v, int n_heads, int group, int few, void *ws, uint16_t *__restrict__ out)
 {
     __shared__ float s_o[8][128], s_m[8], s_l[8];
-    const int h = blockIdx.x, i = blockIdx.y, b = blockIdx.z, D = blockDim.x, d = threadIdx.x, groups = blockDim.y, u = threadIdx.y;
+    const int h = blockIdx.x, D = blockDim.x, d = threadIdx.x, groups = blockDim.y, u = threadIdx.y;
+    int i = blockIdx.y, b = blockIdx.z;
+    if ((int)gridDim.z != v.n_seqs && !kv_find(v, i, b, [&](const KvSequence &seq) { return seq.count * group < few ? seq.count : 0; })) return;
     const KvPartial part(ws, v.n_seqs);
     const int before = part.before[b], share = part.before[v.n_seqs];
     const KvSequence seq(v, b);
     if (!seq.has_row(i)) return;
-    const KvLines x = kv_lines_of(v, seq, group);
+    const KvLines x = kv_lines_of(v, seq, group, few);
+    if (x.lines == 0) return;
     const int row = i * group + h % group, piece = row / KVA_ROWS, r = row % KVA_ROWS, line = piece * v.n_kv_heads + h / group;
     const int mine = kv_parts(x.tiles, share);
     if (mine == 1) return;                                    // (written by the first launch)
@@ -436,7 +431,7 @@ __global__ __launch_bounds__(1024) void kv_attn_merge_kernel(KvView v, int n_hea
 typedef float kv_float16 __attribute__((ext_vector_type(16)));
 
 template <typename T, int RG, int PG, int STAGES>
-__global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_rows_kernel(KvView v, const uint16_t *__restrict__ q, int n_heads, int group, KvDivide by_group, float scale_log2e,
+__global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_rows_kernel(KvView v, const uint16_t *__restrict__ q, int n_heads, int group, int few, KvDivide by_group, float scale_log2e,
                                                                                           uint16_t *__restrict__ out)
 {
     constexpr int D = T::D, NU = D / 16, NC = D / 32, STEP = 2 * KV_TILE;      // NU: steps of 16 components; NC: groups of 32
@@ -452,14 +447,19 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), rg = wave % RG, pg = wave / RG;
     const int li = lane & 31, hf = lane >> 5;
-    const int head = blockIdx.x, b = blockIdx.z;
+    int head = blockIdx.x, b = blockIdx.z, block = blockIdx.y;
+    if (few > 0) {                                            // the blocks of the sequences that have as many rows, one after another
+        block = blockIdx.x / (unsigned)v.n_kv_heads;
+        head = blockIdx.x - block * v.n_kv_heads;
+        if (!kv_find(v, block, b, [&](const KvSequence &seq) { return seq.count * group < few ? 0 : (seq.count * group + ROWS - 1) / ROWS; })) return;
+    }
     // where tile 64 n + lane is: the first 64 are asked for before the sequence's length is known
     uint64_t my_tile = 0;
     auto find_tiles = [&](int t0) { my_tile = (t0 + lane) * KV_TILE < v.max_seq ? reinterpret_cast<uint64_t>(kv_tile_at(v, b, head, t0 + lane, T::BYTES)) : 0; };
     find_tiles(0);
     const KvSequence seq(v, b);
     const int n_rows = seq.count * group;
-    const int r0 = ((int)gridDim.y - 1 - (int)blockIdx.y) * ROWS;      // (the last rows, which see most, first)
+    const int r0 = ((few > 0 ? (n_rows + ROWS - 1) / ROWS : (int)gridDim.y) - 1 - block) * ROWS;      // (the last rows, which see most, first)
     if (r0 >= n_rows) return;
     // (the same for the wavefront, as the compiler is told: what it takes for different in the lanes costs a loop around every load)
     auto same = [](int n) { return __builtin_amdgcn_readfirstlane(n); };
@@ -788,7 +788,16 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     }
 }
 
-// Whether a line is a workgroup's, without a second launch, and of how many wavefronts then (0: lines are cut).  Us (graph replay; one page table, lengths an eighth to the whole), cut / direct with four
+// How a call is served.  `rows`: of a workgroup that decodes for many (0: by sixteens).  Us, by sixteens / 64 rows / 128 rows, for so many blocks of 64 rows (graph replay):
+//   32/8 heads x 128, 4 bits, one sequence of 4000                   64: 39 / 51 / 92    128: 66 / 54 / 94    256: 100 / 61 / 96   512: 181 / 109 / 104  1024: 298 / 184 / 139
+//   ... eight of 250 to 2000 (blocks: if all had as many as most)    128: 24 / 30 / 51   256: 30 / 31 / 52    512: 49 / 46 / 55    1024: 82 / 62 / 60
+//   64/8 heads x 128, 8 bits, one of 1000                            64: 13 / 24 / 38    128: 19 / 25 / 41    256: 30 / 27 / 45    512: 48 / 48 / 51
+//   71/1 heads x 64, 4 bits, one of 2000                             71: 19 / 21 / 44    142: 26 / 22 / 44
+// Blocks of 64 rows take as long for one as for 256; those of 128 take two for each compute unit to hide one another's waits.
+// A batch with a few long sequences among many short ones (`packed`: a quarter of n_seqs * max_tokens rows or fewer) is numbered by what there is of it, and its sequences of fewer rows
+// than `few` go by sixteens beside the others.  (Us, numbered by max_tokens and all in blocks / so, 32/8 heads x 128, 4 bits: 2000 tokens of one sequence and one each of 63 others, all of 2000
+// positions, 168 / 90; of 255 others 452 / 156; 8000 tokens and 63 others of 8000 positions 1221 / 733.)
+// `direct`: a line is a workgroup's, without a second launch, of so many wavefronts (0: lines are cut).  Us (graph replay; one page table, lengths an eighth to the whole), cut / direct with four
 // wavefronts / with eight, for the longest sequence's positions:
 //                                        512               768               1024              2048
 //   32/8 heads x 128, 4 bits,  8 lines   8.0 / 6.5 / 6.0   8.3 / 8.5 / 7.6   8.4 / 10.2 / 9.1  8.7 / 16.9 / 14.4
@@ -798,69 +807,70 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
 //   71/1 heads x 64, 4 bits,   5         7.3 / 5.5 / 5.2   7.3 / 6.6 / 6.0   7.3 / 7.7 / 6.9   7.8 / 12.2 / 11
 //                            320         11.9 / 7.8 / 7.8  14.0 / 9.6 / 9.4  15.5 / 10.9 / 10.4 18.3 / 16.9 / 15.9
 // The boundaries lie where the longest line alone takes as long as the parts and their merge, and later where there is a line for every compute unit.
-constexpr int KVA_SPLIT_WAVES = 4;
-static int64_t kv_attn_lines(const KvView &v, int n_heads)    // of a sequence, at most
-{
-    return v.n_kv_heads * (((int64_t)v.max_tokens * (n_heads / v.n_kv_heads) + KVA_ROWS - 1) / KVA_ROWS);
-}
-// Rows of a workgroup that decodes for many (0: by sixteens, as above).  Us, by sixteens / 64 rows / 128 rows, for so many blocks of 64 rows (graph replay):
-//   32/8 heads x 128, 4 bits, one sequence of 4000                   64: 39 / 51 / 92    128: 66 / 54 / 94    256: 100 / 61 / 96   512: 181 / 109 / 104  1024: 298 / 184 / 139
-//   ... eight of 250 to 2000 (blocks: if all had as many as most)    128: 24 / 30 / 51   256: 30 / 31 / 52    512: 49 / 46 / 55    1024: 82 / 62 / 60
-//   64/8 heads x 128, 8 bits, one of 1000                            64: 13 / 24 / 38    128: 19 / 25 / 41    256: 30 / 27 / 45    512: 48 / 48 / 51
-//   71/1 heads x 64, 4 bits, one of 2000                             71: 19 / 21 / 44    142: 26 / 22 / 44
-// Blocks of 64 rows take as long for one as for 256; those of 128 take two for each compute unit to hide one another's waits.
-static int kv_attn_rows(const KvView &v, int n_heads)
-{
-    const int64_t rows = (int64_t)v.max_tokens * (n_heads / v.n_kv_heads), lines = v.n_seqs * v.n_kv_heads;
-    if (rows < 64 || lines * ((rows + 63) / 64) < (v.n_seqs == 1 ? 128 : 256)) return 0;
-    return lines * ((rows + 127) / 128) >= 512 ? 128 : 64;
-}
-static int kv_attn_direct(const KvView &v, int head_dim, int n_heads)
-{
-    const int64_t tiles = (v.max_seq + KV_TILE - 1) / KV_TILE, lines = v.n_seqs * kv_attn_lines(v, n_heads);
-    const int waves = head_dim == 64 || lines < 256 ? 8 : 4;
-    if (lines * tiles > (1LL << 30)) return waves;            // (more tiles than the cut counts in 32 bits)
-    return v.max_seq <= (lines >= 256 ? 2560 : head_dim == 64 ? 1024 : 768) ? waves : 0;
-}
+constexpr int KVA_SPLIT_WAVES = 4, KVA_FEW = 128;
+struct KvPlan {
+    int rows, few, direct;
+    bool packed, sixteens;
+    int64_t blocks, lines;                                    // at most: blocks of `rows` rows of a key/value head if packed; lines of sixteen rows
+    KvPlan(const KvView &v, int head_dim, int n_heads)
+    {
+        const int64_t group = n_heads / v.n_kv_heads, most = v.max_tokens * group, all = v.n_tokens * group, seqs = v.n_seqs, kv = v.n_kv_heads;
+        packed = seqs > 1 && 4 * v.n_tokens < seqs * v.max_tokens;
+        auto blocks_of = [&](int n) { return packed ? kv * (all / n) : seqs * kv * ((most + n - 1) / n); };
+        rows = most < 64 || blocks_of(64) < (seqs == 1 ? 128 : 256) ? 0 : blocks_of(128) >= 512 ? 128 : 64;
+        few = rows && packed ? KVA_FEW : 0;
+        sixteens = !rows || few;
+        blocks = rows ? all / rows + std::min(seqs, all / KVA_FEW) : 0;
+        lines = seqs * kv * (((few ? std::min<int64_t>(most, few - 1) : most) + KVA_ROWS - 1) / KVA_ROWS);
+        if (packed) lines = std::min(lines, kv * (all / KVA_ROWS + seqs));
+        const int64_t tiles = (v.max_seq + KV_TILE - 1) / KV_TILE;
+        direct = head_dim == 64 || lines < 256 ? 8 : 4;
+        // (beyond 2^30 there are more tiles than the cut counts in 32 bits)
+        if (lines * tiles <= (1LL << 30) && v.max_seq > (lines >= 256 ? 2560 : head_dim == 64 ? 1024 : 768)) direct = 0;
+    }
+};
 
 size_t kv_attn_workspace_bytes(const KvView &v, int head_dim, int n_heads)
 {
-    return kv_attn_rows(v, n_heads) || kv_attn_direct(v, head_dim, n_heads) ? 0 : KvPartial::bytes(v.n_seqs, head_dim);
+    const KvPlan plan(v, head_dim, n_heads);
+    return plan.sixteens && !plan.direct ? KvPartial::bytes(v.n_seqs, head_dim) : 0;
 }
 
 hipError_t launch_kv_attn(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace, hipStream_t s)
 {
     const int group = n_heads / v.n_kv_heads;
-    const int64_t lines = kv_attn_lines(v, n_heads);
     const float scale_log2e = scale * 1.4426950408889634f;
-    const int direct = kv_attn_direct(v, head_dim, n_heads);
+    const KvPlan plan(v, head_dim, n_heads);
     const KvDivide by_group(group), by_heads(v.n_kv_heads);
-    if (const int rows = kv_attn_rows(v, n_heads)) {
-        const int64_t blocks = ((int64_t)v.max_tokens * group + rows - 1) / rows;      // (at most 2^22 rows: 32768)
-        return for_kv_tile(format, head_dim, [&](auto tag) {
+    if (plan.rows) {
+        const int64_t blocks = ((int64_t)v.max_tokens * group + plan.rows - 1) / plan.rows;      // (at most 2^22 rows: 32768)
+        const dim3 grid = plan.packed ? dim3((unsigned)(plan.blocks * v.n_kv_heads)) : dim3((unsigned)v.n_kv_heads, (unsigned)blocks, (unsigned)v.n_seqs);
+        const hipError_t e = for_kv_tile(format, head_dim, [&](auto tag) {
             typedef decltype(tag) T;
-            const dim3 grid((unsigned)v.n_kv_heads, (unsigned)blocks, (unsigned)v.n_seqs);
-            if (rows == 64) hipLaunchKernelGGL((kv_attn_rows_kernel<T, 2, 4, 1>), grid, dim3(512), 0, s, v, q, n_heads, group, by_group, scale_log2e, out);
-            else hipLaunchKernelGGL((kv_attn_rows_kernel<T, 4, 1, 2>), grid, dim3(256), 0, s, v, q, n_heads, group, by_group, scale_log2e, out);
+            if (plan.rows == 64) hipLaunchKernelGGL((kv_attn_rows_kernel<T, 2, 4, 1>), grid, dim3(512), 0, s, v, q, n_heads, group, plan.few, by_group, scale_log2e, out);
+            else hipLaunchKernelGGL((kv_attn_rows_kernel<T, 4, 1, 2>), grid, dim3(256), 0, s, v, q, n_heads, group, plan.few, by_group, scale_log2e, out);
             return hipGetLastError();
         });
+        if (e != hipSuccess || !plan.sixteens) return e;
     }
+    const int few = plan.few ? plan.few : 0x7fffffff;
     hipError_t e = for_kv_tile(format, head_dim, [&](auto tag) {
         typedef decltype(tag) T;
-#define IFLOW_KVA_GO(W, DIRECT, GRID) hipLaunchKernelGGL((kv_attn_kernel<T, W, DIRECT>), GRID, dim3(64 * W), 0, s, v, q, n_heads, group, by_group, by_heads, scale_log2e, out, workspace)
-        if (direct == 8) IFLOW_KVA_GO(8, true, dim3((unsigned)lines, (unsigned)v.n_seqs));
-        else if (direct) IFLOW_KVA_GO(4, true, dim3((unsigned)lines, (unsigned)v.n_seqs));
-        else IFLOW_KVA_GO(KVA_SPLIT_WAVES, false, dim3((unsigned)(KVA_PER_CU<T> * KVA_CUS + v.n_seqs * lines + 1)));
+        const dim3 direct = plan.packed ? dim3((unsigned)plan.lines) : dim3((unsigned)(plan.lines / v.n_seqs), (unsigned)v.n_seqs);
+#define IFLOW_KVA_GO(W, DIRECT, GRID) hipLaunchKernelGGL((kv_attn_kernel<T, W, DIRECT>), GRID, dim3(64 * W), 0, s, v, q, n_heads, group, few, by_group, by_heads, scale_log2e, out, workspace)
+        if (plan.direct == 8) IFLOW_KVA_GO(8, true, direct);
+        else if (plan.direct) IFLOW_KVA_GO(4, true, direct);
+        else IFLOW_KVA_GO(KVA_SPLIT_WAVES, false, dim3((unsigned)(KVA_PER_CU<T> * KVA_CUS + plan.lines + 1)));
 #undef IFLOW_KVA_GO
         return hipGetLastError();
     });
-    if (e != hipSuccess || direct) return e;
+    if (e != hipSuccess || plan.direct) return e;
     // Groups of threads for the results that a long line is likely to have: sequences as long as max_seq, or of several, half of it in the mean.
     const int tiles = (v.max_seq + KV_TILE - 1) / KV_TILE;
-    const int64_t part = std::max<int64_t>(2 * KVA_SPLIT_WAVES, v.n_seqs * lines * tiles / (v.n_seqs > 1 ? 2 : 1) / (4 * KVA_CUS));
+    const int64_t part = std::max<int64_t>(2 * KVA_SPLIT_WAVES, plan.lines * tiles / (v.n_seqs > 1 ? 2 : 1) / (4 * KVA_CUS));
     const int groups = (int)((tiles / part + 2 + KVA_MERGE - 1) / KVA_MERGE);
-    hipLaunchKernelGGL(kv_attn_merge_kernel, dim3((unsigned)n_heads, (unsigned)v.max_tokens, (unsigned)v.n_seqs), dim3((unsigned)head_dim, (unsigned)(groups > 8 ? 8 : groups)), 0, s, v,
-                       n_heads, group, workspace, out);
+    const dim3 tokens = plan.packed ? dim3((unsigned)n_heads, (unsigned)std::min<int64_t>(v.n_tokens, (int64_t)v.n_seqs * v.max_tokens)) : dim3((unsigned)n_heads, (unsigned)v.max_tokens, (unsigned)v.n_seqs);
+    hipLaunchKernelGGL(kv_attn_merge_kernel, tokens, dim3((unsigned)head_dim, (unsigned)(groups > 8 ? 8 : groups)), 0, s, v, n_heads, group, few, workspace, out);
     return hipGetLastError();
 }
 

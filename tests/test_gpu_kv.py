@@ -412,3 +412,43 @@ def test_refusals_name_themselves(gpu):  # noqa: F811
         with pytest.raises(it.IflowError) as info:
             call()
         assert info.value.status == status
+
+
+@pytest.mark.parametrize("name,n_heads,n_kv,d,page,n_seqs,long,history", [
+    ("Q4_B64", 8, 2, 128, 64, 70, 40, 60),                     # sixteens only, a line to a workgroup, numbered by what there is
+    ("Q4_B32", 4, 2, 64, 32, 5, 60, 2600),                     # ... lines cut into parts, merged by token
+    ("Q8_B32", 64, 8, 64, 32, 6, 270, 40),                     # blocks of 64 rows, few rows by sixteens beside them
+    ("Q4_B64", 128, 16, 64, 96, 67, 520, 30),                  # blocks of 128
+    ("Q8_B64", 64, 4, 128, 64, 6, 270, 800),                   # of 64, and the rest in parts with a merge
+    ("Q4_B32", 71, 1, 64, 64, 66, 300, 70)])                   # one head's 71 queries: a token alone has more rows than a block
+def test_batches_of_long_and_short(gpu, name, n_heads, n_kv, d, page, n_seqs, long, history):  # noqa: F811
+    """One or two sequences with many tokens among many with one or none: appended, read back, attended to."""
+    say(f"[case] kv {name} {n_heads}/{n_kv} heads of {d}: {n_seqs} sequences, {long} tokens and single ones")
+    counts = [1] * n_seqs
+    counts[n_seqs // 2], counts[1], counts[-1] = long, 0, 2
+    lens = [history + 7 * (b % 3) if c < long else long + 5 for b, c in enumerate(counts)]
+    lens[0] = 1
+    s = Setup(gpu, name, n_kv, d, page, lens, counts, 4500 + n_heads + n_seqs, n_heads)
+    assert 4 * s.n_tokens < n_seqs * s.max_tokens
+    s.fill([n - c for n, c in zip(lens, counts)])
+    append_and_compare(s, 0)
+    s.check_attend(s.queries(), d ** -0.5)
+
+
+def test_more_rows_claimed_than_there_are(gpu):  # noqa: F811
+    """Sequences of many tokens that share their rows: every one's positions are written (as at the fork of a sequence)."""
+    say("[case] kv: shared rows")
+    torch, it = gpu
+    many = 12
+    s = Setup(gpu, "Q4_B64", 2, 64, 32, [200] * many, [200] * many, 4601, 4, first=[0] + [200] * many, n_tokens=200)
+    # every other sequence has rows 0 .. 199, those between have none: together six times the rows that there are
+    s.first = np.array([0, 200] * (many // 2) + [0], np.int32)
+    s.describe()
+    k, v = s.values(200)
+    q = s.queries()
+    out = torch.zeros((200, 4, 64), dtype=torch.float16, device="cuda")
+    it.kv_append(s.d_cache, s.d_batch, s.dev(q), s.dev(k), s.dev(v), 4, BASE, 1, out)
+    torch.cuda.synchronize()
+    want = np.zeros_like(q)
+    s.kv_cache.append(s.cache, *s.args(), q, k, v, BASE, 1, want)
+    assert np.array_equal(s.d_pages.cpu().numpy(), s.pages) and np.array_equal(out.cpu().numpy().view(np.uint16), want)
