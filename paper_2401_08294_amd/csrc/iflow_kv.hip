@@ -88,19 +88,36 @@ template <typename T> struct KvLane {
     }
     template <typename Turn> __device__ __forceinline__ void rotate(int pair_mode, Turn turn)
     {
-        auto pair = [&](int i, int j, int e) {
-            double sn, cs;
-            turn(e, &sn, &cs);
-            const double a = (double)x[i], b = (double)x[j];
-            x[i] = (float)kv_half_once(__builtin_fma(a, cs, -(b * sn)));
-            x[j] = (float)kv_half_once(__builtin_fma(a, sn, b * cs));
+        // Four pairs at a time are rounded by way of 32 bits, which differs from one rounding only where the 32 bits end on a tie of fp16, with twelve zeros: then they are rounded again, with care.
+        auto pairs = [&](int e0, auto first, auto second) {
+            double sn[4], cs[4];
+            float a[4], b[4];
+            uint32_t low = 0xFFFFFFFFu;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                turn(e0 + e, &sn[e], &cs[e]);
+                const double u = (double)x[first(e0 + e)], w = (double)x[second(e0 + e)];
+                a[e] = (float)__builtin_fma(u, cs[e], -(w * sn[e]));
+                b[e] = (float)__builtin_fma(u, sn[e], w * cs[e]);
+                low = min(low, min(__builtin_bit_cast(uint32_t, a[e]) & 0xFFFu, __builtin_bit_cast(uint32_t, b[e]) & 0xFFFu));
+            }
+            if (low == 0) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const double u = (double)x[first(e0 + e)], w = (double)x[second(e0 + e)];
+                    a[e] = (float)kv_half_once(__builtin_fma(u, cs[e], -(w * sn[e])));
+                    b[e] = (float)kv_half_once(__builtin_fma(u, sn[e], w * cs[e]));
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { x[first(e0 + e)] = (float)(half_t)a[e]; x[second(e0 + e)] = (float)(half_t)b[e]; }
         };
         if (pair_mode == IFLOW_ROPE_HALVES) {
 #pragma unroll
-            for (int e = 0; e < H; ++e) pair(e, H + e, e);
+            for (int e = 0; e < H; e += 4) pairs(e, [](int n) { return n; }, [](int n) { return H + n; });
         } else {
 #pragma unroll
-            for (int e = 0; e < H; ++e) pair(2 * e, 2 * e + 1, e);
+            for (int e = 0; e < H; e += 4) pairs(e, [](int n) { return 2 * n; }, [](int n) { return 2 * n + 1; });
         }
     }
     // The lane's levels, as iflow_quantize_'s kernel finds them (multiplied by the reciprocal, divided where that could decide differently), and the headers of its blocks, by half of the head.
@@ -134,10 +151,9 @@ template <typename T> struct KvLane {
             float edge = 0.f;
 #pragma unroll
             for (int e = 0; e < H; ++e) {
-                const float f = __builtin_amdgcn_fmed3f((x[half * H + e] - of) * rs, -1.0f, (float)T::L + 1.0f) + 0.5f;
-                const float r = floorf(f);
-                edge = fmaxf(edge, fabsf((f - r) - 0.5f));
-                level[half * H + e] = (uint32_t)__builtin_amdgcn_fmed3f(r, 0.0f, (float)T::L);
+                const float f = __builtin_fmaf(x[half * H + e] - of, rs, 0.5f);       // (not negative: the offset is the smallest)
+                edge = fmaxf(edge, fabsf(__builtin_amdgcn_fractf(f) - 0.5f));
+                level[half * H + e] = min((uint32_t)f, (uint32_t)T::L);
             }
             if (edge > 0.5f - 0.0001220703125f) {
 #pragma unroll
