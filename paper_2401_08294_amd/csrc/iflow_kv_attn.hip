@@ -366,12 +366,10 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
 // Merge of a line's partial results: one workgroup per (sequence, token, query head), thread (d, u) for component d of results 8u .. 8u + 7, then 8 (u + groups) ..: a group's eight are requested
 // at once, and the groups' states meet in LDS and are added in order.
 constexpr int KVA_MERGE = 8;
-__global__ __launch_bounds__(1024) void kv_attn_merge_kernel(KvView v, int n_heads, int group, int few, void *ws, uint16_t *__restrict__ out)
+__device__ __forceinline__ void kv_attn_merge(const KvView &v, int b, int i, int h, int n_heads, int group, int few, void *ws, uint16_t *__restrict__ out)
 {
     __shared__ float s_o[8][128], s_m[8], s_l[8];
-    const int h = blockIdx.x, D = blockDim.x, d = threadIdx.x, groups = blockDim.y, u = threadIdx.y;
-    int i = blockIdx.y, b = blockIdx.z;
-    if ((int)gridDim.z != v.n_seqs && !kv_find(v, i, b, [&](const KvSequence &seq) { return seq.count * group < few ? seq.count : 0; })) return;
+    const int D = blockDim.x, d = threadIdx.x, groups = blockDim.y, u = threadIdx.y;
     const KvPartial part(ws, v.n_seqs);
     const int before = part.before[b], share = part.before[v.n_seqs];
     const KvSequence seq(v, b);
@@ -417,6 +415,15 @@ __global__ __launch_bounds__(1024) void kv_attn_merge_kernel(KvView v, int n_hea
         }
     }
     out[((int64_t)(seq.row + i) * n_heads + h) * D + d] = as_u16((half_t)(L > 0.f ? O / L : 0.f));
+}
+// Token y of sequence z for head x; packed (one z): the x-th, the x + grid-th, .. token of the sequences that sixteens serve, for head y.
+__global__ __launch_bounds__(1024) void kv_attn_merge_kernel(KvView v, int n_heads, int group, int few, void *ws, uint16_t *__restrict__ out)
+{
+    if ((int)gridDim.z == v.n_seqs) return kv_attn_merge(v, blockIdx.z, blockIdx.y, blockIdx.x, n_heads, group, few, ws, out);
+    for (int x = blockIdx.x, b, i; i = x, kv_find(v, i, b, [&](const KvSequence &seq) { return seq.count * group < few ? seq.count : 0; }); x += gridDim.x) {
+        kv_attn_merge(v, b, i, blockIdx.y, n_heads, group, few, ws, out);
+        __syncthreads();
+    }
 }
 
 // ---- many rows: prompts -----------------------------------------------------------------------------------------------------
@@ -653,6 +660,9 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     if constexpr (STAGES == 1) {
         uint8_t *k_at = stage, *v_at = stage + KEYS;
         load_keys(first_of(0)); load_values(first_of(0));
+        // Half the groups are a phase behind: the two wavefronts of a SIMD are of either half, and one decodes while the other uses the matrix cores.  (512 tokens behind 3888, 32/8 heads x 128, 4 bits:
+        // 64.7 us in step, 61.4 so; neighbouring groups in turn 66.)
+        if (pg >= PG / 2) __syncthreads();
         for (int trip = 0; trip < trips; ++trip) {
             const int t0 = first_of(trip);
             if (trip > 0) __syncthreads();                    // (the last step's operands have been read)
@@ -670,6 +680,7 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
 #pragma unroll
             for (int n = 0; n < 4 * NC; ++n) add(value_operand(v_at, n), n);
         }
+        if (pg < PG / 2) __syncthreads();
     } else {
         // Step n's probabilities are made while step n + 1 is scored, and its values added while step n + 2's keys and n + 1's values are decoded: matrix and vector instructions of one
         // wavefront do not wait for one another.  Two places for keys and for values, one barrier a step.
@@ -869,7 +880,7 @@ hipError_t launch_kv_attn(int format, int head_dim, const KvView &v, const uint1
     const int tiles = (v.max_seq + KV_TILE - 1) / KV_TILE;
     const int64_t part = std::max<int64_t>(2 * KVA_SPLIT_WAVES, plan.lines * tiles / (v.n_seqs > 1 ? 2 : 1) / (4 * KVA_CUS));
     const int groups = (int)((tiles / part + 2 + KVA_MERGE - 1) / KVA_MERGE);
-    const dim3 tokens = plan.packed ? dim3((unsigned)n_heads, (unsigned)std::min<int64_t>(v.n_tokens, (int64_t)v.n_seqs * v.max_tokens)) : dim3((unsigned)n_heads, (unsigned)v.max_tokens, (unsigned)v.n_seqs);
+    const dim3 tokens = plan.packed ? dim3((unsigned)std::min<int64_t>(v.n_tokens, 2 * (int64_t)v.n_seqs), (unsigned)n_heads) : dim3((unsigned)n_heads, (unsigned)v.max_tokens, (unsigned)v.n_seqs);
     hipLaunchKernelGGL(kv_attn_merge_kernel, tokens, dim3((unsigned)head_dim, (unsigned)(groups > 8 ? 8 : groups)), 0, s, v, n_heads, group, few, workspace, out);
     return hipGetLastError();
 }

@@ -435,6 +435,19 @@ def test_batches_of_long_and_short(gpu, name, n_heads, n_kv, d, page, n_seqs, lo
     s.check_attend(s.queries(), d ** -0.5)
 
 
+def test_rows_of_no_token_and_long_limits(gpu):  # noqa: F811
+    """Limits far above what the batch holds: 70000 rows, 8000 tokens a sequence; lines in parts, more tokens of short sequences than the merge has workgroups."""
+    say("[case] kv attention: limits far above the batch")
+    counts = [1, 20, 1, 0] * 10
+    counts[7] = 300
+    lens = [3100 if b in (0, 9, 30) else 340 if c == 300 else 33 + b for b, c in enumerate(counts)]
+    s = Setup(gpu, "Q4_B64", 2, 64, 64, lens, counts, 4700, 4, max_seq=8000, max_tokens=8000, n_tokens=70000)
+    s.fill()
+    s.describe()
+    assert s.iflow.kv_attn_workspace_bytes(s.d_cache, s.d_batch, 4) > 0
+    s.check_attend(s.queries(), 0.125, rows=slice(0, sum(counts) + 50))
+
+
 def test_more_rows_claimed_than_there_are(gpu):  # noqa: F811
     """Sequences of many tokens that share their rows: every one's positions are written (as at the fork of a sequence)."""
     say("[case] kv: shared rows")
