@@ -805,9 +805,10 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
 //   64/8 heads x 128, 8 bits, one of 1000                            64: 13 / 24 / 38    128: 19 / 25 / 41    256: 30 / 27 / 45    512: 48 / 48 / 51
 //   71/1 heads x 64, 4 bits, one of 2000                             71: 19 / 21 / 44    142: 26 / 22 / 44
 // Blocks of 64 rows take as long for one as for 256; those of 128 take two for each compute unit to hide one another's waits.
-// A batch with a few long sequences among many short ones (`packed`: a quarter of n_seqs * max_tokens rows or fewer) is numbered by what there is of it, and its sequences of fewer rows
+// A batch with a few long sequences among many short ones (`packed`: fewer than half of n_seqs * max_tokens rows) is numbered by what there is of it, and its sequences of fewer rows
 // than `few` go by sixteens beside the others.  (Us, numbered by max_tokens and all in blocks / so, 32/8 heads x 128, 4 bits: 2000 tokens of one sequence and one each of 63 others, all of 2000
-// positions, 168 / 90; of 255 others 452 / 156; 8000 tokens and 63 others of 8000 positions 1221 / 733.)
+// positions, 168 / 90; of 255 others 452 / 156; 8000 tokens and 63 others of 8000 positions 1221 / 733; one of 2000 and two single ones 80 / 84, two and five 135 / 110, three and five 169 / 157.  Where most have many tokens it is two
+// launches for little or nothing, as for one of 2000 and one single one, 80 / 88; but three of 500 and three single ones of 4000 positions, on the boundary, 97 / 45.)
 // `direct`: a line is a workgroup's, without a second launch, of so many wavefronts (0: lines are cut).  Us (graph replay; one page table, lengths an eighth to the whole), cut / direct with four
 // wavefronts / with eight, for the longest sequence's positions:
 //                                        512               768               1024              2048
@@ -826,7 +827,7 @@ struct KvPlan {
     KvPlan(const KvView &v, int head_dim, int n_heads)
     {
         const int64_t group = n_heads / v.n_kv_heads, most = v.max_tokens * group, all = v.n_tokens * group, seqs = v.n_seqs, kv = v.n_kv_heads;
-        packed = seqs > 1 && 4 * v.n_tokens < seqs * v.max_tokens;
+        packed = seqs > 1 && 2 * v.n_tokens < seqs * v.max_tokens;
         auto blocks_of = [&](int n) { return packed ? kv * (all / n) : seqs * kv * ((most + n - 1) / n); };
         rows = most < 64 || blocks_of(64) < (seqs == 1 ? 128 : 256) ? 0 : blocks_of(128) >= 512 ? 128 : 64;
         few = rows && packed ? KVA_FEW : 0;
