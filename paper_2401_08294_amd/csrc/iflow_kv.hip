@@ -400,6 +400,8 @@ __global__ __launch_bounds__(256) void kv_append_tile_kernel(KvView v, const uin
 }
 
 // ---- read back ----------------------------------------------------------------------------------------------------------------
+// A workgroup takes a tile of a head; bound by memory where there are many (16001 positions of 8 heads, 84 MB: 15.4 us), else by length -> page -> codes.  (Us, values asked for behind the keys' results /
+// all at first: prompts of 5400 tokens 8.0 / 7.6.  Whether any row is the batch's was a loop over 32 positions before, 16001 positions 18.6.)
 template <typename T>
 __device__ __forceinline__ void kv_read_tile(const KvView &v, int b, int nth, int tid, uint16_t *__restrict__ k_out, uint16_t *__restrict__ v_out)
 {
@@ -410,34 +412,48 @@ __device__ __forceinline__ void kv_read_tile(const KvView &v, int b, int nth, in
     const KvSequence seq(v, b);
     const int t = seq.first_tile() + nth, first_token = (int)((uint32_t)t * KV_TILE - (uint32_t)seq.position);
     auto has = [&](int p) { return seq.has_row(first_token + p); };
-    bool any = false;
-    for (int i = 0; i < KV_TILE; ++i) any |= has(i);
-    if (!any) return;
+    if (__builtin_amdgcn_ballot_w64(has(tid & (KV_TILE - 1))) == 0) return;
     const uint8_t *tile = t >= 0 && t <= (v.max_seq - 1) / KV_TILE ? kv_tile_at(v, b, head, (int)t, T::BYTES) : nullptr;
     auto there = [&](int p) { return tile && t * KV_TILE + p < v.max_seq; };
     auto out_at = [&](int p, int c) { return (((int64_t)seq.row + first_token + p) * v.n_kv_heads + head) * D + c; };
-    const uint16_t *kh = reinterpret_cast<const uint16_t *>(tile + T::KH_AT), *vh = reinterpret_cast<const uint16_t *>(tile + T::VH_AT);
-    for (int n = tid; n < KV_TILE * D / 8; n += 256) {
-        const int p = n / (D / 8), c = n % (D / 8) * 8;
+    // Eight components of a position's key, and one component of eight positions' values, N times for each thread; all of it is asked for before any of it is used.
+    constexpr int N = KV_TILE * D / 8 / 256, W = 8 / T::PER_WORD;
+    static_assert(N * 256 == 4 * D, "as many runs of eight positions as of eight components");
+    uint32_t key[N][W], key_header[N], value[N][W];
+    kv_u32x4 scales[N], offsets[N];
+    if (tile) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int n = tid + 256 * i, p = n / (D / 8), c = n % (D / 8) * 8, vc = n % D, g = n / D;
+            const uint32_t *k_at = reinterpret_cast<const uint32_t *>(tile) + kv_key_word<T>(p, c), *v_at = reinterpret_cast<const uint32_t *>(tile + T::V_AT) + kv_value_word<T>(g, 0, vc);
+#pragma unroll
+            for (int x = 0; x < W; ++x) { key[i][x] = k_at[x]; value[i][x] = v_at[x]; }
+            key_header[i] = *reinterpret_cast<const uint32_t *>(tile + T::KH_AT + 2 * kv_key_header(p, c / T::BLOCK));
+            const kv_u32x4 *header = reinterpret_cast<const kv_u32x4 *>(tile + T::VH_AT + 2 * kv_value_header(4 * g, vc / T::BLOCK));
+            scales[i] = header[0]; offsets[i] = header[1];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int n = tid + 256 * i, p = n / (D / 8), c = n % (D / 8) * 8;
         if (!has(p)) continue;
         kv_u32x4 w = {0u, 0u, 0u, 0u};
         if (there(p)) {
-            const KvPairs level = kv_levels<T::BITS>(reinterpret_cast<const uint32_t *>(tile) + kv_key_word<T>(p, c), magic);
-            const int at = kv_key_header(p, c / T::BLOCK);
-            const half_t sc = as_h(kh[at]), of = as_h(kh[at + 1]);
+            const KvPairs level = kv_levels<T::BITS>(key[i], magic);
+            const half2_t pair = as_h2(key_header[i]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = as_u32(kv_value(level.p[e], (half2_t){sc, sc}, (half2_t){of, of}));
+            for (int e = 0; e < 4; ++e) w[e] = as_u32(kv_value(level.p[e], (half2_t){pair.x, pair.x}, (half2_t){pair.y, pair.y}));
         }
         kv_store(k_out + out_at(p, c), w);
     }
     if (tile) {
-        for (int n = tid; n < 4 * D; n += 256) {
-            const int c = n % D, g = n / D;
-            const KvPairs level = kv_levels<T::BITS>(reinterpret_cast<const uint32_t *>(tile + T::V_AT) + kv_value_word<T>(g, 0, c), magic);
-            const int at = kv_value_header(4 * g, c / T::BLOCK);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int n = tid + 256 * i, c = n % D, g = n / D;
+            const KvPairs level = kv_levels<T::BITS>(value[i], magic);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const half2_t x = kv_value(level.p[e], (half2_t){as_h(vh[at + 2 * e]), as_h(vh[at + 2 * e + 1])}, (half2_t){as_h(vh[at + 8 + 2 * e]), as_h(vh[at + 9 + 2 * e])});
+                const half2_t x = kv_value(level.p[e], as_h2(scales[i][e]), as_h2(offsets[i][e]));
                 s_value[kv_value_position(g, 2 * e)][c] = as_u16(x.x);
                 s_value[kv_value_position(g, 2 * e + 1)][c] = as_u16(x.y);
             }
