@@ -465,3 +465,46 @@ def test_more_rows_claimed_than_there_are(gpu):  # noqa: F811
     want = np.zeros_like(q)
     s.kv_cache.append(s.cache, *s.args(), q, k, v, BASE, 1, want)
     assert np.array_equal(s.d_pages.cpu().numpy(), s.pages) and np.array_equal(out.cpu().numpy().view(np.uint16), want)
+
+
+def test_long_and_short_change_places_between_replays(gpu):  # noqa: F811
+    """One captured append and attention, replayed for batches whose long sequence is another each time, and for one without a long one; the pool's and the outputs' every byte each time."""
+    say("[case] kv: a graph of long and short sequences")
+    torch, it = gpu
+    batches = [[270, 1, 1, 2, 1, 0], [1, 2, 0, 1, 270, 1], [1, 1, 1, 1, 1, 1], [3, 1, 130, 0, 100, 40]]
+    s = Setup(gpu, "Q8_B32", 8, 64, 64, [900] * 6, batches[0], 4800, 64, max_seq=900, max_tokens=270, n_tokens=275)
+    s.fill([150] * 6)
+    s.describe()
+    assert 2 * s.n_tokens < 6 * s.max_tokens
+    k, v = s.values(275)
+    q = s.queries()
+    qd, kd, vd = s.dev(q), s.dev(k), s.dev(v)
+    need = it.kv_attn_workspace_bytes(s.d_cache, s.d_batch, 64)
+    ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    rotated, out = [torch.empty((275, 64, 64), dtype=torch.float16, device="cuda") for _ in range(2)]
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream), torch.cuda.graph(graph, stream=stream):
+        it.kv_append(s.d_cache, s.d_batch, qd, kd, vd, 64, BASE, 1, rotated, stream=stream)
+        it.kv_attn(s.d_cache, s.d_batch, rotated, 64, 0.125, out, ws, need, stream=stream)
+    held = np.full(6, 150, np.int64)
+    for counts in batches:
+        held += counts
+        s.lens, s.first = held.astype(np.int32), np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        s.d_lens.copy_(s.dev(s.lens))
+        s.d_first.copy_(s.dev(s.first))
+        rotated.fill_(7.0)
+        out.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want_q = np.full(q.shape, np.float16(7.0).view(np.uint16))
+        s.kv_cache.append(s.cache, *s.args(), q, k, v, BASE, 1, want_q)
+        assert np.array_equal(rotated.cpu().numpy().view(np.uint16), want_q) and np.array_equal(s.d_pages.cpu().numpy(), s.pages), counts
+        want = np.full((275, 64, 64), 7.0)
+        s.kv_cache.attend(s.cache, *s.args(), want_q, 0.125, want)
+        got = out.cpu().numpy().astype(np.float64)
+        rms = np.sqrt(np.mean(want ** 2, axis=-1, keepdims=True))
+        e = np.abs(got - want) / np.maximum(np.abs(want), rms)
+        assert np.isfinite(got).all() and e.max() <= TOL, (counts, float(e.max()))
