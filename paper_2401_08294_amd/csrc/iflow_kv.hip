@@ -3,7 +3,7 @@
 
 namespace iflow {
 
-// Whole rows of results are not kept in the caches.  (Us, kept / not: 16001 positions of 8 heads read back 20.0 / 18.7, prompts of 5400 tokens appended 42.9 / 38.4.)
+// Whole rows of results are not kept in the caches.  (Us, kept / not, when both took longer than now: 16001 positions of 8 heads read back 20.0 / 18.7, prompts of 5400 tokens appended 42.9 / 38.4.)
 template <typename V> __device__ __forceinline__ void kv_store(uint16_t *to, V x) { __builtin_nontemporal_store(x, reinterpret_cast<V *>(to)); }
 
 // ---- append -------------------------------------------------------------------------------------------------------------------
