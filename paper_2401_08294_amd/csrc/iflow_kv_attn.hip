@@ -683,7 +683,8 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
         if (pg < PG / 2) __syncthreads();
     } else {
         // Step n's probabilities are made while step n + 1 is scored, and its values added while step n + 2's keys and n + 1's values are decoded: matrix and vector instructions of one
-        // wavefront do not wait for one another.  Two places for keys and for values, one barrier a step.
+        // wavefront do not wait for one another.  Two places for keys and for values, one barrier a step: what a step overwrites was read before the barrier at the end of the step before.
+        // (The first step overwrites the keys that were scored in front of it: a barrier of its own.)
         auto k_at = [&](int trip) { return stage + (trip & 1) * KEYS; };
         auto v_at = [&](int trip) { return stage + (2 + (trip & 1)) * KEYS; };
         load_keys(first_of(0));
@@ -701,6 +702,7 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
         load_values(first_of(1));
         __syncthreads();
         score(k_at(0), sacc);
+        __syncthreads();
         settle(first_of(0), there(first_of(0)), there(first_of(0) + 1));
         for (int trip = 0; trip < trips; ++trip) {
             kv_float16 next[2];

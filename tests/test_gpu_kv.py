@@ -508,3 +508,25 @@ def test_long_and_short_change_places_between_replays(gpu):  # noqa: F811
         rms = np.sqrt(np.mean(want ** 2, axis=-1, keepdims=True))
         e = np.abs(got - want) / np.maximum(np.abs(want), rms)
         assert np.isfinite(got).all() and e.max() <= TOL, (counts, float(e.max()))
+
+
+@pytest.mark.parametrize("name,d,n", [("Q4_B64", 128, 60), ("Q8_B64", 128, 64), ("Q4_B32", 64, 64), ("Q8_B32", 64, 65), ("Q4_B64", 128, 100), ("Q4_B32", 128, 128)])
+def test_first_positions_of_blocks_that_share_keys(gpu, name, d, n):  # noqa: F811
+    """Blocks of 128 rows score the first 64 positions in front of their loop, whose first step already decodes later keys (or none) to the same place: prompts whose first positions have nearly all the
+    weight, one step long and two, the same bits call after call."""
+    n_heads = 64 if n >= 64 else 128                           # (64 rows and more to a key/value head)
+    say(f"[case] kv attention of prompts, weight on the first positions: {name} {n_heads}/64 heads of {d}, eight sequences of {n}")
+    s = Setup(gpu, name, 64, d, 64, [n] * 8, [n] * 8, 4900 + n, n_heads, spare_pages=0)
+    s.table[1:] = s.table[0]                                   # (pages that are only read may be shared)
+    k, v = s.values(n)
+    k, q = k.view(np.float16), s.queries().view(np.float16)
+    k[:, :, 0] = (10.0 - 0.5 * np.arange(n))[:, None]
+    q[..., 0] = 2.0 * d ** 0.5 * np.log(2.0)                   # (a position has half the weight of the one before, but for what the other components make of it)
+    for p in range(n):
+        s.cache.store(s.table[0], p, k[p].view(np.uint16), v[p])
+    s.describe()
+    q = q.view(np.uint16)
+    s.check_attend(q, d ** -0.5)
+    first = s.attend(q, d ** -0.5)
+    for _ in range(20):
+        assert np.array_equal(s.attend(q, d ** -0.5), first)
