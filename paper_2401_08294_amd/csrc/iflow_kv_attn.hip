@@ -433,8 +433,9 @@ __global__ __launch_bounds__(1024) void kv_attn_merge_kernel(KvView v, int n_hea
 //   O[component][row] = V^T P^T: element e of a tile's scores is position 4g + e % 4 or 16 + 4g + e % 4 of g = 2 (e / 8) + h where row i of S is position i with bits 3 and 4 changed
 //   over, so a lane's probabilities are its own operand, and a value's eight positions are a word of the cache's.  The sums' factors are the lane's own too.
 // Keys in LDS: [tile][component / 8][i: 32][8 components], values: [tile][g][component][8 positions]: 16-byte pieces that 32 lanes read side by side.
-// PG groups of wavefronts take every PG-th 64 positions and add up in LDS: where there are too few rows to fill the device.  The probabilities are rounded to fp16 once (and summed as rounded):
-// as large an error as the output's own rounding, where a second product for the rest would be half as much work again for the matrix cores.
+// PG groups of wavefronts take every PG-th 64 positions and add up in LDS: where there are too few rows to fill the device.  The probabilities are two fp16 numbers each, and two products of every value,
+// as in kv_attn_kernel: a token's output does not depend on how many rows its batch has but for the order of fp32 sums.  (Rounded to fp16 once, with one product, they made the largest error 1.4e-3 of a
+// row's rms where the output's own rounding is 4.9e-4, and prompts of 2500 tokens, 64/8 heads, took 284 us for the 352 now; 512 tokens behind 3888, 32/8 heads, 60 for 71.)
 typedef float kv_float16 __attribute__((ext_vector_type(16)));
 
 template <typename T, int RG, int PG, int STAGES>
@@ -602,11 +603,15 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     // what a row does not see goes, and the reference and the sums follow where a score is far above
     auto settle = [&](int t0, bool there0, bool there1) {
         if (!there0 || !there1 || t0 * KV_TILE + STEP > shortest) {
+            int seen = limit - t0 * KV_TILE - 4 * hf;         // of the step's positions, less the lane's own first
+            asm volatile("" : "+v"(seen));                    // (else the compiler keeps the limit less each of 32 constants in registers through the steps)
 #pragma unroll
-            for (int tl = 0; tl < 2; ++tl)
+            for (int tl = 0; tl < 2; ++tl) {
+                const int seen_of_tile = (tl ? there1 : there0) ? seen : 0;
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if (!(tl ? there1 : there0) || (t0 + tl) * KV_TILE + 16 * ((e >> 2) & 1) + 8 * (e >> 3) + 4 * hf + (e & 3) >= limit) sacc[tl][e] = -INFINITY;
+                    if (32 * tl + 16 * ((e >> 2) & 1) + 8 * (e >> 3) + (e & 3) >= seen_of_tile) sacc[tl][e] = -INFINITY;
+            }
         }
         float bm = kv_max3(sacc[0][0], sacc[0][1], sacc[1][0]);
         bm = kv_max3(bm, sacc[1][1], sacc[0][2]);
@@ -627,21 +632,22 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
                 for (int e = 0; e < 16; ++e) oacc[c][e] *= alpha;
         }
     };
-    const half2_t ones = {(half_t)1.f, (half_t)1.f};
-    KvPairs pb[2][2];
+    // The probabilities of eight positions as operand n of four: two fp16 numbers each, the first cut off, together within 2^-21 of them (as in kv_attn_kernel).
+    KvPairs pb[2], pr[2];                                     // of operands n % 2
     float below = 0.f;                                        // what is added to a score (a row that has seen nothing: no -inf - -inf)
-    auto weigh_pair = [&](int n) {                            // scores 2 n, 2 n + 1 of 32 to probabilities, in place of operands
+    auto weigh_pair = [&](int n) {                            // scores 2 n, 2 n + 1 of 32 to probabilities, in place of operand n / 4
         const int tl = n / 8, z = n / 4 % 2, e = n % 4;
         const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tl][8 * z + 2 * e], scale_log2e, below));
         const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tl][8 * z + 2 * e + 1], scale_log2e, below));
-        pb[tl][z].p[e] = (half2_t){(half_t)p0, (half_t)p1};
-        l = __builtin_amdgcn_fdot2(pb[tl][z].p[e], ones, l, false);
+        l += p0; l += p1;
+        asm volatile("" : "+v"(l));                           // (added here, not all of a step's at its end, kept in registers until then)
+        const half2_t first = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(p0, p1));
+        pb[z].p[e] = first;
+        pr[z].p[e] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(kv_less_low(p0, first), kv_less_high(p1, first)));
     };
-    // product n of 4 NC: positions of operand n / NC, components 32 (n % NC) ..
+    // products n of 4 NC: operand n / NC, components 32 (n % NC) ..
     auto value_operand = [&](const uint8_t *from, int n) { return *reinterpret_cast<const kv_half8 *>(from + ((n / (2 * NC) * 4 + 2 * (n / NC % 2) + hf) * D + 32 * (n % NC) + li) * 16); };
-    auto add = [&](kv_half8 a, int n) {
-        oacc[n % NC] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, __builtin_bit_cast(kv_half8, pb[n / (2 * NC)][n / NC % 2]), oacc[n % NC], 0, 0, 0);
-    };
+    auto add = [&](kv_half8 a, const KvPairs *p, int n) { oacc[n % NC] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, __builtin_bit_cast(kv_half8, p[n / NC % 2]), oacc[n % NC], 0, 0, 0); };
     // which tiles are there, of the 64 that lanes know and of the 64 before
     uint64_t known = 0, before = 0;
     int window = 0;
@@ -676,9 +682,15 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
             settle(t0, there(t0), there(t0 + 1));
             below = (m == -INFINITY) ? 0.f : -m;
 #pragma unroll
-            for (int n = 0; n < 16; ++n) weigh_pair(n);
+            for (int o = 0; o < 4; ++o) {
 #pragma unroll
-            for (int n = 0; n < 4 * NC; ++n) add(value_operand(v_at, n), n);
+                for (int n = 4 * o; n < 4 * o + 4; ++n) weigh_pair(n);
+#pragma unroll
+                for (int n = o * NC; n < (o + 1) * NC; ++n) {
+                    const kv_half8 a = value_operand(v_at, n);
+                    add(a, pb, n); add(a, pr, n);
+                }
+            }
         }
         if (pg < PG / 2) __syncthreads();
     } else {
@@ -709,24 +721,30 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
             clear(next);
             below = (m == -INFINITY) ? 0.f : -m;
             cut_values(first_of(trip + 1));
-            // (Operands are read AHEAD products before theirs; the barriers hold the order, which the scheduler takes apart into matrix and vector instructions.)
-            constexpr int AHEAD = 4;
-            kv_half8 a[AHEAD];
+            // Of 2 NU = 4 NC scores' products NC are ahead of the values' by which the first operand is made; then a value's two products, a score's and the making of a part of the next operand go
+            // together.  (Values and keys are read two products ahead; the barriers hold the order, which the scheduler takes apart into matrix and vector instructions.)
+            static_assert(NU == 2 * NC, "as many products for the scores of a step as operands of values");
+            kv_half8 ka[2], va[2];
 #pragma unroll
-            for (int n = 0; n < AHEAD; ++n) a[n] = key_operand(k_at(trip + 1), n);
+            for (int n = 0; n < 2; ++n) { ka[n] = key_operand(k_at(trip + 1), n); va[n] = value_operand(v_at(trip), n); }
+            auto score_and_weigh = [&](int n) {
+                next[n % 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ka[n % 2], qb[n / 2], next[n % 2], 0, 0, 0);
+                if (n + 2 < 2 * NU) ka[n % 2] = key_operand(k_at(trip + 1), n + 2);
 #pragma unroll
-            for (int n = 0; n < 2 * NU; ++n) {
+                for (int y = 0; y < 4 / NC; ++y) weigh_pair(n * (4 / NC) + y);
+            };
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
                 __builtin_amdgcn_sched_barrier(0);
-                next[n % 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[n % AHEAD], qb[n / 2], next[n % 2], 0, 0, 0);
-                a[n % AHEAD] = n + AHEAD < 2 * NU ? key_operand(k_at(trip + 1), n + AHEAD) : value_operand(v_at(trip), n + AHEAD - 2 * NU);
-#pragma unroll
-                for (int y = 0; y < 8 / NU; ++y) { weigh_pair(n * (8 / NU) + y); }
+                score_and_weigh(n);
             }
 #pragma unroll
             for (int n = 0; n < 4 * NC; ++n) {
                 __builtin_amdgcn_sched_barrier(0);
-                add(a[n % AHEAD], n);
-                if (n + AHEAD < 4 * NC) a[n % AHEAD] = value_operand(v_at(trip), n + AHEAD);
+                add(va[n % 2], pb, n);
+                add(va[n % 2], pr, n);
+                if (n + 2 < 4 * NC) va[n % 2] = value_operand(v_at(trip), n + 2);
+                if (n + NC < 4 * NC) score_and_weigh(n + NC);
                 if (n % 2 == 0) {
                     constexpr int EACH = 2 * CHUNKS / (2 * NC) > 0 ? 2 * CHUNKS / (2 * NC) : 1;
 #pragma unroll

@@ -530,3 +530,20 @@ def test_first_positions_of_blocks_that_share_keys(gpu, name, d, n):  # noqa: F8
     first = s.attend(q, d ** -0.5)
     for _ in range(20):
         assert np.array_equal(s.attend(q, d ** -0.5), first)
+
+
+@pytest.mark.parametrize("name,n_heads,n_kv,d,lens,counts", [
+    ("Q4_B64", 32, 8, 128, [1, 33, 300, 700], None), ("Q8_B32", 17, 1, 64, [5, 64, 513], None),              # by sixteens, a line to a workgroup
+    ("Q4_B32", 16, 2, 128, [3000, 1, 900], None), ("Q8_B64", 8, 8, 64, [1500, 40], None),                    # ... lines in parts
+    ("Q4_B64", 64, 64, 128, [300], [130]), ("Q4_B32", 64, 64, 64, [400], [129]), ("Q8_B64", 64, 64, 128, [330, 65], [65, 65]), ("Q8_B32", 64, 64, 64, [90], [90]),             # blocks of 64 rows
+    ("Q4_B64", 64, 64, 128, [150, 333, 200, 260], [150, 150, 140, 129]), ("Q4_B32", 64, 64, 64, [129, 170, 300, 64], [129, 72, 130, 64]),                                       # blocks of 128
+    ("Q8_B64", 64, 64, 64, [200, 150, 131, 129], [129, 130, 131, 129]), ("Q8_B32", 64, 64, 128, [140, 131, 180, 129], [140, 129, 130, 1])])
+def test_attention_is_rounded_once(gpu, name, n_heads, n_kv, d, lens, counts):  # noqa: F811
+    """Whatever number of rows a batch has, the output is the 64-bit one rounded to fp16, 2^-11 of the value, and what 32 bits leave.  That is, relative to the output's rms: a score is a sum of 64 or 128
+    products in fp32, 2^-23 of their absolute sum (12 in units of log2 for these inputs) is 1.4e-6; its distance from the reference rounds by 1e-6 and the exponential by 1e-7; two fp16 numbers
+    hold a probability to 2^-21 = 5e-7.  3e-6 of each of many terms, of either sign, is 3e-6 of their sum's rms, and five of these are 1.5e-5: half of the 2^-15 allowed here."""
+    say(f"[case] kv attention rounded once {name} {n_heads}/{n_kv} heads of {d}, lengths {lens}, tokens {counts}")
+    s = Setup(gpu, name, n_kv, d, 64, lens, counts, 5000 + n_heads + d, n_heads)
+    s.fill()
+    s.describe()
+    s.check_attend(s.queries(), d ** -0.5, tol=2.0 ** -11 + 2.0 ** -15)
