@@ -58,7 +58,9 @@ __device__ __forceinline__ float kva_max_of_rows(float x)
 // leaves partial results, which a second launch adds up.
 // (Tried: ranges of a fixed number of positions: a die gets the same range of every sequence, 66 us for 32 sequences of 1000 to 8001 positions, 32/8 heads, turned by head and
 // sequence 51; exactly equal shares of consecutive tiles that cross from line to line: a workgroup that crosses takes 5 us longer, and the rest wait for it, 45.)
-// (Tiles are counted in 32 bits: where all lines might have more, every line is a workgroup's.)
+// (Tiles are counted in 32 bits: where all lines might have more, every line is a workgroup's.  The device trusts no count that the host has not bounded: where the arrays make more lines than
+// `max_lines`, which only sequences that claim the same rows do, a line is one part, whatever it is long, and nothing but lines is counted: those are below 2^30 whatever the arrays hold.)
+constexpr int KVA_WHOLE = 1 << 20;                            // a part of more tiles than a line has
 struct KvLines { int tiles, lines; };                         // of each line; lines of the sequence
 // (sequences of `few` rows and more are not served by sixteens)
 __device__ __forceinline__ KvLines kv_lines_of(const KvView &v, const KvSequence &seq, int group, int few)
@@ -77,6 +79,8 @@ struct KvPartial {
     static __host__ __device__ __forceinline__ size_t head(int n_seqs) { return ((size_t)n_seqs + 4) / 4 * 4; }
     __device__ __forceinline__ KvPartial(void *ws, int n_seqs)
         : before(static_cast<int32_t *>(ws)), m(reinterpret_cast<float *>(before + head(n_seqs))), l(m + SLOTS * KVA_ROWS), o(l + SLOTS * KVA_ROWS) {}
+    // (number n is one of them; also where another stream changes the lengths meanwhile)
+    static __device__ __forceinline__ int slot(int n) { return (int)min((uint32_t)n, (uint32_t)(SLOTS - 1)); }
     static size_t bytes(int n_seqs, int d) { return head(n_seqs) * 4 + (size_t)SLOTS * KVA_ROWS * (2 + d) * 4; }
 };
 __device__ __forceinline__ int kv_parts(int tiles, int share) { return (int)((uint32_t)(tiles + share - 1) / (uint32_t)share); }
@@ -97,8 +101,8 @@ struct KvTileRegs {
 
 // DIRECT: a workgroup is a line.
 template <typename T, int WAVES, bool DIRECT>
-__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv_attn_kernel(KvView v, const uint16_t *__restrict__ q, int n_heads, int group, int few, KvDivide by_group,
-                                                                                           KvDivide by_heads, float scale_log2e, uint16_t *__restrict__ out, void *ws)
+__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv_attn_kernel(KvView v, const uint16_t *__restrict__ q, int n_heads, int group, int few, int max_lines,
+                                                                                           KvDivide by_group, KvDivide by_heads, float scale_log2e, uint16_t *__restrict__ out, void *ws)
 {
     constexpr int D = T::D, NU = D / 32, NC = D / 16;
     constexpr int PAD = 4;                                    // floats: rows four apart in banks of their own
@@ -123,15 +127,21 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
         };
         auto last = [](int x) { return __builtin_amdgcn_readlane(x, 63); };
         KvLines mine = lines_of(lane);                        // (the first 64 sequences are all in most calls)
-        int total = last(wave_scan(mine.tiles * mine.lines)), lines = last(wave_scan(mine.lines));
+        // (unsigned: where lines turn out to be too many, this has wrapped and is not used)
+        auto tiles_of = [&](const KvLines &x) { return (uint32_t)last(wave_scan((int)((uint32_t)x.tiles * (uint32_t)x.lines))); };
+        uint32_t sum = tiles_of(mine);
+        int lines = last(wave_scan(mine.lines));
         for (int s = 64; s < v.n_seqs; s += 64) {
             const KvLines x = lines_of(s + lane);
-            total += last(wave_scan(x.tiles * x.lines)); lines += last(wave_scan(x.lines));
+            sum += tiles_of(x); lines += last(wave_scan(x.lines));
         }
+        const int total = (int)sum;
         // The parts' tiles: one for each wavefront where all are few, else at least two (a part costs about as much as four tiles besides).  The fewest that leave no more parts than the device
         // holds at once, for what does not fit waits for a whole part; where there are half as many lines already, 1 / capacity of all tiles: parts are then about as many again as lines.
         constexpr int UNIT = WAVES, CAPACITY = KVA_PER_CU<T> * KVA_CUS;
-        if (lines > CAPACITY / 2) {
+        if (lines > max_lines) {
+            share = KVA_WHOLE;
+        } else if (lines > CAPACITY / 2) {
             share = max(2 * UNIT, (total / CAPACITY + UNIT) / UNIT * UNIT);
         } else if (v.n_seqs > 64) {
             share = max(2 * UNIT, (total / (CAPACITY - lines) + UNIT) / UNIT * UNIT);      // (a line has less than one part more than its tiles over a part's)
@@ -328,7 +338,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
 #pragma unroll
             for (int e = 0; e < 4; ++e) my_o[e * (D + PAD) + 16 * c] = oacc[c][e];
         __syncthreads();
-        const int slot = min(slots + at, KvPartial::SLOTS - 1);      // (below that; also where another stream changes the lengths meanwhile)
+        const int slot = KvPartial::slot(slots + at);
         constexpr int QUADS = D / 4;                          // a thread takes four components of a row
 #pragma unroll
         for (int i = 0; i < (KVA_ROWS * QUADS + 64 * WAVES - 1) / (64 * WAVES); ++i) {
@@ -379,7 +389,7 @@ __device__ __forceinline__ void kv_attn_merge(const KvView &v, int b, int i, int
     const int row = i * group + h % group, piece = row / KVA_ROWS, r = row % KVA_ROWS, line = piece * v.n_kv_heads + h / group;
     const int mine = kv_parts(x.tiles, share);
     if (mine == 1) return;                                    // (written by the first launch)
-    auto slot = [&](int s) { return min(before + line * mine + s, KvPartial::SLOTS - 1) * KVA_ROWS + r; };
+    auto slot = [&](int s) { return KvPartial::slot(before + line * mine + s) * KVA_ROWS + r; };
     float M = -INFINITY, L = 0.f, O = 0.f;                    // relative to to_base(M)
     auto to_base = [](float m) { return m == -INFINITY ? 0.f : m - KVA_SPARE; };
     for (int s0 = u * KVA_MERGE; s0 < mine; s0 += groups * KVA_MERGE) {
@@ -889,7 +899,7 @@ hipError_t launch_kv_attn(int format, int head_dim, const KvView &v, const uint1
     hipError_t e = for_kv_tile(format, head_dim, [&](auto tag) {
         typedef decltype(tag) T;
         const dim3 direct = plan.packed ? dim3((unsigned)plan.lines) : dim3((unsigned)(plan.lines / v.n_seqs), (unsigned)v.n_seqs);
-#define IFLOW_KVA_GO(W, DIRECT, GRID) hipLaunchKernelGGL((kv_attn_kernel<T, W, DIRECT>), GRID, dim3(64 * W), 0, s, v, q, n_heads, group, few, by_group, by_heads, scale_log2e, out, workspace)
+#define IFLOW_KVA_GO(W, DIRECT, GRID) hipLaunchKernelGGL((kv_attn_kernel<T, W, DIRECT>), GRID, dim3(64 * W), 0, s, v, q, n_heads, group, few, (int)plan.lines, by_group, by_heads, scale_log2e, out, workspace)
         if (plan.direct == 8) IFLOW_KVA_GO(8, true, direct);
         else if (plan.direct) IFLOW_KVA_GO(4, true, direct);
         else IFLOW_KVA_GO(KVA_SPLIT_WAVES, false, dim3((unsigned)(KVA_PER_CU<T> * KVA_CUS + plan.lines + 1)));

@@ -547,3 +547,89 @@ def test_attention_is_rounded_once(gpu, name, n_heads, n_kv, d, lens, counts):  
     s.fill()
     s.describe()
     s.check_attend(s.queries(), d ** -0.5, tol=2.0 ** -11 + 2.0 ** -15)
+
+
+def _guarded(torch, n, guard=1 << 22):
+    """n bytes with 4 MiB of a pattern on either side: (the bytes, a function that says whether the pattern is whole)."""
+    whole = torch.full((n + 2 * guard,), 0x5A, dtype=torch.uint8, device="cuda")
+    return whole[guard:guard + n], lambda: bool((whole[:guard] == 0x5A).all() and (whole[guard + n:] == 0x5A).all())
+
+
+def test_sequences_that_claim_the_same_rows_many_times(gpu):  # noqa: F811
+    """More lines than the batch's rows make, and so many tiles in all of them that 32 bits do not count them: nothing is written but the call's outputs and workspace, and rows that a call serves
+    after it are right."""
+    say("[case] kv attention: sequences that claim 500 rows 2^18 times")
+    torch, it = gpu
+    n_seqs, kv, heads, d, tokens, rows, most = 64, 2, 32, 64, 1 << 18, 500, 1 << 20
+    need_of = it.kv_cache(it.Q4_B64, kv, d, 1 << 15, 1, None)
+    pages = torch.zeros(it.kv_cache_bytes(need_of), dtype=torch.uint8, device="cuda")
+    cache = it.kv_cache(it.Q4_B64, kv, d, 1 << 15, 1, pages)
+    table = torch.full((n_seqs, 32), -1, dtype=torch.int32, device="cuda")
+    table[3:] = 0
+    first = torch.zeros(n_seqs + 1, dtype=torch.int32, device="cuda")
+    lens = torch.zeros(n_seqs, dtype=torch.int32, device="cuda")
+    batch = it.kv_batch(n_seqs, 32, table, lens, most, first, rows, tokens)
+    need = it.kv_attn_workspace_bytes(cache, batch, heads)
+    assert need > 0
+    ws, ws_whole = _guarded(torch, need)
+    out, out_whole = _guarded(torch, rows * heads * d * 2)
+    q = torch.randn((rows, heads, d), device="cuda").half()
+    # 2^18 tokens that begin long before the rows do and end with them, twice; 2^18 of which all but 500 lie behind; all rows by four sequences; by 32
+    for starts, lengths in (([-tokens + rows, rows, -tokens + rows, rows], [32767 * 32, 32, most]), ([0, tokens, 0, tokens], [32767 * 32, 32, most]),
+                            ([0, rows, 0, rows, 0, rows, 0, rows, 0], [most] * 8), ([0] + [rows, 0] * 31 + [rows], [5000 + i for i in range(63)])):
+        first.fill_(starts[-1])
+        first[:len(starts)] = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        lens.zero_()
+        lens[:len(lengths)] = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+        out.zero_()
+        torch.cuda.synchronize()
+        it.kv_attn(cache, batch, q, heads, 0.125, out, ws, need)
+        torch.cuda.synchronize()
+        assert ws_whole() and out_whole()
+        assert torch.isfinite(out.view(torch.float16)).all()
+    # the same description, workspace and outputs with arrays that hold a batch: values of zeros and scale, one row each of two sequences
+    first.fill_(2)
+    first[:2] = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    lens.zero_()
+    lens[:2] = torch.tensor([40000, 3], dtype=torch.int32, device="cuda")
+    table.zero_()
+    out.fill_(0x47)
+    it.kv_attn(cache, batch, q, heads, 0.125, out, ws, need)
+    torch.cuda.synchronize()
+    got = out.view(rows, heads * d * 2)
+    assert ws_whole() and out_whole() and (got[:2] == 0).all() and (got[2:] == 0x47).all()
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_arrays_of_any_numbers(gpu, seed):  # noqa: F811
+    """Lengths, first tokens and pages of any 32 bits, some of them plausible: the three calls write nothing but their outputs, the pool and the workspace."""
+    torch, it = gpu
+    rng = np.random.default_rng(synth.BASE_SEED + 5200 + seed)
+    fmt, d = it.FORMATS[FORMATS[seed % 4]], (64, 128)[seed // 4 % 2]
+    n_seqs, kv, group = int(rng.choice([1, 3, 64, 70])), int(rng.choice([1, 2, 8])), int(rng.choice([1, 4, 16]))
+    tokens, rows, most = int(rng.choice([1, 7, 300, 4000])), int(rng.choice([80, 900])), int(rng.choice([4000, 9000, 1 << 20]))
+    page, n_pages = 64, 50
+    max_pages = -(-most // page)
+    say(f"[case] kv: arrays of any numbers, seed {seed}: {n_seqs} sequences, {kv} x {group} heads of {d}, {tokens} tokens, {rows} rows, {most} positions")
+
+    def any_of(n, top):
+        plausible, wild = rng.integers(0, top + 1, n), rng.integers(-2 ** 31, 2 ** 31, n)
+        return np.where(rng.random(n) < 0.25, wild, np.where(rng.random(n) < 0.2, rng.choice([-1, 0, 2 ** 31 - 1, -2 ** 31, top + 1], n), plausible)).astype(np.int32)
+    size = it.kv_cache_bytes(it.kv_cache(fmt, kv, d, page, n_pages, None))
+    pool, pool_whole = _guarded(torch, size)
+    pool.zero_()
+    table, first, lens = [torch.from_numpy(a).cuda() for a in (any_of(n_seqs * max_pages, n_pages), any_of(n_seqs + 1, rows), any_of(n_seqs, most))]
+    cache, batch = it.kv_cache(fmt, kv, d, page, n_pages, pool), it.kv_batch(n_seqs, max_pages, table, lens, most, first, rows, tokens)
+    heads = kv * group
+    need = it.kv_attn_workspace_bytes(cache, batch, heads)
+    buffers = [_guarded(torch, n) for n in [max(need, 16)] + [rows * heads * d * 2] * 2 + [rows * kv * d * 2] * 2]
+    (ws, _), (rotated, _), (out, _), (k_out, _), (v_out, _) = buffers
+    q, k, v = [torch.randn((rows, h, d), device="cuda").half() for h in (heads, kv, kv)]
+    for b in (rotated, out, k_out, v_out):
+        b.zero_()
+    it.kv_append(cache, batch, q, k, v, heads, BASE, 1, rotated)
+    it.kv_read(cache, batch, k_out, v_out)
+    it.kv_attn(cache, batch, q, heads, d ** -0.5, out, ws, need)
+    torch.cuda.synchronize()
+    assert pool_whole() and all(whole() for _, whole in buffers)
+    assert all(torch.isfinite(b.view(torch.float16)).all() for b in (rotated, out, k_out, v_out))
