@@ -99,7 +99,7 @@ struct KvTileRegs {
     kv_u32x4 vh[T::NB][2];                                    // scales, offsets of its eight positions, by block
 };
 
-// DIRECT: a workgroup is a line.
+// DIRECT: a workgroup is a line: blockIdx.x of sequence blockIdx.y (max_lines 0), or, by its number in both, of all.
 template <typename T, int WAVES, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv_attn_kernel(KvView v, const uint16_t *__restrict__ q, int n_heads, int group, int few, int max_lines,
                                                                                            KvDivide by_group, KvDivide by_heads, float scale_log2e, uint16_t *__restrict__ out, void *ws)
@@ -116,8 +116,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
     // which sequence, which line and part of it, and where the sequence's partial results begin
     int b = 0, at = 0, slots = 0, share = 0;
     if constexpr (DIRECT) {
-        at = blockIdx.x;
-        if ((int)gridDim.y == v.n_seqs) b = blockIdx.y;
+        at = max_lines ? blockIdx.y * gridDim.x + blockIdx.x : blockIdx.x;
+        if (!max_lines) b = blockIdx.y;
         else if (!kv_find(v, at, b, [&](const KvSequence &seq) { return kv_lines_of(v, seq, group, few).lines; })) return;
     } else {
         auto lines_of = [&](int s) {
@@ -467,8 +467,9 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     const int li = lane & 31, hf = lane >> 5;
     int head = blockIdx.x, b = blockIdx.z, block = blockIdx.y;
     if (few > 0) {                                            // the blocks of the sequences that have as many rows, one after another
-        block = blockIdx.x / (unsigned)v.n_kv_heads;
-        head = blockIdx.x - block * v.n_kv_heads;
+        const unsigned number = blockIdx.y * gridDim.x + blockIdx.x;
+        block = number / (unsigned)v.n_kv_heads;
+        head = number - block * v.n_kv_heads;
         if (!kv_find(v, block, b, [&](const KvSequence &seq) { return seq.count * group < few ? 0 : (seq.count * group + ROWS - 1) / ROWS; })) return;
     }
     // where tile 64 n + lane is: the first 64 are asked for before the sequence's length is known
@@ -872,6 +873,13 @@ struct KvPlan {
     }
 };
 
+// The launch of n numbered workgroups: in x and y, because a launch has less than 2^32 threads in either (65535 sequences of 64 key/value heads and 1.1 million rows make 8.4 million lines, 512 threads each).
+static dim3 kv_numbered(int64_t n)
+{
+    const int64_t x = std::min<int64_t>(n, 1 << 22);
+    return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
+}
+
 size_t kv_attn_workspace_bytes(const KvView &v, int head_dim, int n_heads)
 {
     const KvPlan plan(v, head_dim, n_heads);
@@ -886,7 +894,7 @@ hipError_t launch_kv_attn(int format, int head_dim, const KvView &v, const uint1
     const KvDivide by_group(group), by_heads(v.n_kv_heads);
     if (plan.rows) {
         const int64_t blocks = ((int64_t)v.max_tokens * group + plan.rows - 1) / plan.rows;      // (at most 2^22 rows: 32768)
-        const dim3 grid = plan.packed ? dim3((unsigned)(plan.blocks * v.n_kv_heads)) : dim3((unsigned)v.n_kv_heads, (unsigned)blocks, (unsigned)v.n_seqs);
+        const dim3 grid = plan.packed ? kv_numbered(plan.blocks * v.n_kv_heads) : dim3((unsigned)v.n_kv_heads, (unsigned)blocks, (unsigned)v.n_seqs);
         const hipError_t e = for_kv_tile(format, head_dim, [&](auto tag) {
             typedef decltype(tag) T;
             if (plan.rows == 64) hipLaunchKernelGGL((kv_attn_rows_kernel<T, 2, 4, 1>), grid, dim3(512), 0, s, v, q, n_heads, group, plan.few, by_group, scale_log2e, out);
@@ -898,8 +906,9 @@ hipError_t launch_kv_attn(int format, int head_dim, const KvView &v, const uint1
     const int few = plan.few ? plan.few : 0x7fffffff;
     hipError_t e = for_kv_tile(format, head_dim, [&](auto tag) {
         typedef decltype(tag) T;
-        const dim3 direct = plan.packed ? dim3((unsigned)plan.lines) : dim3((unsigned)(plan.lines / v.n_seqs), (unsigned)v.n_seqs);
-#define IFLOW_KVA_GO(W, DIRECT, GRID) hipLaunchKernelGGL((kv_attn_kernel<T, W, DIRECT>), GRID, dim3(64 * W), 0, s, v, q, n_heads, group, few, (int)plan.lines, by_group, by_heads, scale_log2e, out, workspace)
+        const dim3 direct = plan.packed ? kv_numbered(plan.lines) : dim3((unsigned)(plan.lines / v.n_seqs), (unsigned)v.n_seqs);
+        const int max_lines = plan.packed || !plan.direct ? (int)plan.lines : 0;
+#define IFLOW_KVA_GO(W, DIRECT, GRID) hipLaunchKernelGGL((kv_attn_kernel<T, W, DIRECT>), GRID, dim3(64 * W), 0, s, v, q, n_heads, group, few, max_lines, by_group, by_heads, scale_log2e, out, workspace)
         if (plan.direct == 8) IFLOW_KVA_GO(8, true, direct);
         else if (plan.direct) IFLOW_KVA_GO(4, true, direct);
         else IFLOW_KVA_GO(KVA_SPLIT_WAVES, false, dim3((unsigned)(KVA_PER_CU<T> * KVA_CUS + plan.lines + 1)));

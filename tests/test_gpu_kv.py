@@ -633,3 +633,33 @@ def test_arrays_of_any_numbers(gpu, seed):  # noqa: F811
     torch.cuda.synchronize()
     assert pool_whole() and all(whole() for _, whole in buffers)
     assert all(torch.isfinite(b.view(torch.float16)).all() for b in (rotated, out, k_out, v_out))
+
+
+def test_more_workgroups_than_a_launch_has_in_one_dimension(gpu):  # noqa: F811
+    """65535 sequences of 64 key/value heads, up to 33 tokens each, in 1.06 million rows: 8.4 million lines of 512 threads, 2^32 and more.  Every sequence's row is that of a small batch with its length."""
+    say("[case] kv attention: 65535 sequences, 64 heads, 1.06 million rows")
+    torch, it = gpu
+    n_seqs, rows, heads, d = 65535, 1060000, 64, 64
+    s = Setup(gpu, "Q4_B64", heads, d, 64, [60], None, 5300, heads, max_seq=64, spare_pages=0)
+    s.fill()
+    s.describe()
+    lens = 1 + torch.arange(n_seqs, dtype=torch.int32, device="cuda") % 60
+    first = torch.arange(n_seqs + 1, dtype=torch.int32, device="cuda")
+    first[-1] += 32                                            # (the last one has 33)
+    lens[-1] = 60
+    table = torch.zeros((n_seqs, 1), dtype=torch.int32, device="cuda")
+    batch = it.kv_batch(n_seqs, 1, table, lens, 64, first, rows, 33)
+    assert it.kv_attn_workspace_bytes(s.d_cache, batch, heads) == 0
+    one = torch.randn((heads, d), device="cuda").half()
+    q, out = [torch.empty((rows, heads, d), dtype=torch.float16, device="cuda") for _ in range(2)]
+    q[:n_seqs + 32] = one
+    out[:n_seqs + 64] = 7.0
+    it.kv_attn(s.d_cache, batch, q, heads, 0.125, out, None, 0)
+    small = it.kv_batch(60, 1, table, lens, 64)
+    want = torch.empty((60, heads, d), dtype=torch.float16, device="cuda")
+    it.kv_attn(s.d_cache, small, q, heads, 0.125, want, None, 0)
+    torch.cuda.synchronize()
+    # (both rounded once, from fp32 sums of another order: next to one another)
+    where = torch.cat([lens[:-1].long() - 1, torch.arange(27, 60, device="cuda")])
+    far = (out[:n_seqs + 32].float() - want[where].float()).abs() / want[where].float().abs().clamp_min(2.0 ** -6)
+    assert float(far.max()) <= 2.0 ** -10 and bool((out[n_seqs + 32:n_seqs + 64] == 7.0).all())
