@@ -406,6 +406,11 @@ static iflow_status_t kv_pointers(const iflow::KvView &v)
 }
 
 static bool overlaps_pages(const iflow::KvView &v, const void *p, int64_t n) { return overlaps(p, n, v.pages, v.n_pages * v.page_bytes); }
+// the batch's arrays, which every workgroup reads while others write
+static bool overlaps_arrays(const iflow::KvView &v, const void *p, int64_t n)
+{
+    return overlaps(p, n, v.lens, 4LL * v.n_seqs) || (v.first && overlaps(p, n, v.first, 4LL * v.n_seqs + 4)) || (v.table && overlaps(p, n, v.table, 4LL * v.n_seqs * v.max_pages));
+}
 
 iflow_status_t iflow_kv_cache_bytes(const iflow_kv_cache_t *cache, size_t *bytes)
 {
@@ -433,6 +438,8 @@ iflow_status_t iflow_kv_append(const iflow_kv_cache_t *cache, const iflow_kv_bat
     // rows are read and written by different workgroups: only a row in its own place is read before it is written
     if (q_out != q && overlaps(q_out, q_bytes, q, q_bytes)) return IFLOW_ERR_SHAPE;
     if (overlaps(q_out, q_bytes, k_new, kv_bytes) || overlaps(q_out, q_bytes, v_new, kv_bytes) || overlaps_pages(v, q_out, q_bytes)) return IFLOW_ERR_SHAPE;
+    if (overlaps_pages(v, q, q_bytes) || overlaps_pages(v, k_new, kv_bytes) || overlaps_pages(v, v_new, kv_bytes)) return IFLOW_ERR_SHAPE;
+    if (overlaps_arrays(v, q_out, q_bytes) || overlaps_arrays(v, v.pages, v.n_pages * v.page_bytes)) return IFLOW_ERR_SHAPE;
     return device_status(iflow::launch_kv_append((int)cache->format, cache->head_dim, v, q, k_new, v_new, n_heads, (double)base, (int)pair_mode, q_out, (hipStream_t)stream));
 }
 
@@ -447,6 +454,7 @@ iflow_status_t iflow_kv_read(const iflow_kv_cache_t *cache, const iflow_kv_batch
     if (!aligned16(k_out) || !aligned16(v_out)) return IFLOW_ERR_ALIGN;
     const int64_t bytes = v.n_tokens * v.n_kv_heads * cache->head_dim * 2;
     if (overlaps(k_out, bytes, v_out, bytes) || overlaps_pages(v, k_out, bytes) || overlaps_pages(v, v_out, bytes)) return IFLOW_ERR_SHAPE;
+    if (overlaps_arrays(v, k_out, bytes) || overlaps_arrays(v, v_out, bytes)) return IFLOW_ERR_SHAPE;
     return device_status(iflow::launch_kv_read((int)cache->format, cache->head_dim, v, k_out, v_out, (hipStream_t)stream));
 }
 
@@ -476,7 +484,7 @@ iflow_status_t iflow_kv_attn(const iflow_kv_cache_t *cache, const iflow_kv_batch
     if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return IFLOW_ERR_ALIGN;
     if (workspace_bytes < need) return IFLOW_ERR_SIZE;
     const int64_t bytes = v.n_tokens * n_heads * cache->head_dim * 2;
-    if (overlaps(out, bytes, q, bytes) || overlaps_pages(v, out, bytes)) return IFLOW_ERR_SHAPE;
+    if (overlaps(out, bytes, q, bytes) || overlaps_pages(v, out, bytes) || overlaps_arrays(v, out, bytes) || (need && overlaps_arrays(v, workspace, (int64_t)need))) return IFLOW_ERR_SHAPE;
     if (need && (overlaps(workspace, (int64_t)need, q, bytes) || overlaps(workspace, (int64_t)need, out, bytes) || overlaps_pages(v, workspace, (int64_t)need))) return IFLOW_ERR_SHAPE;
     return device_status(iflow::launch_kv_attn((int)cache->format, cache->head_dim, v, q, n_heads, scale, out, workspace, (hipStream_t)stream));
 }

@@ -202,3 +202,31 @@ def test_extension_hands_the_cache_calls_on(iflow):  # noqa: F811
             with pytest.raises(iflow.IflowError) as info:
                 f(*given)
             assert info.value.status == iflow.ERR_NULL
+
+
+def test_inputs_inside_what_a_call_writes_are_refused(iflow):  # noqa: F811
+    """Queries, keys and values that lie in the pages, and a batch's arrays in the pages, the outputs or the workspace: other workgroups would read what has been written over them."""
+    L, at, far = iflow.lib(), 0x100000, 0x10000000
+    c = iflow.kv_cache(iflow.Q4_B64, 8, 128, 64, 100, far)
+    pool, kv, q = iflow.kv_cache_bytes(c), 9 * 8 * 128 * 2, 9 * 32 * 128 * 2
+
+    def batch(**change):
+        return iflow.kv_batch(4, 20, change.get("table", 30 * at), change.get("lens", 31 * at), 1280, first_token=change.get("first", 32 * at), n_tokens=9, max_tokens=5)
+
+    def append(b, q_in=20 * at, k=21 * at, v=22 * at, out=23 * at):
+        return L.iflow_kv_append(c, b, q_in, k, v, 32, 10000.0, 1, out, None)
+    for near in (far + pool - 16, far + 16 - q):
+        assert append(batch(), q_in=near) == iflow.ERR_SHAPE and append(batch(), q_in=near, out=near) == iflow.ERR_SHAPE
+    for near in (far + pool - 16, far + 16 - kv):
+        assert append(batch(), k=near) == iflow.ERR_SHAPE and append(batch(), v=near) == iflow.ERR_SHAPE
+    need = iflow.kv_attn_workspace_bytes(c, batch(), 32)
+    assert need > 0
+    for name, size in (("table", 4 * 20 * 4), ("lens", 4 * 4), ("first", 5 * 4)):
+        for start, end in ((far, far + pool), (23 * at, 23 * at + q)):
+            for place in (end - 4, start + 4 - size):
+                assert append(batch(**{name: place})) == iflow.ERR_SHAPE, (name, start)
+        for place in (24 * at + kv - 4, 24 * at + 4 - size):
+            assert L.iflow_kv_read(c, batch(**{name: place}), 24 * at, 25 * at, None) == iflow.ERR_SHAPE and L.iflow_kv_read(c, batch(**{name: place}), 25 * at, 24 * at, None) == iflow.ERR_SHAPE
+        for start, end in ((26 * at, 26 * at + q), (3 * far, 3 * far + need)):
+            for place in (end - 4, start + 4 - size):
+                assert L.iflow_kv_attn(c, batch(**{name: place}), 20 * at, 32, 0.1, 26 * at, 3 * far, need, None) == iflow.ERR_SHAPE, (name, start)
