@@ -352,7 +352,8 @@ iflow_status_t iflow_kv_cache_bytes(const iflow_kv_cache_t *cache, size_t *bytes
 iflow_status_t iflow_kv_append(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new, int n_heads,
                                float base, iflow_rope_pairing_t pair_mode, uint16_t *q_out, void *stream);
 
-/* What the cache stands for: keys and values of the batch's tokens, k_out, v_out [n_tokens][n_kv_heads][head_dim] fp16.  (A whole sequence: n_b = seq_lens[b].) */
+/* What the cache stands for: keys and values of the batch's tokens, k_out, v_out [n_tokens][n_kv_heads][head_dim] fp16.  (A whole sequence: n_b = seq_lens[b].)  The row of a token
+ * whose position is outside 0 .. max_seq - 1, or on a page that is not there, becomes zeros. */
 iflow_status_t iflow_kv_read(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, uint16_t *k_out, uint16_t *v_out, void *stream);
 
 /* Grouped-query attention of the batch's tokens over the cache, causal: with K, V what iflow_kv_read gives, token i of sequence b, at position p, and query head h
