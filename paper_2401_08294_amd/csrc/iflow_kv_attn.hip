@@ -24,7 +24,8 @@ template <typename T> constexpr int KVA_PER_CU = T::D == 64 ? 4 : 3;
 constexpr int KVA_CUS = 256;
 constexpr float KVA_BELOW = 7.f, KVA_LAG = 15.f, KVA_SPARE = 16.f;       // in units of log2: see attn_decode_mfma_kernel
 
-// (the compiler quiets every operand of fmaxf first)
+// (The compiler quiets every operand of fmaxf first.  It does not see what these read: an accumulator of the matrix instructions is read by one of its own before, on whose result these depend, because it
+// waits for them - up to twelve instructions long - only there.)
 __device__ __forceinline__ float kv_max3(float a, float b, float c)
 {
     float r;
@@ -270,7 +271,10 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
                     for (int e = 0; e < 8; ++e)
                         if (!there || p0 + 16 * (e >> 2) + 4 * g + (e & 3) >= limit) sacc[e >> 2][e & 3] = -INFINITY;
                 }
-                float bm = kv_max3(kv_max3(kv_max3(sacc[0][0], sacc[0][1], sacc[0][2]), sacc[0][3], sacc[1][0]), kv_max3(sacc[1][1], sacc[1][2], sacc[1][3]), -INFINITY);
+                float bm = fmaxf(sacc[0][3], sacc[1][3]);     // (the compiler's own: see kv_max3)
+                bm = kv_max3(bm, sacc[0][0], sacc[0][1]);
+                bm = kv_max3(bm, sacc[0][2], sacc[1][0]);
+                bm = kv_max3(bm, sacc[1][1], sacc[1][2]);
                 bm = kva_max_of_rows(bm) * scale_log2e;
                 const bool follow = bm > m + KVA_LAG;         // (the first tile with a score above -inf: always)
                 if (__builtin_amdgcn_ballot_w64(follow) != 0) {
@@ -624,12 +628,9 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
                     if (32 * tl + 16 * ((e >> 2) & 1) + 8 * (e >> 3) + (e & 3) >= seen_of_tile) sacc[tl][e] = -INFINITY;
             }
         }
-        float bm = kv_max3(sacc[0][0], sacc[0][1], sacc[1][0]);
-        bm = kv_max3(bm, sacc[1][1], sacc[0][2]);
+        float bm = fmaxf(sacc[0][15], sacc[1][15]);           // (the compiler's own: see kv_max3)
 #pragma unroll
-        for (int e = 3; e < 15; e += 2) { bm = kv_max3(bm, sacc[0][e], sacc[0][e + 1]); bm = kv_max3(bm, sacc[1][e - 1], sacc[1][e]); }
-        bm = kv_max3(bm, sacc[0][15], sacc[1][14]);
-        bm = kv_max3(bm, sacc[1][15], -INFINITY);
+        for (int e = 0; e < 15; ++e) bm = kv_max3(bm, sacc[0][e], sacc[1][e]);
         const auto other = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, bm), __builtin_bit_cast(uint32_t, bm), false, false);
         bm = kv_max3(__builtin_bit_cast(float, (uint32_t)other[0]), __builtin_bit_cast(float, (uint32_t)other[1]), -INFINITY) * scale_log2e;
         const bool follow = bm > m + KVA_LAG;                 // (the first step with a score above -inf: always)
