@@ -360,7 +360,8 @@ iflow_status_t iflow_kv_read(const iflow_kv_cache_t *cache, const iflow_kv_batch
  *   out = fp16( sum_{t <= p} softmax_t(scale * q . K[j][t]) V[j][t] ),   j = h / (n_heads / n_kv_heads),
  * zeros where it sees no position.  The tokens' own keys and values are in the cache already (iflow_kv_append first).  One token per sequence is a decode step, a few a check of drafted
  * tokens, many a prompt or its next chunk.
- *   q, out [n_tokens][n_heads][head_dim] fp16, not overlapping; n_heads as for iflow_kv_append, max_tokens * n_heads / n_kv_heads at most 2^22; scale > 0.
+ *   q, out [n_tokens][n_heads][head_dim] fp16, not overlapping; n_heads as for iflow_kv_append, max_tokens * n_heads / n_kv_heads at most 2^22; 0 < scale < 2e38, and
+ *   scale times a score is assumed to be finite in fp32.
  *   workspace: device memory of iflow_kv_attn_workspace_bytes() bytes for this description, 16-byte aligned (null if that is 0): partial results of the position ranges, which mean
  *   nothing before and after the call.  Calls that share one must be ordered.
  * Sums, maxima and the output before its one rounding are fp32; sums are taken in a fixed order. */

@@ -475,7 +475,7 @@ iflow_status_t iflow_kv_attn(const iflow_kv_cache_t *cache, const iflow_kv_batch
     iflow::KvView v;
     iflow_status_t st = kv_shapes(cache, batch, true, n_heads, &v);
     if (st != IFLOW_OK) return st;
-    if (!(scale > 0.0f && scale < 3.0e38f)) return IFLOW_ERR_SHAPE;
+    if (!(scale > 0.0f && scale < 2.0e38f)) return IFLOW_ERR_SHAPE;      // (times log2 e it is a number too)
     if ((int64_t)v.max_tokens * (n_heads / v.n_kv_heads) > (1 << 22)) return IFLOW_ERR_SHAPE;
     const size_t need = iflow::kv_attn_workspace_bytes(v, cache->head_dim, n_heads);
     if (!q || !out || (need && !workspace)) return IFLOW_ERR_NULL;

@@ -23,6 +23,9 @@ constexpr int KVA_ROWS = 16;                                  // rows of a workg
 template <typename T> constexpr int KVA_PER_CU = T::D == 64 ? 4 : 3;
 constexpr int KVA_CUS = 256;
 constexpr float KVA_BELOW = 7.f, KVA_LAG = 15.f, KVA_SPARE = 16.f;       // in units of log2: see attn_decode_mfma_kernel
+// A score's distance from the reference is one multiply-add, rounded once, while the reference is a rounded product: they differ by half a step of it, 2^-4 at 2^20.  Where a reference is as large, the scores
+// are multiplied and rounded first, as it was (else the largest probability is two to that difference: no number from 2^32 on).
+constexpr float KVA_FAR = 1048576.f;
 
 // (The compiler quiets every operand of fmaxf first.  It does not see what these read: an accumulator of the matrix instructions is read by one of its own before, on whose result these depend, because it
 // waits for them - up to twelve instructions long - only there.)
@@ -200,6 +203,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
             qb[u] = __builtin_bit_cast(kv_half8, w);
         }
         float m = -INFINITY, l = 0.f;                         // of row li (m is the same in the row's four lanes)
+        bool far = false;                                     // a row's reference is, or was, as large as KVA_FAR
         kv_float4 oacc[NC];                                   // oacc[c][e] = O[row 4g+e][16c + li]
 #pragma unroll
         for (int c = 0; c < NC; ++c) oacc[c] = (kv_float4){0.f, 0.f, 0.f, 0.f};
@@ -282,6 +286,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
                     const bool nothing = __builtin_amdgcn_ballot_w64(m != -INFINITY) == 0;
                     l *= alpha;
                     m = follow ? bm - KVA_BELOW : m;
+                    far = far || __builtin_amdgcn_ballot_w64(fabsf(m) >= KVA_FAR && m != -INFINITY) != 0;
                     if (!nothing) {                           // the accumulators hold rows 4g .. 4g+3: their factors live in lanes 4g .. 4g+3
                         float al[4];
 #pragma unroll
@@ -293,12 +298,17 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
                     }
                 }
                 const float below = (m == -INFINITY) ? 0.f : -m;       // (a row that has seen nothing: no -inf - -inf)
+                if (__builtin_expect(far, false)) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sacc[e >> 2][e & 3] *= scale_log2e;
+                }
+                const float by = far ? 1.f : scale_log2e;
                 // the probabilities as two fp16 numbers, the first cut off so that both are positive: together within 2^-21 of them
                 KvPairs pa, pr;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float p0e = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e >> 1][2 * (e & 1)], scale_log2e, below));          // exp2(-inf) = 0 for masked positions
-                    const float p1e = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e >> 1][2 * (e & 1) + 1], scale_log2e, below));
+                    const float p0e = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e >> 1][2 * (e & 1)], by, below));          // exp2(-inf) = 0 for masked positions
+                    const float p1e = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e >> 1][2 * (e & 1) + 1], by, below));
                     l += p0e; l += p1e;
                     pa.p[e] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(p0e, p1e));
                     pr.p[e] = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(kv_less_low(p0e, pa.p[e]), kv_less_high(p1e, pa.p[e])));
@@ -503,6 +513,7 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
         qb[u] = __builtin_bit_cast(kv_half8, w);
     }
     float m = -INFINITY, l = 0.f;
+    bool far = false;                                         // a row's reference is, or was, as large as KVA_FAR
     kv_float16 oacc[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -616,6 +627,7 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
         for (int n = 0; n < 2 * NU; ++n) to[n % 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_operand(from, n), qb[n / 2], to[n % 2], 0, 0, 0);
     };
     // what a row does not see goes, and the reference and the sums follow where a score is far above
+    float by = scale_log2e;                                   // what the scores that have been settled are still to be multiplied by
     auto settle = [&](int t0, bool there0, bool there1) {
         if (!there0 || !there1 || t0 * KV_TILE + STEP > shortest) {
             int seen = limit - t0 * KV_TILE - 4 * hf;         // of the step's positions, less the lane's own first
@@ -638,19 +650,27 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
             const float alpha = follow ? __builtin_amdgcn_exp2f(m - (bm - KVA_BELOW)) : 1.0f;
             l *= alpha;
             m = follow ? bm - KVA_BELOW : m;
+            far = far || __builtin_amdgcn_ballot_w64(fabsf(m) >= KVA_FAR && m != -INFINITY) != 0;
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) oacc[c][e] *= alpha;
         }
+        if (__builtin_expect(far, false)) {
+#pragma unroll
+            for (int tl = 0; tl < 2; ++tl)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sacc[tl][e] *= scale_log2e;
+        }
+        by = far ? 1.f : scale_log2e;
     };
     // The probabilities of eight positions as operand n of four: two fp16 numbers each, the first cut off, together within 2^-21 of them (as in kv_attn_kernel).
     KvPairs pb[2], pr[2];                                     // of operands n % 2
     float below = 0.f;                                        // what is added to a score (a row that has seen nothing: no -inf - -inf)
     auto weigh_pair = [&](int n) {                            // scores 2 n, 2 n + 1 of 32 to probabilities, in place of operand n / 4
         const int tl = n / 8, z = n / 4 % 2, e = n % 4;
-        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tl][8 * z + 2 * e], scale_log2e, below));
-        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tl][8 * z + 2 * e + 1], scale_log2e, below));
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tl][8 * z + 2 * e], by, below));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[tl][8 * z + 2 * e + 1], by, below));
         l += p0; l += p1;
         asm volatile("" : "+v"(l));                           // (added here, not all of a step's at its end, kept in registers until then)
         const half2_t first = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(p0, p1));

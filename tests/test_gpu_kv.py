@@ -663,3 +663,23 @@ def test_more_workgroups_than_a_launch_has_in_one_dimension(gpu):  # noqa: F811
     where = torch.cat([lens[:-1].long() - 1, torch.arange(27, 60, device="cuda")])
     far = (out[:n_seqs + 32].float() - want[where].float()).abs() / want[where].float().abs().clamp_min(2.0 ** -6)
     assert float(far.max()) <= 2.0 ** -10 and bool((out[n_seqs + 32:n_seqs + 64] == 7.0).all())
+
+
+@pytest.mark.parametrize("name,n_heads,n_kv,d,lens,counts", [("Q4_B64", 8, 2, 128, [300, 33, 70], None), ("Q8_B32", 8, 1, 64, [2000, 40], None), ("Q8_B64", 64, 64, 128, [150], [130]), ("Q4_B32", 64, 64, 64, [129, 170, 150, 80], [129, 72, 130, 80])])
+def test_attention_with_scores_of_millions_and_more(gpu, name, n_heads, n_kv, d, lens, counts):  # noqa: F811
+    """Finite queries and keys as large as fp16 has them: scores of 10^4 to 10^11 of either sign, whose neighbours are 2^-11 of themselves apart, far more than fp32 sums round by.  The largest has all the
+    weight (those equal to it share it: keys are one number in all their components, so equal scores are equal bits), and the output is its value, rounded once."""
+    say(f"[case] kv attention, large scores: {name} {n_heads}/{n_kv} heads of {d}, lengths {lens}, tokens {counts}")
+    s = Setup(gpu, name, n_kv, d, 64, lens, counts, 5400 + n_heads + d, n_heads)
+    for b, n in enumerate(lens):
+        k, v = s.values(n)
+        c = np.ldexp(s.rng.integers(1024, 2048, n).astype(np.float64), s.rng.integers(0, 5, n)) * s.rng.choice([1.0, -1.0], n)
+        if b == 1:
+            c = -np.abs(c)                                     # (all of one sign: scores that are all far below zero for one sign of the queries)
+        k.view(np.float16)[:] = c.astype(np.float16)[:, None, None]
+        for p in range(n):
+            s.cache.store(s.table[b], p, k[p], v[p])
+    s.describe()
+    q = np.zeros((s.n_tokens, n_heads, d), np.float16)
+    q[:] = np.resize([1.0, -1.0, 40.0, -40.0, 1000.0, -3000.0, 60000.0, -60000.0], n_heads)[None, :, None]
+    s.check_attend(q.view(np.uint16), d ** -0.5, tol=2.0 ** -11 + 2.0 ** -15)
