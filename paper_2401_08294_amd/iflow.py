@@ -395,10 +395,13 @@ def kv_cache(fmt: int, n_kv_heads: int, head_dim: int, page_positions: int, n_pa
     return d
 
 
-def kv_batch(n_seqs: int, max_pages: int, page_table, seq_lens, max_seq: int, first_token=None, n_tokens=None, max_tokens: int = 1) -> KvBatch:
+def kv_batch(n_seqs: int, max_pages: int, page_table, seq_lens, max_seq: int, first_token=None, n_tokens=None, max_tokens=None) -> KvBatch:
     """Describes the tokens of a call: int32 device tensors page_table [n_seqs][max_pages] (None: sequence b's pages are b * max_pages ..), seq_lens [n_seqs], and, unless every
-    sequence has one token, first_token [n_seqs + 1].  The description keeps the tensors; their contents are read when a call's kernels run."""
-    d = KvBatch(n_seqs, max_pages, _ptr(page_table), _ptr(seq_lens), _ptr(first_token), n_seqs if n_tokens is None else n_tokens, max_tokens, max_seq)
+    sequence has one token, first_token [n_seqs + 1] with n_tokens, the rows of the call's arrays, and max_tokens, the most of one sequence: what lies past either is left out by the calls, so neither
+    has a default then.  The description keeps the tensors; their contents are read when a call's kernels run."""
+    if first_token is not None and (n_tokens is None or max_tokens is None):
+        raise ArgumentError("first_token says how many tokens a sequence has: n_tokens and max_tokens are wanted with it")
+    d = KvBatch(n_seqs, max_pages, _ptr(page_table), _ptr(seq_lens), _ptr(first_token), n_seqs if n_tokens is None else n_tokens, 1 if max_tokens is None else max_tokens, max_seq)
     d._keep = (page_table, seq_lens, first_token)
     return d
 

@@ -230,3 +230,14 @@ def test_inputs_inside_what_a_call_writes_are_refused(iflow):  # noqa: F811
         for start, end in ((26 * at, 26 * at + q), (3 * far, 3 * far + need)):
             for place in (end - 4, start + 4 - size):
                 assert L.iflow_kv_attn(c, batch(**{name: place}), 20 * at, 32, 0.1, 26 * at, 3 * far, need, None) == iflow.ERR_SHAPE, (name, start)
+
+
+def test_a_batch_of_several_tokens_says_how_many(iflow):  # noqa: F811
+    """Rows past n_tokens and a sequence's tokens past max_tokens are left out by the calls: with first_token neither is guessed."""
+    for given in ({}, {"n_tokens": 9}, {"max_tokens": 5}):
+        with pytest.raises(TypeError):
+            iflow.kv_batch(4, 20, 64, 128, 1280, first_token=192, **given)
+    d = iflow.kv_batch(4, 20, 64, 128, 1280, first_token=192, n_tokens=9, max_tokens=5)
+    assert (d.n_tokens, d.max_tokens) == (9, 5)
+    d = iflow.kv_batch(4, 20, 64, 128, 1280)
+    assert (d.n_tokens, d.max_tokens, d.first_token) == (4, 1, None)
