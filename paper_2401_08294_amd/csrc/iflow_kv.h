@@ -48,8 +48,8 @@ struct KvView {
 };
 
 // One sequence's new tokens as the kernels take them: rows row .. row + count - 1 of the batch's tokens at positions position .. .  Whatever the arrays
-// hold, what comes out of here stays inside the call's buffers: count is at most max_tokens and ends with the rows that there are, and every token is asked for with has().  (In 32 bits: where numbers
-// that no batch has leave them, what has() sees is other numbers, and it still sees them.)
+// hold, what comes out of here stays inside the call's buffers: count is at most max_tokens, and every token is asked for with has().  (In 32 bits: where numbers that no batch has
+// leave them, what has() sees is other numbers, and it still sees them.)
 struct KvSequence {
     int row, position, count, n_tokens, max_seq;
     __device__ __forceinline__ KvSequence(const KvView &v, int b)
@@ -58,7 +58,7 @@ struct KvSequence {
         const int n = v.first ? (int)((uint32_t)v.first[b + 1] - (uint32_t)row) : 1;
         n_tokens = (int)v.n_tokens; max_seq = v.max_seq;
         position = (int)((uint32_t)v.lens[b] - (uint32_t)n);
-        count = max(0, min(min(n, v.max_tokens), (int)((uint32_t)n_tokens - (uint32_t)row)));
+        count = max(0, min(n, v.max_tokens));
     }
     // token i has a row, and a position that the cache has
     __device__ __forceinline__ bool has_row(int i) const { return (uint32_t)i < (uint32_t)count && (uint32_t)row + (uint32_t)i < (uint32_t)n_tokens; }
