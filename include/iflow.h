@@ -324,7 +324,8 @@ iflow_status_t iflow_rope_append(uint16_t *q, const uint16_t *k_new, const uint1
  *   caller's buffers: rows outside 0 .. n_tokens - 1, tokens of a sequence past max_tokens and positions outside 0 .. max_seq - 1 are left out; a page outside 0 .. n_pages - 1 is
  *   not there: nothing is written to it, it reads back as zeros, attention passes its positions over.  Rows of no token are left as they were; of a row that
  *   two sequences claim, it is unspecified whose it becomes, and where they claim more rows than n_tokens together, which rows attention serves.
- *   Two sequences of one iflow_kv_append call must not share the page that either of them writes to (what they write there is unspecified); pages that are only read may be shared.
+ *   Two sequences of one iflow_kv_append call must not share the page that either of them writes to, nor may a sequence have one page in two places and write to both (what is written there is
+ *   unspecified); pages that are only read may be shared.
  * Values are assumed finite, and so is what they stand for.  Sizes: head_dim 64 or 128; 1 <= n_kv_heads <= 64; page_positions a multiple of 32, at most 2^20; 1 <= n_pages < 2^31, at most 2^46 bytes;
  * 1 <= n_seqs <= 65535; 1 <= max_tokens <= max_seq <= max_pages * page_positions, max_seq <= 2^20; 1 <= n_tokens <= 2^24; n_seqs * max_tokens <= 2^24.  The three
  * arrays are 4-byte aligned, the others 16; what a call writes overlaps nothing else of it but where that is said. */

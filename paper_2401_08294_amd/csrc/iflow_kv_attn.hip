@@ -63,7 +63,7 @@ __device__ __forceinline__ float kva_max_of_rows(float x)
 // (Tried: ranges of a fixed number of positions: a die gets the same range of every sequence, 66 us for 32 sequences of 1000 to 8001 positions, 32/8 heads, turned by head and
 // sequence 51; exactly equal shares of consecutive tiles that cross from line to line: a workgroup that crosses takes 5 us longer, and the rest wait for it, 45.)
 // (Tiles are counted in 32 bits: where all lines might have more, every line is a workgroup's.  The device trusts no count that the host has not bounded: where the arrays make more lines than
-// `max_lines`, which only sequences that claim the same rows do, a line is one part, whatever it is long, and nothing but lines is counted: those are below 2^30 whatever the arrays hold.)
+// `max_lines`, which only sequences that claim rows twice or rows that there are not do, a line is one part, however long, and nothing but lines is counted: those are below 2^30 whatever the arrays hold.)
 constexpr int KVA_WHOLE = 1 << 20;                            // a part of more tiles than a line has
 struct KvLines { int tiles, lines; };                         // of each line; lines of the sequence
 // (sequences of `few` rows and more are not served by sixteens)
@@ -699,7 +699,7 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
         uint8_t *k_at = stage, *v_at = stage + KEYS;
         load_keys(first_of(0)); load_values(first_of(0));
         // Half the groups are a phase behind: the two wavefronts of a SIMD are of either half, and one decodes while the other uses the matrix cores.  (512 tokens behind 3888, 32/8 heads x 128, 4 bits:
-        // 64.7 us in step, 61.4 so; neighbouring groups in turn 66.)
+        // 75.8 us in step, 72.3 so; neighbouring groups in turn 84.8.)
         if (pg >= PG / 2) __syncthreads();
         for (int trip = 0; trip < trips; ++trip) {
             const int t0 = first_of(trip);
@@ -755,7 +755,7 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
             cut_values(first_of(trip + 1));
             // Of 2 NU = 4 NC scores' products NC are ahead of the values' by which the first operand is made; then a value's two products, a score's and the making of a part of the next operand go
             // together.  (Values and keys are read two products ahead; the barriers hold the order, which the scheduler takes apart into matrix and vector instructions.)
-            static_assert(NU == 2 * NC, "as many products for the scores of a step as operands of values");
+            static_assert(NU == 2 * NC, "as many products for the scores of a step as operands of its values");
             kv_half8 ka[2], va[2];
 #pragma unroll
             for (int n = 0; n < 2; ++n) { ka[n] = key_operand(k_at(trip + 1), n); va[n] = value_operand(v_at(trip), n); }
@@ -852,15 +852,19 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
 }
 
 // How a call is served.  `rows`: of a workgroup that decodes for many (0: by sixteens).  Us, by sixteens / 64 rows / 128 rows, for so many blocks of 64 rows (graph replay):
-//   32/8 heads x 128, 4 bits, one sequence of 4000                   64: 39 / 51 / 92    128: 66 / 54 / 94    256: 100 / 61 / 96   512: 181 / 109 / 104  1024: 298 / 184 / 139
-//   ... eight of 250 to 2000 (blocks: if all had as many as most)    128: 24 / 30 / 51   256: 30 / 31 / 52    512: 49 / 46 / 55    1024: 82 / 62 / 60
-//   64/8 heads x 128, 8 bits, one of 1000                            64: 13 / 24 / 38    128: 19 / 25 / 41    256: 30 / 27 / 45    512: 48 / 48 / 51
-//   71/1 heads x 64, 4 bits, one of 2000                             71: 19 / 21 / 44    142: 26 / 22 / 44
+//   32/8 heads x 128, 4 bits, one sequence of 4000                   64: 40 / 56 / 102   128: 66 / 59 / 103   256: 103 / 71 / 107  512: 177 / 122 / 122  1024: 291 / 204 / 172
+//   ... eight of 250 to 2000 (blocks: if all had as many as most)    128: 24 / 33 / 56   256: 30 / 34 / 57    512: 49 / 50 / 60    1024: 81 / 69 / 70
+//   64/8 heads x 128, 8 bits, one of 1000                            64: 13 / 23 / 41    128: 19 / 24 / 43    256: 30 / 26 / 48    512: 49 / 43 / 55
+//   71/1 heads x 64, 4 bits, one of 2000                             71: 19 / 23 / 49    142: 27 / 23 / 50
+// and of several sequences, by sixteens / 64 rows at 256 blocks and 384:
+//   32/8 x 128, 4 bits, two of 4000  74 / 59, 98 / 68    four of 4000  68 / 59, 76 / 62    32/32 x 128, two of 2000  32 / 35, 48 / 44
+//   64/8 x 128, 8 bits, four of 1000  20 / 24, 23 / 25   64/8 x 64, three of 2000  27 / 24, 24 / 29   64/64 x 64, two of 300  11 / 10, 13 / 13
 // Blocks of 64 rows take as long for one as for 256; those of 128 take two for each compute unit to hide one another's waits.
 // A batch with a few long sequences among many short ones (`packed`: fewer than half of n_seqs * max_tokens rows) is numbered by what there is of it, and its sequences of fewer rows
 // than `few` go by sixteens beside the others.  (Us, numbered by max_tokens and all in blocks / so, 32/8 heads x 128, 4 bits: 2000 tokens of one sequence and one each of 63 others, all of 2000
-// positions, 168 / 90; of 255 others 452 / 156; 8000 tokens and 63 others of 8000 positions 1221 / 733; one of 2000 and two single ones 80 / 84, two and five 135 / 110, three and five 169 / 157.  Where most have many tokens it is two
-// launches for little or nothing, as for one of 2000 and one single one, 80 / 88; but three of 500 and three single ones of 4000 positions, on the boundary, 97 / 45.)
+// positions, 202 / 101; of 255 others 547 / 168; 8000 tokens and 63 others of 8000 positions 1553 / 850; two of 2000 and five single ones 164 / 137, three and five 206 / 195.  Where most have many tokens it
+// is two launches for little or nothing, and left: one of 2000 and one single one 90, where the prompt alone takes 84; but also three of 500 and three single ones of 4000 positions, on the boundary, 107,
+// where the prompts alone take 35 and the others 11.)
 // `direct`: a line is a workgroup's, without a second launch, of so many wavefronts (0: lines are cut).  Us (graph replay; one page table, lengths an eighth to the whole), cut / direct with four
 // wavefronts / with eight, for the longest sequence's positions:
 //                                        512               768               1024              2048
