@@ -370,6 +370,30 @@ iflow_status_t iflow_kv_attn_workspace_bytes(const iflow_kv_cache_t *cache, cons
 iflow_status_t iflow_kv_attn(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace,
                              size_t workspace_bytes, void *stream);
 
+/* A step's page table, first tokens and slots, built on the device from the sequences' lengths: what a program that serves does before iflow_kv_append.  The batch is described as for the other
+ * calls, with seq_lens as they will be after the step (0: a sequence that has ended, or none), and `new_tokens[b]` of these positions the step's own; page_table and first_token, which the other
+ * calls read, are WRITTEN here.  (The cache gives n_pages and page_positions; its pages are not touched.)  With P = page_positions:
+ *   a sequence of n positions needs max(0, ceil(n / P) - n_shared) pages of its own behind the n_shared that all have in common; it has held[b], entries n_shared .. of its row.
+ *   It takes what it lacks, and gives back what it has too many, its last; held_out[b] says how many it has then, first_token[b + 1] - first_token[b] = new_tokens[b].
+ *   free_pages [n_pages] is a ring of the pages that no sequence holds, free_state = {where the first of them is, how many they are, not read}.  Pages are taken from its front in the order of the
+ *   sequences and of a sequence's positions, and given back behind its end in the same order: what is given back can be taken from the next call on.  free_state_out = {first, how many, how many
+ *   pages were wanted and not there}.  Where none is left the entry becomes -1, the page that is not there, and is wanted again in the next call.
+ *   The entries of a sequence's shared pages are written where it has positions; those of pages that it had or gives back stay as they were.
+ *   slots (may be null) [n_tokens]: where a token's position lies, page * P + position mod P, or -1 without a position or page.  Rows of no token are left as they were.
+ * new_tokens is taken as 0 .. max_tokens, a length as at most max_seq.  first_token null: one token each, row b, and new_tokens is not read.
+ * All arrays are device arrays, int32 and 4-byte aligned but for slots (int64, 8).  held_out may be held, and free_state_out free_state; nothing else that is written may overlap anything
+ * (IFLOW_ERR_SHAPE).  n_seqs * max_pages < 2^31.  Whatever the arrays hold, what is read and written lies inside them; a ring of fewer entries than are given back loses the rest.
+ * workspace: iflow_kv_tables_workspace_bytes() bytes, 16-byte aligned.  Calls that share one must be ordered. */
+typedef struct iflow_kv_pages_t {
+    const int32_t *held, *free_state;
+    int32_t *held_out, *free_state_out, *free_pages;
+    const int32_t *shared_pages;    /* device [n_shared]; null without */
+    int32_t n_shared;
+} iflow_kv_pages_t;
+iflow_status_t iflow_kv_tables_workspace_bytes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, size_t *bytes);
+iflow_status_t iflow_kv_tables(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const iflow_kv_pages_t *pages, const int32_t *new_tokens, int64_t *slots, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
 /* A whole decode step of a decoder stack in ONE launch (Section 5: Infer() = one pass over all layers for the step's token;
  * Section 2's module table for the LLaMA family: "rms" normalization, "rope" position embedding, "silu" activation with a gate;
  * section "Grouped-query attention").  Per layer, with h the layer's input [hidden]:

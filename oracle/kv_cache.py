@@ -162,3 +162,34 @@ def attend(cache: Cache, table, lens, first, max_tokens: int, max_seq: int, q16,
             s = scale * (k[there, j] @ q16[row, h].view(np.float16).astype(np.float64))
             e = np.exp(s - s.max())
             out[row, h] = (e / e.sum()) @ v[there, j]
+
+
+def tables(lens, new, held, free, ring, table, shared, page: int, n_pages: int, n_tokens: int, max_tokens: int, max_seq: int, slots):
+    """Page table, first tokens and slots of a step, one sequence and one page after another (include/iflow.h: iflow_kv_tables).  new None: one token each.  ring, table and slots are
+    modified in place; returns held, {first free, how many, missing} and first_token as they are then."""
+    n_shared = len(shared)
+    start, count = int(free[0]), int(free[1])
+    front, end, missing, row = start, start + count, 0, 0
+    held, first = [int(h) for h in held], [0]
+    for b in range(len(lens)):
+        n = min(max(int(lens[b]), 0), max_seq)
+        if n > 0:
+            table[b, :n_shared] = shared
+        need, had = max(0, -(-n // page) - n_shared), held[b]
+        held[b] = min(need, had)
+        for j in range(need, had):
+            ring[end % n_pages] = table[b, n_shared + j]
+            end += 1
+        for j in range(had, need):
+            there = front < start + count
+            table[b, n_shared + j] = ring[front % n_pages] if there else -1
+            front, held[b], missing = (front + 1, held[b] + 1, missing) if there else (front, held[b], missing + 1)
+        tokens = 1 if new is None else min(max(int(new[b]), 0), max_tokens)
+        for i in range(tokens):
+            p = int(lens[b]) - tokens + i
+            at = int(table[b, p // page]) if 0 <= p < max_seq else -1
+            if row < n_tokens:
+                slots[row] = at * page + p % page if 0 <= at < n_pages else -1
+            row += 1
+        first.append(row)
+    return held, [front % n_pages, end - front, missing], first

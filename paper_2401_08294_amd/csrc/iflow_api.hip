@@ -489,6 +489,56 @@ iflow_status_t iflow_kv_attn(const iflow_kv_cache_t *cache, const iflow_kv_batch
     return device_status(iflow::launch_kv_attn((int)cache->format, cache->head_dim, v, q, n_heads, scale, out, workspace, (hipStream_t)stream));
 }
 
+// the sizes of a call that builds a batch's tables, without their pointers (the cache's pages are not touched)
+static iflow_status_t kv_tables_shapes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, iflow::KvView *v)
+{
+    const iflow_status_t st = kv_shapes(cache, batch, false, 0, v);
+    if (st != IFLOW_OK) return st;
+    return (int64_t)v->n_seqs * v->max_pages >= (1LL << 31) ? IFLOW_ERR_SHAPE : IFLOW_OK;      // (pages are numbered in 32 bits)
+}
+
+iflow_status_t iflow_kv_tables_workspace_bytes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, size_t *bytes)
+{
+    iflow::KvView v;
+    if (!bytes) return IFLOW_ERR_NULL;
+    const iflow_status_t st = kv_tables_shapes(cache, batch, &v);
+    if (st != IFLOW_OK) return st;
+    *bytes = iflow::kv_tables_workspace_bytes(v);
+    return IFLOW_OK;
+}
+
+iflow_status_t iflow_kv_tables(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const iflow_kv_pages_t *pages, const int32_t *new_tokens, int64_t *slots, void *workspace,
+                               size_t workspace_bytes, void *stream)
+{
+    iflow::KvView v;
+    const iflow_status_t st = kv_tables_shapes(cache, batch, &v);
+    if (st != IFLOW_OK) return st;
+    if (!pages) return IFLOW_ERR_NULL;
+    if (pages->n_shared < 0 || pages->n_shared > v.max_pages) return IFLOW_ERR_SHAPE;
+    const iflow::KvTables t = {new_tokens, pages->held, pages->free_state, pages->shared_pages, pages->held_out, pages->free_state_out, pages->free_pages, slots, pages->n_shared};
+    if (!v.table || !v.lens || !t.held || !t.free_state || !t.held_out || !t.free_out || !t.ring || !workspace || (v.first && !new_tokens) || (t.n_shared > 0 && !t.shared)) return IFLOW_ERR_NULL;
+    // (all that the call reads and writes: address, bytes, whether it is written)
+    const int64_t n = v.n_seqs;
+    struct { const void *at; int64_t bytes; bool written; } all[] = {
+        {v.lens, 4 * n, false}, {v.first ? new_tokens : nullptr, 4 * n, false}, {t.held, 4 * n, false}, {t.free_state, 12, false}, {t.n_shared > 0 ? t.shared : nullptr, 4LL * t.n_shared, false},
+        {v.table, 4 * n * v.max_pages, true}, {v.first, 4 * n + 4, true}, {t.held_out, 4 * n, true}, {t.free_out, 12, true}, {t.ring, 4 * v.n_pages, true}, {slots, 8 * v.n_tokens, true},
+        {workspace, (int64_t)iflow::kv_tables_workspace_bytes(v), true}};
+    const auto *held = &all[2], *free_state = &all[3], *held_out = &all[7], *free_out = &all[8];
+    for (const auto &a : all)
+        if ((reinterpret_cast<uintptr_t>(a.at) & 3) != 0) return IFLOW_ERR_ALIGN;
+    if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(slots) & 7) != 0) return IFLOW_ERR_ALIGN;
+    if (workspace_bytes < iflow::kv_tables_workspace_bytes(v)) return IFLOW_ERR_SIZE;
+    for (const auto &a : all)
+        for (const auto &b : all) {
+            if (&a == &b || !a.at || !b.at || !b.written || !overlaps(a.at, a.bytes, b.at, b.bytes)) continue;
+            // (in place: a sequence's pages, or the ring's ends, are read before they are written)
+            const bool in_place = (t.held == t.held_out && ((&a == held && &b == held_out) || (&a == held_out && &b == held))) ||
+                                  (t.free_state == t.free_out && ((&a == free_state && &b == free_out) || (&a == free_out && &b == free_state)));
+            if (!in_place) return IFLOW_ERR_SHAPE;
+        }
+    return device_status(iflow::launch_kv_tables(v, t, workspace, (hipStream_t)stream));
+}
+
 // ---- the chained launch ---------------------------------------------------------------------------------------------
 namespace {
 

@@ -47,6 +47,14 @@ struct KvView {
     __device__ __forceinline__ int page_of(int t) const { return page_magic ? (int)__umulhi((uint32_t)t, page_magic) : t; }      // t / tiles_per_page, exact for t, tiles_per_page < 2^16
 };
 
+// Who has which page, as iflow_kv_tables reads and writes it.
+struct KvTables {
+    const int32_t *new_tokens, *held, *free_state, *shared;   // new_tokens: not read where every sequence has one
+    int32_t *held_out, *free_out, *ring;
+    int64_t *slots;                                           // may be null
+    int32_t n_shared;
+};
+
 // One sequence's new tokens as the kernels take them: rows row .. row + count - 1 of the batch's tokens at positions position .. .  Whatever the arrays
 // hold, what comes out of here stays inside the call's buffers: count is at most max_tokens, and every token is asked for with has().  (In 32 bits: where numbers that no batch has
 // leave them, what has() sees is other numbers, and it still sees them.)

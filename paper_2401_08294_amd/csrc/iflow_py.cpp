@@ -32,7 +32,8 @@ decltype(&iflow_kv_append) p_kv_append;
 decltype(&iflow_kv_read) p_kv_read;
 decltype(&iflow_kv_attn) p_kv_attn;
 PyObject *s_data_ptr, *general;                                // general(name, arguments ...): the call that takes every form of argument
-PyTypeObject *cache_type, *batch_type;                         // the classes of iflow_kv_cache_t and iflow_kv_batch_t
+decltype(&iflow_kv_tables) p_kv_tables;
+PyTypeObject *cache_type, *batch_type, *pages_type;            // the classes of iflow_kv_cache_t, iflow_kv_batch_t and iflow_kv_pages_t
 
 // One call's arguments in order; the first that does not fit ends the reading (bad; perhaps a Python exception) and turns the rest into zeros.
 struct Args {
@@ -341,13 +342,27 @@ PyObject *kv_attn(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     return run(a, [&] { return p_kv_attn(&cache, &batch, q, heads, scale, out, workspace, (size_t)bytes, stream); });
 }
 
-// bind(addresses of the twelve functions, in this order)
+PyObject *kv_tables(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a("kv_tables", args, nargs, 8);
+    const iflow_kv_cache_t cache = a.description<iflow_kv_cache_t>(cache_type);
+    const iflow_kv_batch_t batch = a.description<iflow_kv_batch_t>(batch_type);
+    const iflow_kv_pages_t pages = a.description<iflow_kv_pages_t>(pages_type);
+    const int32_t *new_tokens = a.ptr<const int32_t>();
+    int64_t *slots = a.ptr<int64_t>();
+    void *workspace = a.ptr<void>();
+    const int64_t bytes = a.num();
+    void *stream = a.handle();
+    return run(a, [&] { return p_kv_tables(&cache, &batch, &pages, new_tokens, slots, workspace, (size_t)bytes, stream); });
+}
+
+// bind(addresses of the functions, in this order)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    Args a("bind", args, nargs, 12);
-    void *f[12];
+    void *f[13];
+    Args a("bind", args, nargs, sizeof f / sizeof f[0]);
     for (void *&p : f) p = a.handle();
-    if (a.bad) { PyErr_SetString(PyExc_TypeError, "twelve addresses are wanted"); return nullptr; }
+    if (a.bad) { PyErr_SetString(PyExc_TypeError, "an address for each function is wanted"); return nullptr; }
     p_quantize = reinterpret_cast<decltype(p_quantize)>(f[0]);
     p_dequant = reinterpret_cast<decltype(p_dequant)>(f[1]);
     p_qgemv = reinterpret_cast<decltype(p_qgemv)>(f[2]);
@@ -360,6 +375,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     p_kv_append = reinterpret_cast<decltype(p_kv_append)>(f[9]);
     p_kv_read = reinterpret_cast<decltype(p_kv_read)>(f[10]);
     p_kv_attn = reinterpret_cast<decltype(p_kv_attn)>(f[11]);
+    p_kv_tables = reinterpret_cast<decltype(p_kv_tables)>(f[12]);
     Py_RETURN_NONE;
 }
 
@@ -373,22 +389,25 @@ PyObject *otherwise(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     Py_RETURN_NONE;
 }
 
-// descriptions(class of iflow_kv_cache_t, class of iflow_kv_batch_t)
+// descriptions(class of iflow_kv_cache_t, class of iflow_kv_batch_t, class of iflow_kv_pages_t)
 PyObject *descriptions(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    if (nargs != 2 || !PyType_Check(args[0]) || !PyType_Check(args[1])) { PyErr_SetString(PyExc_TypeError, "two classes are wanted"); return nullptr; }
-    PyTypeObject *was[2] = {cache_type, batch_type};
-    cache_type = reinterpret_cast<PyTypeObject *>(Py_NewRef(args[0]));
-    batch_type = reinterpret_cast<PyTypeObject *>(Py_NewRef(args[1]));
-    Py_XDECREF(was[0]);
-    Py_XDECREF(was[1]);
+    PyTypeObject **to[3] = {&cache_type, &batch_type, &pages_type};
+    bool types = nargs == 3;
+    for (Py_ssize_t i = 0; types && i < 3; ++i) types = PyType_Check(args[i]);
+    if (!types) { PyErr_SetString(PyExc_TypeError, "three classes are wanted"); return nullptr; }
+    for (int i = 0; i < 3; ++i) {
+        PyTypeObject *was = *to[i];
+        *to[i] = reinterpret_cast<PyTypeObject *>(Py_NewRef(args[i]));
+        Py_XDECREF(was);
+    }
     Py_RETURN_NONE;
 }
 
 #define IFLOW_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {IFLOW_METHOD(bind), IFLOW_METHOD(otherwise), IFLOW_METHOD(quantize), IFLOW_METHOD(dequant), IFLOW_METHOD(qgemv), IFLOW_METHOD(qgemm),
                          IFLOW_METHOD(qgemv_fused), IFLOW_METHOD(qgemv_gated), IFLOW_METHOD(qgemm_fused), IFLOW_METHOD(attn_decode),
-                         IFLOW_METHOD(rope_append), IFLOW_METHOD(kv_append), IFLOW_METHOD(kv_read), IFLOW_METHOD(kv_attn), IFLOW_METHOD(descriptions), {nullptr, nullptr, 0, nullptr}};
+                         IFLOW_METHOD(rope_append), IFLOW_METHOD(kv_append), IFLOW_METHOD(kv_read), IFLOW_METHOD(kv_attn), IFLOW_METHOD(kv_tables), IFLOW_METHOD(descriptions), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -60,6 +60,12 @@ class KvBatch(C.Structure):
                 ("n_tokens", C.c_int64), ("max_tokens", C.c_int32), ("max_seq", C.c_int32)]
 
 
+class KvPages(C.Structure):
+    """iflow_kv_pages_t: who has which page of a cache."""
+    _fields_ = [("held", C.c_void_p), ("free_state", C.c_void_p), ("held_out", C.c_void_p), ("free_state_out", C.c_void_p), ("free_pages", C.c_void_p), ("shared_pages", C.c_void_p),
+                ("n_shared", C.c_int32)]
+
+
 class IflowError(RuntimeError):
     def __init__(self, status: int, what: str):
         self.status = status
@@ -70,7 +76,8 @@ _lib = None
 _native = None                 # the extension, bound to the library's functions (without one: the same calls through ctypes)
 # Enqueueing from Python, us, ctypes / here: a product with one vector 5.2 / 4.6, the attention's two launches 8.6 / 7.7, a decoder layer's six calls (seven
 # launches) 43 / 32 (on another host 4.4 / 3.7, 7.1 / 6.1, 35.0 / 24.6) - of which 2.3 and more a launch are the launch itself.
-_NATIVE_CALLS = ("quantize", "dequant", "qgemv", "qgemm", "qgemv_fused", "qgemv_gated", "qgemm_fused", "attn_decode", "rope_append", "kv_append", "kv_read", "kv_attn")
+_NATIVE_CALLS = ("quantize", "dequant", "qgemv", "qgemm", "qgemv_fused", "qgemv_gated", "qgemm_fused", "attn_decode", "rope_append", "kv_append", "kv_read", "kv_attn",
+                 "kv_tables")
 
 
 class ArgumentError(C.ArgumentError, TypeError):
@@ -139,6 +146,10 @@ class _Ctypes:
     def kv_attn(cache, batch, q, n_heads, scale, out, workspace, workspace_bytes, stream):
         return _lib.iflow_kv_attn(cache, batch, _ptr(q), n_heads, scale, _ptr(out), _ptr(workspace), workspace_bytes, stream)
 
+    @staticmethod
+    def kv_tables(cache, batch, pages, new_tokens, slots, workspace, workspace_bytes, stream):
+        return _lib.iflow_kv_tables(cache, batch, pages, _ptr(new_tokens), _ptr(slots), _ptr(workspace), workspace_bytes, stream)
+
 
 def _through_ctypes(name, *args):
     try:
@@ -201,6 +212,8 @@ def lib():
         L.iflow_kv_read.argtypes = [cache, batch, p, p, p]
         L.iflow_kv_attn_workspace_bytes.argtypes = [cache, batch, C.c_int, C.POINTER(sz)]
         L.iflow_kv_attn.argtypes = [cache, batch, p, C.c_int, C.c_float, p, p, sz, p]
+        L.iflow_kv_tables_workspace_bytes.argtypes = [cache, batch, C.POINTER(sz)]
+        L.iflow_kv_tables.argtypes = [cache, batch, C.POINTER(KvPages), p, p, p, sz, p]
         L.iflow_qgemv_chain_workspace_bytes.argtypes = [C.c_int, C.POINTER(i64), C.POINTER(sz)]
         L.iflow_qgemv_chain_plan_bytes.argtypes = [C.c_int, C.c_int, C.POINTER(sz)]
         L.iflow_qgemv_chain_plan.argtypes = [C.c_int, C.c_int, C.POINTER(C.c_int), C.POINTER(i64), C.POINTER(p), C.POINTER(p),
@@ -214,7 +227,7 @@ def lib():
         L.iflow_decode_stack_plan.argtypes = [C.POINTER(DecodeStack), p, sz, p, sz, p, C.POINTER(Chain)]
         L.iflow_decode_stack_launch.argtypes = [C.POINTER(Chain), i64, p]
         if native is not None:
-            native.descriptions(KvCache, KvBatch)
+            native.descriptions(KvCache, KvBatch, KvPages)
             native.bind(*[C.cast(getattr(L, "iflow_" + name), p).value for name in _NATIVE_CALLS])
             native.otherwise(_through_ctypes)
         else:
@@ -432,6 +445,28 @@ def kv_attn_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int) -> int
 def kv_attn(cache: KvCache, batch: KvBatch, q, n_heads: int, scale: float, out, workspace, workspace_bytes: int, stream=None) -> None:
     """Causal grouped-query attention of the batch's tokens, q [n_tokens][n_heads][head_dim], over their sequences' cached positions."""
     _check((_native or _calls()).kv_attn(cache, batch, q, n_heads, scale, out, workspace, workspace_bytes, _stream(stream)), "iflow_kv_attn")
+
+
+def kv_pages(free_pages, free_state, held, free_state_out=None, held_out=None, shared_pages=None, n_shared: int = 0) -> KvPages:
+    """Describes who has which page: int32 device tensors free_pages [n_pages] (a ring), free_state [3] = {first free, how many, -}, held [n_seqs], and the n_shared pages that every sequence's row
+    begins with.  Without free_state_out and held_out both are updated in place.  The description keeps the tensors."""
+    free_state_out = free_state if free_state_out is None else free_state_out
+    held_out = held if held_out is None else held_out
+    d = KvPages(_ptr(held), _ptr(free_state), _ptr(held_out), _ptr(free_state_out), _ptr(free_pages), _ptr(shared_pages), n_shared)
+    d._keep = (held, free_state, held_out, free_state_out, free_pages, shared_pages)
+    return d
+
+
+def kv_tables_workspace_bytes(cache: KvCache, batch: KvBatch) -> int:
+    out = C.c_size_t(0)
+    _check(lib().iflow_kv_tables_workspace_bytes(C.byref(cache), C.byref(batch), C.byref(out)), "iflow_kv_tables_workspace_bytes")
+    return int(out.value)
+
+
+def kv_tables(cache: KvCache, batch: KvBatch, pages: KvPages, new_tokens, slots, workspace, workspace_bytes: int, stream=None) -> None:
+    """Writes the batch's page_table and first_token from its seq_lens (as they are after the step) and new_tokens int32 [n_seqs], taking pages from and giving pages back to the ring of free
+    ones; slots int64 [n_tokens] (or None): where each token goes."""
+    _check((_native or _calls()).kv_tables(cache, batch, pages, new_tokens, slots, workspace, workspace_bytes, _stream(stream)), "iflow_kv_tables")
 
 
 def qgemv_chain_workspace_bytes(rows_list) -> int:
