@@ -370,6 +370,13 @@ iflow_status_t iflow_kv_attn_workspace_bytes(const iflow_kv_cache_t *cache, cons
 iflow_status_t iflow_kv_attn(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace,
                              size_t workspace_bytes, void *stream);
 
+/* iflow_kv_attn with a sliding window: token i of sequence b, at position p, sees position t <= p where t > p - window (the last `window`, its own among them) or t < sinks (the sequence's first, which
+ * stay visible).  window >= 1, sinks >= 0; what no token of the batch sees is not read, and may be on pages that are not there any more.  Everything else as for iflow_kv_attn; where window or sinks
+ * reaches max_seq it is iflow_kv_attn. */
+iflow_status_t iflow_kv_attn_window_workspace_bytes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, int n_heads, int window, int sinks, size_t *bytes);
+iflow_status_t iflow_kv_attn_window(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const uint16_t *q, int n_heads, int window, int sinks, float scale, uint16_t *out,
+                                    void *workspace, size_t workspace_bytes, void *stream);
+
 /* A step's page table, first tokens and slots, built on the device from the sequences' lengths: what a program that serves does before iflow_kv_append.  The batch is described as for the other
  * calls, with seq_lens as they will be after the step (0: a sequence that has ended, or none), and `new_tokens[b]` of these positions the step's own; page_table and first_token, which the other
  * calls read, are WRITTEN here.  (The cache gives n_pages and page_positions; its pages are not touched.)  With P = page_positions:

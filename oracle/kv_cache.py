@@ -142,8 +142,8 @@ def read(cache: Cache, table, lens, first, max_tokens: int, max_seq: int, k_out1
         k_out16[row], v_out16[row] = cache.load(table[b], position) if there else (0, 0)
 
 
-def attend(cache: Cache, table, lens, first, max_tokens: int, max_seq: int, q16, scale: float, out):
-    """out [n_tokens][n_heads][d] in fp64, rows of no token as they were."""
+def attend(cache: Cache, table, lens, first, max_tokens: int, max_seq: int, q16, scale: float, out, window=None, sinks: int = 0):
+    """out [n_tokens][n_heads][d] in fp64, rows of no token as they were.  With a window a token sees the last `window` positions up to its own, and the first `sinks`."""
     held = {}
     group = q16.shape[1] // cache.n_kv
     for b, row, position, _ in tokens(lens, first, q16.shape[0], max_tokens, max_seq):
@@ -154,6 +154,9 @@ def attend(cache: Cache, table, lens, first, max_tokens: int, max_seq: int, q16,
             there = np.array([cache.page(table[b], p) is not None for p in range(most)], bool)
             held[b] = [np.array([x[w] for x in kv], np.uint16).reshape(most, cache.n_kv, cache.d).view(np.float16).astype(np.float64) for w in (0, 1)] + [there]
         k, v, there = [x[:n] for x in held[b]]
+        if window is not None:
+            p = np.arange(n)
+            there = there & ((p >= n - window) | (p < sinks))
         out[row] = 0.0
         if not there.any():
             continue

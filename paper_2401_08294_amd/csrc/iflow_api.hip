@@ -458,13 +458,35 @@ iflow_status_t iflow_kv_read(const iflow_kv_cache_t *cache, const iflow_kv_batch
     return device_status(iflow::launch_kv_read((int)cache->format, cache->head_dim, v, k_out, v_out, (hipStream_t)stream));
 }
 
+// the sizes of an attention's description
+static iflow_status_t kv_attn_shapes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, int n_heads, iflow::KvView *v)
+{
+    const iflow_status_t st = kv_shapes(cache, batch, true, n_heads, v);
+    if (st != IFLOW_OK) return st;
+    return (int64_t)v->max_tokens * (n_heads / v->n_kv_heads) > (1 << 22) ? IFLOW_ERR_SHAPE : IFLOW_OK;
+}
+// ... its scale
+static bool kv_attn_scale(float scale) { return scale > 0.0f && scale < 2.0e38f; }      // (times log2 e it is a number too)
+// ... and its arrays
+static iflow_status_t kv_attn_arrays(const iflow::KvView &v, int head_dim, const uint16_t *q, int n_heads, const uint16_t *out, const void *workspace, size_t workspace_bytes, size_t need)
+{
+    if (!q || !out || (need && !workspace)) return IFLOW_ERR_NULL;
+    const iflow_status_t st = kv_pointers(v);
+    if (st != IFLOW_OK) return st;
+    if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return IFLOW_ERR_ALIGN;
+    if (workspace_bytes < need) return IFLOW_ERR_SIZE;
+    const int64_t bytes = v.n_tokens * n_heads * head_dim * 2;
+    if (overlaps(out, bytes, q, bytes) || overlaps_pages(v, out, bytes) || overlaps_arrays(v, out, bytes) || (need && overlaps_arrays(v, workspace, (int64_t)need))) return IFLOW_ERR_SHAPE;
+    if (need && (overlaps(workspace, (int64_t)need, q, bytes) || overlaps(workspace, (int64_t)need, out, bytes) || overlaps_pages(v, workspace, (int64_t)need))) return IFLOW_ERR_SHAPE;
+    return IFLOW_OK;
+}
+
 iflow_status_t iflow_kv_attn_workspace_bytes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, int n_heads, size_t *bytes)
 {
     iflow::KvView v;
     if (!bytes) return IFLOW_ERR_NULL;
-    const iflow_status_t st = kv_shapes(cache, batch, true, n_heads, &v);
+    const iflow_status_t st = kv_attn_shapes(cache, batch, n_heads, &v);
     if (st != IFLOW_OK) return st;
-    if ((int64_t)v.max_tokens * (n_heads / v.n_kv_heads) > (1 << 22)) return IFLOW_ERR_SHAPE;
     *bytes = iflow::kv_attn_workspace_bytes(v, cache->head_dim, n_heads);
     return IFLOW_OK;
 }
@@ -473,20 +495,35 @@ iflow_status_t iflow_kv_attn(const iflow_kv_cache_t *cache, const iflow_kv_batch
                              size_t workspace_bytes, void *stream)
 {
     iflow::KvView v;
-    iflow_status_t st = kv_shapes(cache, batch, true, n_heads, &v);
+    iflow_status_t st = kv_attn_shapes(cache, batch, n_heads, &v);
     if (st != IFLOW_OK) return st;
-    if (!(scale > 0.0f && scale < 2.0e38f)) return IFLOW_ERR_SHAPE;      // (times log2 e it is a number too)
-    if ((int64_t)v.max_tokens * (n_heads / v.n_kv_heads) > (1 << 22)) return IFLOW_ERR_SHAPE;
-    const size_t need = iflow::kv_attn_workspace_bytes(v, cache->head_dim, n_heads);
-    if (!q || !out || (need && !workspace)) return IFLOW_ERR_NULL;
-    st = kv_pointers(v);
+    if (!kv_attn_scale(scale)) return IFLOW_ERR_SHAPE;
+    st = kv_attn_arrays(v, cache->head_dim, q, n_heads, out, workspace, workspace_bytes, iflow::kv_attn_workspace_bytes(v, cache->head_dim, n_heads));
     if (st != IFLOW_OK) return st;
-    if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return IFLOW_ERR_ALIGN;
-    if (workspace_bytes < need) return IFLOW_ERR_SIZE;
-    const int64_t bytes = v.n_tokens * n_heads * cache->head_dim * 2;
-    if (overlaps(out, bytes, q, bytes) || overlaps_pages(v, out, bytes) || overlaps_arrays(v, out, bytes) || (need && overlaps_arrays(v, workspace, (int64_t)need))) return IFLOW_ERR_SHAPE;
-    if (need && (overlaps(workspace, (int64_t)need, q, bytes) || overlaps(workspace, (int64_t)need, out, bytes) || overlaps_pages(v, workspace, (int64_t)need))) return IFLOW_ERR_SHAPE;
     return device_status(iflow::launch_kv_attn((int)cache->format, cache->head_dim, v, q, n_heads, scale, out, workspace, (hipStream_t)stream));
+}
+
+iflow_status_t iflow_kv_attn_window_workspace_bytes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, int n_heads, int window, int sinks, size_t *bytes)
+{
+    iflow::KvView v;
+    if (!bytes) return IFLOW_ERR_NULL;
+    const iflow_status_t st = kv_attn_shapes(cache, batch, n_heads, &v);
+    if (st != IFLOW_OK) return st;
+    if (window < 1 || sinks < 0) return IFLOW_ERR_SHAPE;
+    *bytes = iflow::kv_attn_window_workspace_bytes(v, cache->head_dim, n_heads, window, sinks);
+    return IFLOW_OK;
+}
+
+iflow_status_t iflow_kv_attn_window(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const uint16_t *q, int n_heads, int window, int sinks, float scale, uint16_t *out,
+                                    void *workspace, size_t workspace_bytes, void *stream)
+{
+    iflow::KvView v;
+    iflow_status_t st = kv_attn_shapes(cache, batch, n_heads, &v);
+    if (st != IFLOW_OK) return st;
+    if (window < 1 || sinks < 0 || !kv_attn_scale(scale)) return IFLOW_ERR_SHAPE;
+    st = kv_attn_arrays(v, cache->head_dim, q, n_heads, out, workspace, workspace_bytes, iflow::kv_attn_window_workspace_bytes(v, cache->head_dim, n_heads, window, sinks));
+    if (st != IFLOW_OK) return st;
+    return device_status(iflow::launch_kv_attn_window((int)cache->format, cache->head_dim, v, q, n_heads, window, sinks, scale, out, workspace, (hipStream_t)stream));
 }
 
 // the sizes of a call that builds a batch's tables, without their pointers (the cache's pages are not touched)

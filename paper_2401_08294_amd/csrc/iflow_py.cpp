@@ -31,8 +31,9 @@ decltype(&iflow_rope_append) p_rope_append;
 decltype(&iflow_kv_append) p_kv_append;
 decltype(&iflow_kv_read) p_kv_read;
 decltype(&iflow_kv_attn) p_kv_attn;
-PyObject *s_data_ptr, *general;                                // general(name, arguments ...): the call that takes every form of argument
 decltype(&iflow_kv_tables) p_kv_tables;
+decltype(&iflow_kv_attn_window) p_kv_attn_window;
+PyObject *s_data_ptr, *general;                                // general(name, arguments ...): the call that takes every form of argument
 PyTypeObject *cache_type, *batch_type, *pages_type;            // the classes of iflow_kv_cache_t, iflow_kv_batch_t and iflow_kv_pages_t
 
 // One call's arguments in order; the first that does not fit ends the reading (bad; perhaps a Python exception) and turns the rest into zeros.
@@ -356,10 +357,25 @@ PyObject *kv_tables(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     return run(a, [&] { return p_kv_tables(&cache, &batch, &pages, new_tokens, slots, workspace, (size_t)bytes, stream); });
 }
 
+PyObject *kv_attn_window(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a("kv_attn_window", args, nargs, 11);
+    const iflow_kv_cache_t cache = a.description<iflow_kv_cache_t>(cache_type);
+    const iflow_kv_batch_t batch = a.description<iflow_kv_batch_t>(batch_type);
+    const uint16_t *q = a.ptr<const uint16_t>();
+    const int heads = a.word(), window = a.word(), sinks = a.word();
+    const float scale = a.real();
+    uint16_t *out = a.ptr<uint16_t>();
+    void *workspace = a.ptr<void>();
+    const int64_t bytes = a.num();
+    void *stream = a.handle();
+    return run(a, [&] { return p_kv_attn_window(&cache, &batch, q, heads, window, sinks, scale, out, workspace, (size_t)bytes, stream); });
+}
+
 // bind(addresses of the functions, in this order)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    void *f[13];
+    void *f[14];
     Args a("bind", args, nargs, sizeof f / sizeof f[0]);
     for (void *&p : f) p = a.handle();
     if (a.bad) { PyErr_SetString(PyExc_TypeError, "an address for each function is wanted"); return nullptr; }
@@ -376,6 +392,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     p_kv_read = reinterpret_cast<decltype(p_kv_read)>(f[10]);
     p_kv_attn = reinterpret_cast<decltype(p_kv_attn)>(f[11]);
     p_kv_tables = reinterpret_cast<decltype(p_kv_tables)>(f[12]);
+    p_kv_attn_window = reinterpret_cast<decltype(p_kv_attn_window)>(f[13]);
     Py_RETURN_NONE;
 }
 
@@ -407,7 +424,7 @@ PyObject *descriptions(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 #define IFLOW_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {IFLOW_METHOD(bind), IFLOW_METHOD(otherwise), IFLOW_METHOD(quantize), IFLOW_METHOD(dequant), IFLOW_METHOD(qgemv), IFLOW_METHOD(qgemm),
                          IFLOW_METHOD(qgemv_fused), IFLOW_METHOD(qgemv_gated), IFLOW_METHOD(qgemm_fused), IFLOW_METHOD(attn_decode),
-                         IFLOW_METHOD(rope_append), IFLOW_METHOD(kv_append), IFLOW_METHOD(kv_read), IFLOW_METHOD(kv_attn), IFLOW_METHOD(kv_tables), IFLOW_METHOD(descriptions), {nullptr, nullptr, 0, nullptr}};
+                         IFLOW_METHOD(rope_append), IFLOW_METHOD(kv_append), IFLOW_METHOD(kv_read), IFLOW_METHOD(kv_attn), IFLOW_METHOD(kv_tables), IFLOW_METHOD(kv_attn_window), IFLOW_METHOD(descriptions), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -77,7 +77,7 @@ _native = None                 # the extension, bound to the library's functions
 # Enqueueing from Python, us, ctypes / here: a product with one vector 5.2 / 4.6, the attention's two launches 8.6 / 7.7, a decoder layer's six calls (seven
 # launches) 43 / 32 (on another host 4.4 / 3.7, 7.1 / 6.1, 35.0 / 24.6) - of which 2.3 and more a launch are the launch itself.
 _NATIVE_CALLS = ("quantize", "dequant", "qgemv", "qgemm", "qgemv_fused", "qgemv_gated", "qgemm_fused", "attn_decode", "rope_append", "kv_append", "kv_read", "kv_attn",
-                 "kv_tables")
+                 "kv_tables", "kv_attn_window")
 
 
 class ArgumentError(C.ArgumentError, TypeError):
@@ -150,6 +150,10 @@ class _Ctypes:
     def kv_tables(cache, batch, pages, new_tokens, slots, workspace, workspace_bytes, stream):
         return _lib.iflow_kv_tables(cache, batch, pages, _ptr(new_tokens), _ptr(slots), _ptr(workspace), workspace_bytes, stream)
 
+    @staticmethod
+    def kv_attn_window(cache, batch, q, n_heads, window, sinks, scale, out, workspace, workspace_bytes, stream):
+        return _lib.iflow_kv_attn_window(cache, batch, _ptr(q), n_heads, window, sinks, scale, _ptr(out), _ptr(workspace), workspace_bytes, stream)
+
 
 def _through_ctypes(name, *args):
     try:
@@ -212,6 +216,8 @@ def lib():
         L.iflow_kv_read.argtypes = [cache, batch, p, p, p]
         L.iflow_kv_attn_workspace_bytes.argtypes = [cache, batch, C.c_int, C.POINTER(sz)]
         L.iflow_kv_attn.argtypes = [cache, batch, p, C.c_int, C.c_float, p, p, sz, p]
+        L.iflow_kv_attn_window_workspace_bytes.argtypes = [cache, batch, C.c_int, C.c_int, C.c_int, C.POINTER(sz)]
+        L.iflow_kv_attn_window.argtypes = [cache, batch, p, C.c_int, C.c_int, C.c_int, C.c_float, p, p, sz, p]
         L.iflow_kv_tables_workspace_bytes.argtypes = [cache, batch, C.POINTER(sz)]
         L.iflow_kv_tables.argtypes = [cache, batch, C.POINTER(KvPages), p, p, p, sz, p]
         L.iflow_qgemv_chain_workspace_bytes.argtypes = [C.c_int, C.POINTER(i64), C.POINTER(sz)]
@@ -445,6 +451,17 @@ def kv_attn_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int) -> int
 def kv_attn(cache: KvCache, batch: KvBatch, q, n_heads: int, scale: float, out, workspace, workspace_bytes: int, stream=None) -> None:
     """Causal grouped-query attention of the batch's tokens, q [n_tokens][n_heads][head_dim], over their sequences' cached positions."""
     _check((_native or _calls()).kv_attn(cache, batch, q, n_heads, scale, out, workspace, workspace_bytes, _stream(stream)), "iflow_kv_attn")
+
+
+def kv_attn_window_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int, window: int, sinks: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().iflow_kv_attn_window_workspace_bytes(C.byref(cache), C.byref(batch), n_heads, window, sinks, C.byref(out)), "iflow_kv_attn_window_workspace_bytes")
+    return int(out.value)
+
+
+def kv_attn_window(cache: KvCache, batch: KvBatch, q, n_heads: int, window: int, sinks: int, scale: float, out, workspace, workspace_bytes: int, stream=None) -> None:
+    """kv_attn where a token sees the last `window` positions, its own among them, and its sequence's first `sinks`."""
+    _check((_native or _calls()).kv_attn_window(cache, batch, q, n_heads, window, sinks, scale, out, workspace, workspace_bytes, _stream(stream)), "iflow_kv_attn_window")
 
 
 def kv_pages(free_pages, free_state, held, free_state_out=None, held_out=None, shared_pages=None, n_shared: int = 0) -> KvPages:
