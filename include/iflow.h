@@ -377,6 +377,16 @@ iflow_status_t iflow_kv_attn_window_workspace_bytes(const iflow_kv_cache_t *cach
 iflow_status_t iflow_kv_attn_window(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const uint16_t *q, int n_heads, int window, int sinks, float scale, uint16_t *out,
                                     void *workspace, size_t workspace_bytes, void *stream);
 
+/* iflow_kv_attn for a batch whose sequences begin with the same positions (an instruction, a document), in the same pages: these are read once for the tokens of all sequences, not once for each.
+ *   shared_pages [max_shared / page_positions], device int32: the prefix's pages.  shared_len, device int32: how many positions it has, read when the kernels run, at most max_shared; only whole pages
+ *   count, what is left over of a page is read as every sequence's own.  0 <= max_shared <= max_seq.
+ * Every sequence that has tokens in the call has these pages in its row of page_table (which must not be null), entries 0 .. shared_len / page_positions - 1: where a row has others it is unspecified
+ * which of the two a token sees.  (iflow_kv_tables writes such rows.)  A token at a position inside the prefix sees it up to its own position.
+ * Everything else, the result among it, as for iflow_kv_attn: the sums of the prefix and of what is behind it are taken apart, in fp32, and added. */
+iflow_status_t iflow_kv_attn_shared_workspace_bytes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, int n_heads, int max_shared, size_t *bytes);
+iflow_status_t iflow_kv_attn_shared(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const int32_t *shared_pages, const int32_t *shared_len, int max_shared, const uint16_t *q, int n_heads,
+                                    float scale, uint16_t *out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* A step's page table, first tokens and slots, built on the device from the sequences' lengths: what a program that serves does before iflow_kv_append.  The batch is described as for the other
  * calls, with seq_lens as they will be after the step (0: a sequence that has ended, or none), and `new_tokens[b]` of these positions the step's own; page_table and first_token, which the other
  * calls read, are WRITTEN here.  (The cache gives n_pages and page_positions; its pages are not touched.)  With P = page_positions:

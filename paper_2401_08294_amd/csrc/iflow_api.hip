@@ -526,6 +526,36 @@ iflow_status_t iflow_kv_attn_window(const iflow_kv_cache_t *cache, const iflow_k
     return device_status(iflow::launch_kv_attn_window((int)cache->format, cache->head_dim, v, q, n_heads, window, sinks, scale, out, workspace, (hipStream_t)stream));
 }
 
+iflow_status_t iflow_kv_attn_shared_workspace_bytes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, int n_heads, int max_shared, size_t *bytes)
+{
+    iflow::KvView v;
+    if (!bytes) return IFLOW_ERR_NULL;
+    const iflow_status_t st = kv_attn_shapes(cache, batch, n_heads, &v);
+    if (st != IFLOW_OK) return st;
+    if (max_shared < 0 || max_shared > v.max_seq) return IFLOW_ERR_SHAPE;
+    *bytes = iflow::kv_attn_shared_workspace_bytes(v, cache->head_dim, n_heads, max_shared);
+    return IFLOW_OK;
+}
+
+iflow_status_t iflow_kv_attn_shared(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const int32_t *shared_pages, const int32_t *shared_len, int max_shared, const uint16_t *q, int n_heads,
+                                    float scale, uint16_t *out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    iflow::KvView v;
+    iflow_status_t st = kv_attn_shapes(cache, batch, n_heads, &v);
+    if (st != IFLOW_OK) return st;
+    if (max_shared < 0 || max_shared > v.max_seq || !kv_attn_scale(scale)) return IFLOW_ERR_SHAPE;
+    const size_t need = iflow::kv_attn_shared_workspace_bytes(v, cache->head_dim, n_heads, max_shared);
+    const int64_t n_shared = max_shared / cache->page_positions;
+    if (!v.table || !shared_len || (n_shared > 0 && !shared_pages)) return IFLOW_ERR_NULL;
+    if (((reinterpret_cast<uintptr_t>(shared_pages) | reinterpret_cast<uintptr_t>(shared_len)) & 3) != 0) return IFLOW_ERR_ALIGN;
+    st = kv_attn_arrays(v, cache->head_dim, q, n_heads, out, workspace, workspace_bytes, need);
+    if (st != IFLOW_OK) return st;
+    const int64_t bytes = v.n_tokens * n_heads * cache->head_dim * 2;
+    if (overlaps(out, bytes, shared_len, 4) || (n_shared > 0 && overlaps(out, bytes, shared_pages, 4 * n_shared))) return IFLOW_ERR_SHAPE;
+    if (need && (overlaps(workspace, (int64_t)need, shared_len, 4) || (n_shared > 0 && overlaps(workspace, (int64_t)need, shared_pages, 4 * n_shared)))) return IFLOW_ERR_SHAPE;
+    return device_status(iflow::launch_kv_attn_shared((int)cache->format, cache->head_dim, v, shared_pages, shared_len, max_shared, q, n_heads, scale, out, workspace, (hipStream_t)stream));
+}
+
 // the sizes of a call that builds a batch's tables, without their pointers (the cache's pages are not touched)
 static iflow_status_t kv_tables_shapes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, iflow::KvView *v)
 {

@@ -241,6 +241,10 @@ size_t kv_attn_workspace_bytes(const KvView &v, int head_dim, int n_heads);
 hipError_t launch_kv_attn(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace, hipStream_t s);
 size_t kv_attn_window_workspace_bytes(const KvView &v, int head_dim, int n_heads, int window, int sinks);
 hipError_t launch_kv_attn_window(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, int window, int sinks, float scale, uint16_t *out, void *workspace, hipStream_t s);
+hipError_t launch_kv_attn_blocks(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale, uint16_t *out, int rows, int few, hipStream_t s);
+size_t kv_attn_shared_workspace_bytes(const KvView &v, int head_dim, int n_heads, int max_shared);
+hipError_t launch_kv_attn_shared(int format, int head_dim, const KvView &v, const int32_t *pages, const int32_t *len, int max_shared, const uint16_t *q, int n_heads, float scale, uint16_t *out,
+                                 void *workspace, hipStream_t s);
 size_t kv_tables_workspace_bytes(const KvView &v);
 hipError_t launch_kv_tables(const KvView &v, const KvTables &t, void *workspace, hipStream_t s);
 // ---- the chained launch: description of a chain (host arrays of the caller), plan builder, model, launcher ----

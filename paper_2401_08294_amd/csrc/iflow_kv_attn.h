@@ -65,14 +65,16 @@ struct KvSpan { int front, skip, tiles; };
 // those of any sixteen rows of a sequence, or more.
 //   MAPPED   tiles are not 0, 1, ..: where() says which one is the t-th
 //   LOW      a token does not see every position below its own: hidden(p, limit) for one that sees none from `limit` on
+//   PREFIX   the first positions, which the sequences share, for tokens of all of them
+//   TAIL     what lies behind these, and the sum of both
 struct KvSeesAll {
-    static constexpr bool MAPPED = false, LOW = false;
+    static constexpr bool MAPPED = false, LOW = false, PREFIX = false, TAIL = false;
     __device__ __forceinline__ KvSpan span(int, int longest) const { return {0, 0, (longest + KV_TILE - 1) / KV_TILE}; }
     __device__ __forceinline__ int line_tiles(const KvSequence &seq, int) const { return (seq.sees(seq.count - 1) + KV_TILE - 1) / KV_TILE; }
 };
 // the last `window` positions, its own among them, and the first `sinks`
 struct KvSeesWindow {
-    static constexpr bool MAPPED = true, LOW = true;
+    static constexpr bool MAPPED = true, LOW = true, PREFIX = false, TAIL = false;
     int window, sinks;
     __device__ __forceinline__ KvSpan span(int shortest, int longest) const
     {
@@ -89,6 +91,44 @@ struct KvSeesWindow {
     __device__ __forceinline__ bool hidden(int p, int limit) const { return p < limit - window && p >= sinks; }
     // of tokens whose limits are at most `longest`: some position of tile p0 / 32 may be hidden
     __device__ __forceinline__ bool hides(int p0, int longest) const { return p0 < longest - window && p0 + KV_TILE > sinks; }
+};
+// A prefix that sequences share: its whole pages' positions, and what the rows of all tokens' queries [token][head] have of it: in so many parts their references, sums and values, [part][row].
+struct KvShared {
+    const int32_t *pages, *len;
+    float *m, *l, *o;
+    int64_t rows;
+    int max_len, parts;
+    __device__ __forceinline__ int tiles(const KvView &v) const { return v.page_of(max(0, min(len[0], max_len)) / KV_TILE) * v.tiles_per_page; }
+};
+struct KvSeesPrefix : KvShared {
+    static constexpr bool MAPPED = true, LOW = false, PREFIX = true, TAIL = false;
+    int few;                                                  // sequences of as many rows are served otherwise
+};
+struct KvSeesTail : KvShared {
+    static constexpr bool MAPPED = true, LOW = false, PREFIX = false, TAIL = true;
+    int d_of;                                                 // components of a row
+    int start;                                                // tiles of the prefix: the kernel asks for them first
+    __device__ __forceinline__ KvSpan span(int, int longest) const { return {0, start, max(0, (longest + KV_TILE - 1) / KV_TILE - start)}; }
+    __device__ __forceinline__ int line_tiles(const KvSequence &seq, int) const { return max(0, (seq.sees(seq.count - 1) + KV_TILE - 1) / KV_TILE - start); }
+    // n of a row's values, relative to `base` (-inf: there are none), and the prefix's, relative to what comes back
+    template <int N> __device__ __forceinline__ void add(int64_t row, int d, float base, float &sum, float (&values)[N]) const
+    {
+        float top = base;
+        for (int c = 0; c < parts; ++c) top = fmaxf(top, m[c * rows + row]);
+        const float f0 = base == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base - top);
+        sum *= f0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) values[e] *= f0;
+        for (int c = 0; c < parts; ++c) {
+            const int64_t at = c * rows + row;
+            const float mc = m[at];
+            if (mc == -INFINITY) continue;                    // (nothing is written of a part that a row sees nothing of)
+            const float f = __builtin_amdgcn_exp2f(mc - top);
+            sum = __builtin_fmaf(l[at], f, sum);
+#pragma unroll
+            for (int e = 0; e < N; ++e) values[e] = __builtin_fmaf(o[at * d_of + d + e], f, values[e]);
+        }
+    }
 };
 template <typename SEES> __device__ __forceinline__ int kv_where(const KvSpan &span, int t)
 {
@@ -154,6 +194,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const KvPartial part(ws, v.n_seqs);
+    if constexpr (SEES::TAIL) sees.start = sees.tiles(v);
 
     const int lane = tid & 63, li = lane & 15, g = lane >> 4;
     // which sequence, which line and part of it, and where the sequence's partial results begin
@@ -432,6 +473,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
             }
             if (parts == 1) {
                 if (r < rows && seq.has_row(tok)) {
+                    if constexpr (SEES::TAIL) {
+                        float with[4] = {O[0], O[1], O[2], O[3]};
+                        sees.add((int64_t)(seq.row + tok) * n_heads + head * group + (r0 + r - tok * group), d, M == -INFINITY ? M : to_base, L, with);
+                        O = (kv_float4){with[0], with[1], with[2], with[3]};
+                    }
                     const float div = L > 0.f ? L : 1.f;      // (nothing seen: zeros)
                     const half2_t a = {(half_t)(O[0] / div), (half_t)(O[1] / div)}, c = {(half_t)(O[2] / div), (half_t)(O[3] / div)};
                     const int64_t to = (int64_t)(seq.row + tok) * n_heads + head * group + (r0 + r - tok * group);
@@ -449,7 +495,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
 // at once, and the groups' states meet in LDS and are added in order.
 constexpr int KVA_MERGE = 8;
 template <typename SEES>
-__device__ __forceinline__ void kv_attn_merge(const KvView &v, int b, int i, int h, int n_heads, int group, int few, void *ws, uint16_t *__restrict__ out, const SEES &sees)
+__device__ __forceinline__ void kv_attn_merge(const KvView &v, int b, int i, int h, int n_heads, int group, int few, void *ws, uint16_t *__restrict__ out, SEES sees)
 {
     __shared__ float s_o[8][128], s_m[8], s_l[8];
     const int D = blockDim.x, d = threadIdx.x, groups = blockDim.y, u = threadIdx.y;
@@ -457,6 +503,7 @@ __device__ __forceinline__ void kv_attn_merge(const KvView &v, int b, int i, int
     const int before = part.before[b], share = part.before[v.n_seqs];
     const KvSequence seq(v, b);
     if (!seq.has_row(i)) return;
+    if constexpr (SEES::TAIL) sees.start = sees.tiles(v);
     const KvLines x = kv_lines_of(v, seq, group, few, sees);
     if (x.lines == 0) return;
     const int row = i * group + h % group, piece = row / KVA_ROWS, r = row % KVA_ROWS, line = piece * v.n_kv_heads + h / group;
@@ -497,6 +544,11 @@ __device__ __forceinline__ void kv_attn_merge(const KvView &v, int b, int i, int
             O = __builtin_fmaf(s_o[e][d], f, O);
         }
     }
+    if constexpr (SEES::TAIL) {
+        float with[1] = {O};
+        sees.add((int64_t)(seq.row + i) * n_heads + h, d, M == -INFINITY ? M : to_base(M), L, with);
+        O = with[0];
+    }
     out[((int64_t)(seq.row + i) * n_heads + h) * D + d] = as_u16((half_t)(L > 0.f ? O / L : 0.f));
 }
 // Token y of sequence z for head x; packed (one z): the x-th, the x + grid-th, .. token of the sequences that sixteens serve, for head y.
@@ -516,11 +568,39 @@ __global__ __launch_bounds__(1024) void kv_attn_merge_kernel(KvView v, int n_hea
 //   S[position][row] = K Q^T with the queries in registers; a lane has one row's scores, sixteen of every 32 positions, and its half of the row's maximum and sum;
 //   O[component][row] = V^T P^T: element e of a tile's scores is position 4g + e % 4 or 16 + 4g + e % 4 of g = 2 (e / 8) + h where row i of S is position i with bits 3 and 4 changed
 //   over, so a lane's probabilities are its own operand, and a value's eight positions are a word of the cache's.  The sums' factors are the lane's own too.
+// PREFIX: the rows are those of all sequences' tokens, one after another, the positions a part (blockIdx.z) of the shared ones.  A token's sequence is looked for among the first tokens; sequences that
+// are served otherwise (of `few` rows and more) have no rows here.
 // Keys in LDS: [tile][component / 8][i: 32][8 components], values: [tile][g][component][8 positions]: 16-byte pieces that 32 lanes read side by side.
 // PG groups of wavefronts take every PG-th 64 positions and add up in LDS: where there are too few rows to fill the device.  The probabilities are two fp16 numbers each, and two products of every value,
 // as in kv_attn_kernel: a token's output does not depend on how many rows its batch has but for the order of fp32 sums.  (Rounded to fp16 once, with one product, they made the largest error 1.4e-3 of a
 // row's rms where the output's own rounding is 4.9e-4, and prompts of 2500 tokens, 64/8 heads, took 284 us for the 352 now; 512 tokens behind 3888, 32/8 heads, 60 for 71.)
 typedef float kv_float16 __attribute__((ext_vector_type(16)));
+
+// PREFIX: all rows of the call, of which each sees all of the part
+struct KvCallRows {
+    static constexpr int row = 0;
+    int count, part;
+    __device__ __forceinline__ bool has_row(int i) const { return (uint32_t)i < (uint32_t)count; }
+    __device__ __forceinline__ int sees(int) const { return part; }
+};
+// whether a row of the call's arrays is a token's that sixteens serve, and what it sees
+struct KvToken { bool real; int limit; };
+__device__ __forceinline__ KvToken kv_token(const KvView &v, int row, int group, int few)
+{
+    int b = row;
+    if (v.first) {                                            // the last sequence that begins at or in front of the row
+        b = 0;
+        for (int n = v.n_seqs; n > 1;) {
+            const int half = n >> 1;
+            if (v.first[b + half] <= row) b += half;
+            n -= half;
+        }
+    }
+    if (b >= v.n_seqs) return {false, 0};
+    const KvSequence seq(v, b);
+    const int i = (int)((uint32_t)row - (uint32_t)seq.row);
+    return {seq.has_row(i) && (int64_t)seq.count * group < few, seq.sees(i)};
+}
 
 template <typename T, int RG, int PG, int STAGES, typename SEES>
 __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_rows_kernel(KvView v, const uint16_t *__restrict__ q, int n_heads, int group, int few, KvDivide by_group, float scale_log2e,
@@ -551,23 +631,45 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     KvSpan span = {};
     auto find_tiles = [&](int t0) {
         const int t = kv_where<SEES>(span, t0 + lane);
+        if constexpr (SEES::PREFIX) {
+            const int p = v.page_of(t);
+            my_tile = t0 + lane < span.tiles ? reinterpret_cast<uint64_t>(kv_tile_in(v, sees.pages[p], head, t - p * v.tiles_per_page, T::BYTES)) : 0;
+            return;
+        }
         my_tile = t * KV_TILE < v.max_seq ? reinterpret_cast<uint64_t>(kv_tile_at(v, b, head, t, T::BYTES)) : 0;
     };
     if constexpr (!SEES::MAPPED) find_tiles(0);
-    const KvSequence seq(v, b);
+    const auto seq = [&] {
+        if constexpr (SEES::PREFIX) {
+            const int all = sees.tiles(v), per = ((all + sees.parts - 1) / sees.parts + 1) & ~1, from = min(all, per * b);
+            span = {0, from, min(per, all - from)};
+            return KvCallRows{(int)v.n_tokens, (from + span.tiles) * KV_TILE};
+        } else {
+            return KvSequence(v, b);
+        }
+    }();
     const int n_rows = seq.count * group;
     const int r0 = ((few > 0 ? (n_rows + ROWS - 1) / ROWS : (int)gridDim.y) - 1 - block) * ROWS;      // (the last rows, which see most, first)
     if (r0 >= n_rows) return;
     // (the same for the wavefront, as the compiler is told: what it takes for different in the lanes costs a loop around every load)
     auto same = [](int n) { return __builtin_amdgcn_readfirstlane(n); };
     const int longest = same(seq.sees(by_group(min(n_rows, r0 + ROWS) - 1)));
-    const int my_row = min(n_rows - 1, r0 + rg * 32 + li), token = by_group(my_row), limit = seq.sees(token);
-    const bool real = r0 + rg * 32 + li < n_rows && seq.has_row(token);
+    const int my_row = min(n_rows - 1, r0 + rg * 32 + li), token = by_group(my_row);
+    KvToken found = {true, 0};
+    if constexpr (SEES::PREFIX) found = kv_token(v, token, group, sees.few);
+    const bool real = r0 + rg * 32 + li < n_rows && seq.has_row(token) && found.real;
+    const int limit = SEES::PREFIX && real ? min(found.limit, longest) : seq.sees(token);
     const int64_t my_out = ((int64_t)(seq.row + token) * n_heads + head * group + (my_row - token * group)) * D;
     // of the wavefront's rows: what the first sees, and the last
-    const int shortest = same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32)))), limit_of_wave = same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32 + 31))));
+    const int shortest = SEES::PREFIX ? (__builtin_amdgcn_ballot_w64(limit < longest) == 0 ? longest : 0) : same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32)))), limit_of_wave = same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32 + 31))));
     const int first_limit = same(seq.sees(by_group(r0)));     // of the workgroup's rows: what the first sees
-    span = sees.span(first_limit, longest);
+    __shared__ int s_row[SEES::PREFIX ? ROWS : 1];            // PREFIX: the rows' numbers among all tokens' queries; -1: none
+    if constexpr (SEES::PREFIX) {
+        if (pg == 0 && hf == 0) s_row[rg * 32 + li] = real ? (int)(my_out / D) : -1;
+        if (!__syncthreads_or(real)) return;
+    } else {
+        span = sees.span(first_limit, longest);
+    }
     if constexpr (SEES::MAPPED) {
         span = {same(span.front), same(span.skip), same(span.tiles)};
         find_tiles(0);
@@ -717,7 +819,9 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
 #pragma unroll
             for (int tl = 0; tl < 2; ++tl) {
                 const int p0 = kv_where<SEES>(span, t0 + tl) * KV_TILE;
-                const bool there = tl ? there1 : there0, low = SEES::LOW && sees.hides(p0, limit_of_wave);
+                const bool there = tl ? there1 : there0;
+                bool low = false;
+                if constexpr (SEES::LOW) low = sees.hides(p0, limit_of_wave);
                 if (there && p0 + KV_TILE <= shortest && !low) continue;
                 int from = p0 + 4 * hf;
                 asm volatile("" : "+v"(from));                // (else the compiler keeps 16 positions in registers through the steps)
@@ -905,7 +1009,16 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
 
     // element 4 y + e of oacc[c] is component 32 c + 8 y + 4 hf + e of row li
     l += __shfl_xor(l, 32);
-    if constexpr (PG == 1) {
+    if constexpr (PG == 1 && SEES::PREFIX) {
+        if (!real) return;
+        const int64_t to = b * sees.rows + my_out / D;
+        if (hf == 0) { sees.m[to] = m; sees.l[to] = l; }
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                *reinterpret_cast<kv_float4 *>(sees.o + to * D + 32 * c + 8 * y + 4 * hf) = (kv_float4){oacc[c][4 * y], oacc[c][4 * y + 1], oacc[c][4 * y + 2], oacc[c][4 * y + 3]};
+    } else if constexpr (PG == 1) {
         if (!real) return;
         const float f = l > 0.f ? 1.f / l : 0.f;              // (nothing seen: zeros; 64 divisions would take as long as two steps)
 #pragma unroll
@@ -941,6 +1054,13 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
                 L = __builtin_fmaf(s_l[w][r], f, L);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) O[e] = __builtin_fmaf(o[e], f, O[e]);
+            }
+            if constexpr (SEES::PREFIX) {
+                if (s_row[r] < 0) continue;
+                const int64_t to = b * sees.rows + s_row[r];
+                if (d == 0) { sees.m[to] = M == -INFINITY ? M : to_base; sees.l[to] = L; }
+                *reinterpret_cast<kv_float4 *>(sees.o + to * D + d) = O;
+                continue;
             }
             if (r0 + r >= n_rows || !seq.has_row(tok)) continue;
             const float div = L > 0.f ? L : 1.f;
@@ -1006,25 +1126,13 @@ inline dim3 kv_numbered(int64_t n)
     return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
 }
 
-// The call's launches; `seen`: positions that a token sees, at most.
+// The launches by sixteens, as the plan says; `seen`: positions that a token sees, at most.
 template <typename SEES>
-hipError_t kv_attn_launches(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace, hipStream_t s, int64_t seen, SEES sees)
+hipError_t kv_attn_by_sixteens(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale_log2e, uint16_t *out, void *workspace, hipStream_t s, const KvPlan &plan,
+                               int64_t seen, SEES sees)
 {
     const int group = n_heads / v.n_kv_heads;
-    const float scale_log2e = scale * 1.4426950408889634f;
-    const KvPlan plan(v, head_dim, n_heads, seen);
     const KvDivide by_group(group), by_heads(v.n_kv_heads);
-    if (plan.rows) {
-        const int64_t blocks = ((int64_t)v.max_tokens * group + plan.rows - 1) / plan.rows;      // (at most 2^22 rows: 32768)
-        const dim3 grid = plan.packed ? kv_numbered(plan.blocks * v.n_kv_heads) : dim3((unsigned)v.n_kv_heads, (unsigned)blocks, (unsigned)v.n_seqs);
-        const hipError_t e = for_kv_tile(format, head_dim, [&](auto tag) {
-            typedef decltype(tag) T;
-            if (plan.rows == 64) hipLaunchKernelGGL((kv_attn_rows_kernel<T, 2, 4, 1, SEES>), grid, dim3(512), 0, s, v, q, n_heads, group, plan.few, by_group, scale_log2e, out, sees);
-            else hipLaunchKernelGGL((kv_attn_rows_kernel<T, 4, 1, 2, SEES>), grid, dim3(256), 0, s, v, q, n_heads, group, plan.few, by_group, scale_log2e, out, sees);
-            return hipGetLastError();
-        });
-        if (e != hipSuccess || !plan.sixteens) return e;
-    }
     const int few = plan.few ? plan.few : 0x7fffffff;
     hipError_t e = for_kv_tile(format, head_dim, [&](auto tag) {
         typedef decltype(tag) T;
@@ -1045,6 +1153,36 @@ hipError_t kv_attn_launches(int format, int head_dim, const KvView &v, const uin
     const dim3 tokens = plan.packed ? dim3((unsigned)std::min<int64_t>(v.n_tokens, 2 * (int64_t)v.n_seqs), (unsigned)n_heads) : dim3((unsigned)n_heads, (unsigned)v.max_tokens, (unsigned)v.n_seqs);
     hipLaunchKernelGGL(kv_attn_merge_kernel<SEES>, tokens, dim3((unsigned)head_dim, (unsigned)(groups > 8 ? 8 : groups)), 0, s, v, n_heads, group, few, workspace, out, sees);
     return hipGetLastError();
+}
+
+// The launch by blocks of `rows` rows.
+template <typename SEES>
+hipError_t kv_attn_by_blocks(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale_log2e, uint16_t *out, hipStream_t s, int rows, int few, dim3 grid, SEES sees)
+{
+    const int group = n_heads / v.n_kv_heads;
+    const KvDivide by_group(group);
+    return for_kv_tile(format, head_dim, [&](auto tag) {
+        typedef decltype(tag) T;
+        if (rows == 64) hipLaunchKernelGGL((kv_attn_rows_kernel<T, 2, 4, 1, SEES>), grid, dim3(512), 0, s, v, q, n_heads, group, few, by_group, scale_log2e, out, sees);
+        else hipLaunchKernelGGL((kv_attn_rows_kernel<T, 4, 1, 2, SEES>), grid, dim3(256), 0, s, v, q, n_heads, group, few, by_group, scale_log2e, out, sees);
+        return hipGetLastError();
+    });
+}
+
+// All of a call's launches.
+template <typename SEES>
+hipError_t kv_attn_launches(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace, hipStream_t s, int64_t seen, SEES sees)
+{
+    const int group = n_heads / v.n_kv_heads;
+    const float scale_log2e = scale * 1.4426950408889634f;
+    const KvPlan plan(v, head_dim, n_heads, seen);
+    if (plan.rows) {
+        const int64_t blocks = ((int64_t)v.max_tokens * group + plan.rows - 1) / plan.rows;      // (at most 2^22 rows: 32768)
+        const dim3 grid = plan.packed ? kv_numbered(plan.blocks * v.n_kv_heads) : dim3((unsigned)v.n_kv_heads, (unsigned)blocks, (unsigned)v.n_seqs);
+        const hipError_t e = kv_attn_by_blocks(format, head_dim, v, q, n_heads, scale_log2e, out, s, plan.rows, plan.few, grid, sees);
+        if (e != hipSuccess || !plan.sixteens) return e;
+    }
+    return kv_attn_by_sixteens(format, head_dim, v, q, n_heads, scale_log2e, out, workspace, s, plan, seen, sees);
 }
 
 }  // namespace iflow

@@ -33,6 +33,7 @@ decltype(&iflow_kv_read) p_kv_read;
 decltype(&iflow_kv_attn) p_kv_attn;
 decltype(&iflow_kv_tables) p_kv_tables;
 decltype(&iflow_kv_attn_window) p_kv_attn_window;
+decltype(&iflow_kv_attn_shared) p_kv_attn_shared;
 PyObject *s_data_ptr, *general;                                // general(name, arguments ...): the call that takes every form of argument
 PyTypeObject *cache_type, *batch_type, *pages_type;            // the classes of iflow_kv_cache_t, iflow_kv_batch_t and iflow_kv_pages_t
 
@@ -372,10 +373,27 @@ PyObject *kv_attn_window(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     return run(a, [&] { return p_kv_attn_window(&cache, &batch, q, heads, window, sinks, scale, out, workspace, (size_t)bytes, stream); });
 }
 
+PyObject *kv_attn_shared(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    Args a("kv_attn_shared", args, nargs, 12);
+    const iflow_kv_cache_t cache = a.description<iflow_kv_cache_t>(cache_type);
+    const iflow_kv_batch_t batch = a.description<iflow_kv_batch_t>(batch_type);
+    const int32_t *shared_pages = a.ptr<const int32_t>(), *shared_len = a.ptr<const int32_t>();
+    const int max_shared = a.word();
+    const uint16_t *q = a.ptr<const uint16_t>();
+    const int heads = a.word();
+    const float scale = a.real();
+    uint16_t *out = a.ptr<uint16_t>();
+    void *workspace = a.ptr<void>();
+    const int64_t bytes = a.num();
+    void *stream = a.handle();
+    return run(a, [&] { return p_kv_attn_shared(&cache, &batch, shared_pages, shared_len, max_shared, q, heads, scale, out, workspace, (size_t)bytes, stream); });
+}
+
 // bind(addresses of the functions, in this order)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
-    void *f[14];
+    void *f[15];
     Args a("bind", args, nargs, sizeof f / sizeof f[0]);
     for (void *&p : f) p = a.handle();
     if (a.bad) { PyErr_SetString(PyExc_TypeError, "an address for each function is wanted"); return nullptr; }
@@ -393,6 +411,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     p_kv_attn = reinterpret_cast<decltype(p_kv_attn)>(f[11]);
     p_kv_tables = reinterpret_cast<decltype(p_kv_tables)>(f[12]);
     p_kv_attn_window = reinterpret_cast<decltype(p_kv_attn_window)>(f[13]);
+    p_kv_attn_shared = reinterpret_cast<decltype(p_kv_attn_shared)>(f[14]);
     Py_RETURN_NONE;
 }
 
@@ -424,7 +443,7 @@ PyObject *descriptions(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 #define IFLOW_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {IFLOW_METHOD(bind), IFLOW_METHOD(otherwise), IFLOW_METHOD(quantize), IFLOW_METHOD(dequant), IFLOW_METHOD(qgemv), IFLOW_METHOD(qgemm),
                          IFLOW_METHOD(qgemv_fused), IFLOW_METHOD(qgemv_gated), IFLOW_METHOD(qgemm_fused), IFLOW_METHOD(attn_decode),
-                         IFLOW_METHOD(rope_append), IFLOW_METHOD(kv_append), IFLOW_METHOD(kv_read), IFLOW_METHOD(kv_attn), IFLOW_METHOD(kv_tables), IFLOW_METHOD(kv_attn_window), IFLOW_METHOD(descriptions), {nullptr, nullptr, 0, nullptr}};
+                         IFLOW_METHOD(rope_append), IFLOW_METHOD(kv_append), IFLOW_METHOD(kv_read), IFLOW_METHOD(kv_attn), IFLOW_METHOD(kv_tables), IFLOW_METHOD(kv_attn_window), IFLOW_METHOD(kv_attn_shared), IFLOW_METHOD(descriptions), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

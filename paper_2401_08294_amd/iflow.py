@@ -77,7 +77,7 @@ _native = None                 # the extension, bound to the library's functions
 # Enqueueing from Python, us, ctypes / here: a product with one vector 5.2 / 4.6, the attention's two launches 8.6 / 7.7, a decoder layer's six calls (seven
 # launches) 43 / 32 (on another host 4.4 / 3.7, 7.1 / 6.1, 35.0 / 24.6) - of which 2.3 and more a launch are the launch itself.
 _NATIVE_CALLS = ("quantize", "dequant", "qgemv", "qgemm", "qgemv_fused", "qgemv_gated", "qgemm_fused", "attn_decode", "rope_append", "kv_append", "kv_read", "kv_attn",
-                 "kv_tables", "kv_attn_window")
+                 "kv_tables", "kv_attn_window", "kv_attn_shared")
 
 
 class ArgumentError(C.ArgumentError, TypeError):
@@ -154,6 +154,10 @@ class _Ctypes:
     def kv_attn_window(cache, batch, q, n_heads, window, sinks, scale, out, workspace, workspace_bytes, stream):
         return _lib.iflow_kv_attn_window(cache, batch, _ptr(q), n_heads, window, sinks, scale, _ptr(out), _ptr(workspace), workspace_bytes, stream)
 
+    @staticmethod
+    def kv_attn_shared(cache, batch, shared_pages, shared_len, max_shared, q, n_heads, scale, out, workspace, workspace_bytes, stream):
+        return _lib.iflow_kv_attn_shared(cache, batch, _ptr(shared_pages), _ptr(shared_len), max_shared, _ptr(q), n_heads, scale, _ptr(out), _ptr(workspace), workspace_bytes, stream)
+
 
 def _through_ctypes(name, *args):
     try:
@@ -218,6 +222,8 @@ def lib():
         L.iflow_kv_attn.argtypes = [cache, batch, p, C.c_int, C.c_float, p, p, sz, p]
         L.iflow_kv_attn_window_workspace_bytes.argtypes = [cache, batch, C.c_int, C.c_int, C.c_int, C.POINTER(sz)]
         L.iflow_kv_attn_window.argtypes = [cache, batch, p, C.c_int, C.c_int, C.c_int, C.c_float, p, p, sz, p]
+        L.iflow_kv_attn_shared_workspace_bytes.argtypes = [cache, batch, C.c_int, C.c_int, C.POINTER(sz)]
+        L.iflow_kv_attn_shared.argtypes = [cache, batch, p, p, C.c_int, p, C.c_int, C.c_float, p, p, sz, p]
         L.iflow_kv_tables_workspace_bytes.argtypes = [cache, batch, C.POINTER(sz)]
         L.iflow_kv_tables.argtypes = [cache, batch, C.POINTER(KvPages), p, p, p, sz, p]
         L.iflow_qgemv_chain_workspace_bytes.argtypes = [C.c_int, C.POINTER(i64), C.POINTER(sz)]
@@ -462,6 +468,18 @@ def kv_attn_window_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int,
 def kv_attn_window(cache: KvCache, batch: KvBatch, q, n_heads: int, window: int, sinks: int, scale: float, out, workspace, workspace_bytes: int, stream=None) -> None:
     """kv_attn where a token sees the last `window` positions, its own among them, and its sequence's first `sinks`."""
     _check((_native or _calls()).kv_attn_window(cache, batch, q, n_heads, window, sinks, scale, out, workspace, workspace_bytes, _stream(stream)), "iflow_kv_attn_window")
+
+
+def kv_attn_shared_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int, max_shared: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().iflow_kv_attn_shared_workspace_bytes(C.byref(cache), C.byref(batch), n_heads, max_shared, C.byref(out)), "iflow_kv_attn_shared_workspace_bytes")
+    return int(out.value)
+
+
+def kv_attn_shared(cache: KvCache, batch: KvBatch, shared_pages, shared_len, max_shared: int, q, n_heads: int, scale: float, out, workspace, workspace_bytes: int, stream=None) -> None:
+    """kv_attn for sequences whose rows of the page table begin with the same pages, int32 device tensors shared_pages [max_shared / page_positions] and shared_len [1] (positions, of which whole
+    pages count): the prefix is attended over once for the tokens of all."""
+    _check((_native or _calls()).kv_attn_shared(cache, batch, shared_pages, shared_len, max_shared, q, n_heads, scale, out, workspace, workspace_bytes, _stream(stream)), "iflow_kv_attn_shared")
 
 
 def kv_pages(free_pages, free_state, held, free_state_out=None, held_out=None, shared_pages=None, n_shared: int = 0) -> KvPages:

@@ -1,0 +1,68 @@
+"""iflow_kv_attn_shared without a GPU: refusals, workspace, and the arguments' way through the extension."""
+import ctypes as C
+
+import pytest
+
+from test_host_logic import iflow  # noqa: F401
+
+AT, FAR = 0x100000, 0x40000000                                  # aligned, never dereferenced
+
+
+def described(iflow, cache={}, **change):  # noqa: F811
+    c, b = iflow.KvCache(), iflow.KvBatch()
+    for k, v in {**dict(format=iflow.Q4_B64, n_kv_heads=8, head_dim=128, page_positions=64, n_pages=100, pages=FAR), **cache}.items():
+        setattr(c, k, v)
+    for k, v in {**dict(n_seqs=4, max_pages=60, page_table=AT, seq_lens=AT, first_token=AT, n_tokens=9, max_tokens=5, max_seq=3840), **change}.items():
+        setattr(b, k, v)
+    return c, b
+
+
+def test_refusals_before_any_launch(iflow):  # noqa: F811
+    L = iflow.lib()
+    c, b = described(iflow)
+    need = iflow.kv_attn_shared_workspace_bytes(c, b, 32, 3000)
+    assert need > 9 * 32 * 130 * 4 and need % 16 == 0
+    # one sequence, less than a page: what causal attention needs
+    one = described(iflow, n_seqs=1)
+    assert iflow.kv_attn_shared_workspace_bytes(*one, 32, 3000) == iflow.kv_attn_workspace_bytes(*one, 32)
+    assert iflow.kv_attn_shared_workspace_bytes(c, b, 32, 63) == iflow.kv_attn_shared_workspace_bytes(c, b, 32, 0) == iflow.kv_attn_workspace_bytes(c, b, 32)
+
+    def call(pages=5 * AT, length=6 * AT, most=3000, q=2 * AT, heads=32, scale=0.1, out=3 * AT, ws=8 * AT, size=need, of=(c, b)):
+        return L.iflow_kv_attn_shared(*of, pages, length, most, q, heads, scale, out, ws, size, None)
+    for kw, status in ((dict(most=-1), iflow.ERR_SHAPE), (dict(most=3841), iflow.ERR_SHAPE), (dict(scale=0.0), iflow.ERR_SHAPE), (dict(scale=float("inf")), iflow.ERR_SHAPE), (dict(heads=12), iflow.ERR_SHAPE),
+                       (dict(pages=None), iflow.ERR_NULL), (dict(length=None), iflow.ERR_NULL), (dict(q=None), iflow.ERR_NULL), (dict(out=None), iflow.ERR_NULL), (dict(ws=None), iflow.ERR_NULL),
+                       (dict(size=need - 1), iflow.ERR_SIZE), (dict(pages=5 * AT + 2), iflow.ERR_ALIGN), (dict(length=6 * AT + 1), iflow.ERR_ALIGN), (dict(q=2 * AT + 2), iflow.ERR_ALIGN),
+                       (dict(out=3 * AT + 8), iflow.ERR_ALIGN), (dict(ws=8 * AT + 4), iflow.ERR_ALIGN), (dict(out=2 * AT + 64), iflow.ERR_SHAPE), (dict(ws=2 * AT), iflow.ERR_SHAPE),
+                       (dict(ws=FAR + 4096), iflow.ERR_SHAPE), (dict(out=FAR), iflow.ERR_SHAPE), (dict(out=AT), iflow.ERR_SHAPE), (dict(pages=3 * AT - 4 * 45), iflow.ERR_SHAPE), (dict(length=3 * AT + 9 * 32 * 256 - 4), iflow.ERR_SHAPE),
+                       (dict(pages=8 * AT + need - 4), iflow.ERR_SHAPE), (dict(length=8 * AT), iflow.ERR_SHAPE), (dict(of=(None, b)), iflow.ERR_NULL), (dict(of=(c, None)), iflow.ERR_NULL),
+                       (dict(of=described(iflow, page_table=None, max_pages=25, max_seq=1600), most=1600), iflow.ERR_NULL), (dict(of=described(iflow, max_seq=3841)), iflow.ERR_SHAPE),
+                       (dict(of=described(iflow, seq_lens=None)), iflow.ERR_NULL), (dict(of=described(iflow, cache=dict(format=77))), iflow.ERR_FORMAT)):
+        assert call(**kw) == status, kw
+    size = C.c_size_t(0)
+    for most in (-1, 3841):
+        assert L.iflow_kv_attn_shared_workspace_bytes(c, b, 32, most, C.byref(size)) == iflow.ERR_SHAPE
+    assert L.iflow_kv_attn_shared_workspace_bytes(c, b, 32, 64, None) == iflow.ERR_NULL
+    with pytest.raises(iflow.IflowError) as info:
+        iflow.kv_attn_shared(c, b, 5 * AT, None, 3000, 2 * AT, 32, 0.1, 3 * AT, 8 * AT, need, stream=0)
+    assert info.value.status == iflow.ERR_NULL
+
+
+def test_extension_hands_the_call_on(iflow):  # noqa: F811
+    L, native, seen = iflow.lib(), iflow._native, []
+
+    def record(cache, batch, *args):
+        seen.append((cache.contents.n_pages, batch.contents.n_tokens) + args)
+        return iflow.ERR_SIZE
+    fake = C.CFUNCTYPE(C.c_int, *L.iflow_kv_attn_shared.argtypes)(record)
+    real = [C.cast(getattr(L, "iflow_" + name), C.c_void_p).value for name in iflow._NATIVE_CALLS]
+    native.bind(*[C.cast(fake, C.c_void_p).value if name == "kv_attn_shared" else at for name, at in zip(iflow._NATIVE_CALLS, real)])
+    c, b = described(iflow)
+    try:
+        with pytest.raises(iflow.IflowError):
+            iflow.kv_attn_shared(c, b, 11, 12, 13, 14, 15, 0.25, 16, None, 17 << 40, stream=18)
+        assert seen.pop() == (100, 9, 11, 12, 13, 14, 15, 0.25, 16, None, 17 << 40, 18)
+        with pytest.raises((TypeError, ValueError, AttributeError)):
+            iflow.kv_attn_shared(c, b, 11, 12, "13", 14, 15, 0.25, 16, None, 17, stream=18)
+        assert not seen
+    finally:
+        native.bind(*real)
