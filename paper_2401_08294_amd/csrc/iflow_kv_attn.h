@@ -102,7 +102,7 @@ struct KvShared {
 };
 struct KvSeesPrefix : KvShared {
     static constexpr bool MAPPED = true, LOW = false, PREFIX = true, TAIL = false;
-    int few;                                                  // sequences of as many rows are served otherwise
+    int few, per;                                             // sequences of as many rows are served otherwise; tiles of a part
 };
 struct KvSeesTail : KvShared {
     static constexpr bool MAPPED = true, LOW = false, PREFIX = false, TAIL = true;
@@ -110,23 +110,37 @@ struct KvSeesTail : KvShared {
     int start;                                                // tiles of the prefix: the kernel asks for them first
     __device__ __forceinline__ KvSpan span(int, int longest) const { return {0, start, max(0, (longest + KV_TILE - 1) / KV_TILE - start)}; }
     __device__ __forceinline__ int line_tiles(const KvSequence &seq, int) const { return max(0, (seq.sees(seq.count - 1) + KV_TILE - 1) / KV_TILE - start); }
-    // n of a row's values, relative to `base` (-inf: there are none), and the prefix's, relative to what comes back
+    // N of a row's values, from component d on, and its sum, relative to `base` (-inf: it has none): with the prefix's, relative to the largest reference.  Eight parts are asked for at once.
     template <int N> __device__ __forceinline__ void add(int64_t row, int d, float base, float &sum, float (&values)[N]) const
     {
-        float top = base;
-        for (int c = 0; c < parts; ++c) top = fmaxf(top, m[c * rows + row]);
-        const float f0 = base == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base - top);
-        sum *= f0;
+        typedef float Values __attribute__((ext_vector_type(N)));
+        constexpr int AT_ONCE = 8;
+        for (int c0 = 0; c0 < parts; c0 += AT_ONCE) {
+            float mc[AT_ONCE], lc[AT_ONCE];
+            Values oc[AT_ONCE];
 #pragma unroll
-        for (int e = 0; e < N; ++e) values[e] *= f0;
-        for (int c = 0; c < parts; ++c) {
-            const int64_t at = c * rows + row;
-            const float mc = m[at];
-            if (mc == -INFINITY) continue;                    // (nothing is written of a part that a row sees nothing of)
-            const float f = __builtin_amdgcn_exp2f(mc - top);
-            sum = __builtin_fmaf(l[at], f, sum);
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int64_t at = min(c0 + i, parts - 1) * rows + row;          // (past the end: the last one again, with no weight)
+                mc[i] = c0 + i < parts ? m[at] : -INFINITY;
+                lc[i] = l[at];
+                oc[i] = *reinterpret_cast<const Values *>(o + at * d_of + d);
+            }
+            float top = base;
 #pragma unroll
-            for (int e = 0; e < N; ++e) values[e] = __builtin_fmaf(o[at * d_of + d + e], f, values[e]);
+            for (int i = 0; i < AT_ONCE; ++i) top = fmaxf(top, mc[i]);
+            const float again = base == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base - top);
+            sum *= again;
+#pragma unroll
+            for (int e = 0; e < N; ++e) values[e] *= again;
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+                if (mc[i] == -INFINITY) continue;             // (a part of which the row sees nothing)
+                const float f = __builtin_amdgcn_exp2f(mc[i] - top);
+                sum = __builtin_fmaf(lc[i], f, sum);
+#pragma unroll
+                for (int e = 0; e < N; ++e) values[e] = __builtin_fmaf(oc[i][e], f, values[e]);
+            }
+            base = top;
         }
     }
 };
@@ -568,8 +582,8 @@ __global__ __launch_bounds__(1024) void kv_attn_merge_kernel(KvView v, int n_hea
 //   S[position][row] = K Q^T with the queries in registers; a lane has one row's scores, sixteen of every 32 positions, and its half of the row's maximum and sum;
 //   O[component][row] = V^T P^T: element e of a tile's scores is position 4g + e % 4 or 16 + 4g + e % 4 of g = 2 (e / 8) + h where row i of S is position i with bits 3 and 4 changed
 //   over, so a lane's probabilities are its own operand, and a value's eight positions are a word of the cache's.  The sums' factors are the lane's own too.
-// PREFIX: the rows are those of all sequences' tokens, one after another, the positions a part (blockIdx.z) of the shared ones.  A token's sequence is looked for among the first tokens; sequences that
-// are served otherwise (of `few` rows and more) have no rows here.
+// PREFIX: the rows are those of all sequences' tokens, one after another, the positions a part (blockIdx.z) of the shared ones.  Sequences that are served otherwise (of `few` rows and more) have no
+// rows here.
 // Keys in LDS: [tile][component / 8][i: 32][8 components], values: [tile][g][component][8 positions]: 16-byte pieces that 32 lanes read side by side.
 // PG groups of wavefronts take every PG-th 64 positions and add up in LDS: where there are too few rows to fill the device.  The probabilities are two fp16 numbers each, and two products of every value,
 // as in kv_attn_kernel: a token's output does not depend on how many rows its batch has but for the order of fp32 sums.  (Rounded to fp16 once, with one product, they made the largest error 1.4e-3 of a
@@ -580,26 +594,40 @@ typedef float kv_float16 __attribute__((ext_vector_type(16)));
 struct KvCallRows {
     static constexpr int row = 0;
     int count, part;
-    __device__ __forceinline__ bool has_row(int i) const { return (uint32_t)i < (uint32_t)count; }
+    __device__ __forceinline__ bool has_row(int i) const { return i < count; }
     __device__ __forceinline__ int sees(int) const { return part; }
 };
-// whether a row of the call's arrays is a token's that sixteens serve, and what it sees
-struct KvToken { bool real; int limit; };
-__device__ __forceinline__ KvToken kv_token(const KvView &v, int row, int group, int few)
+// PREFIX: the w-th of all tokens that share the prefix, those of sequences of less than `few` rows in order, each lane its own: its row in the call's arrays (-1: there is none) and what it sees
+struct KvToken { int row, limit; };
+__device__ __forceinline__ KvToken kv_token(const KvView &v, int w, int group, int few)
 {
-    int b = row;
-    if (v.first) {                                            // the last sequence that begins at or in front of the row
-        b = 0;
-        for (int n = v.n_seqs; n > 1;) {
-            const int half = n >> 1;
-            if (v.first[b + half] <= row) b += half;
-            n -= half;
-        }
+    if (!v.first) {                                           // one each
+        if (w >= v.n_seqs) return {-1, 0};
+        return {w, KvSequence(v, w).sees(0)};
     }
-    if (b >= v.n_seqs) return {false, 0};
-    const KvSequence seq(v, b);
-    const int i = (int)((uint32_t)row - (uint32_t)seq.row);
-    return {seq.has_row(i) && (int64_t)seq.count * group < few, seq.sees(i)};
+    const int lane = threadIdx.x & 63;
+    KvToken token = {-1, 0};
+    for (int b = 0; b < v.n_seqs; b += 64) {
+        int mine = 0, row = 0, position = 0;
+        if (b + lane < v.n_seqs) {
+            const KvSequence seq(v, b + lane);
+            mine = seq.count * group < few ? seq.count : 0;
+            row = seq.row; position = seq.position;
+        }
+        const int upto = wave_scan(mine), all = __builtin_amdgcn_readlane(upto, 63);
+        int at = 0;                                           // the first of these sequences with more than w tokens up to its end
+#pragma unroll
+        for (int n = 32; n > 0; n >>= 1)
+            if (__shfl(upto, at + n - 1) <= w) at += n;
+        const int i = w - __shfl(upto - mine, at & 63), first = __shfl(row, at & 63), p = __shfl(position, at & 63);
+        if (w >= 0 && w < all) {
+            const int to = (int)((uint32_t)first + (uint32_t)i);
+            token = {(uint32_t)to < (uint32_t)v.n_tokens ? to : -1, max(0, min((int)((uint32_t)p + (uint32_t)i + 1u), v.max_seq))};
+        }
+        w -= all;
+        if (__builtin_amdgcn_ballot_w64(w >= 0) == 0) break;
+    }
+    return token;
 }
 
 template <typename T, int RG, int PG, int STAGES, typename SEES>
@@ -633,7 +661,7 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
         const int t = kv_where<SEES>(span, t0 + lane);
         if constexpr (SEES::PREFIX) {
             const int p = v.page_of(t);
-            my_tile = t0 + lane < span.tiles ? reinterpret_cast<uint64_t>(kv_tile_in(v, sees.pages[p], head, t - p * v.tiles_per_page, T::BYTES)) : 0;
+            my_tile = t0 + lane < span.tiles && t * KV_TILE < sees.max_len ? reinterpret_cast<uint64_t>(kv_tile_in(v, sees.pages[p], head, t - p * v.tiles_per_page, T::BYTES)) : 0;
             return;
         }
         my_tile = t * KV_TILE < v.max_seq ? reinterpret_cast<uint64_t>(kv_tile_at(v, b, head, t, T::BYTES)) : 0;
@@ -641,9 +669,10 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     if constexpr (!SEES::MAPPED) find_tiles(0);
     const auto seq = [&] {
         if constexpr (SEES::PREFIX) {
-            const int all = sees.tiles(v), per = ((all + sees.parts - 1) / sees.parts + 1) & ~1, from = min(all, per * b);
-            span = {0, from, min(per, all - from)};
-            return KvCallRows{(int)v.n_tokens, (from + span.tiles) * KV_TILE};
+            span = {0, sees.per * b, sees.per};
+            find_tiles(0);                                    // (the prefix's length is asked for beside its pages, not in front of them)
+            span.tiles = max(0, min(sees.per, sees.tiles(v) - span.skip));
+            return KvCallRows{(int)v.n_tokens, (span.skip + span.tiles) * KV_TILE};
         } else {
             return KvSequence(v, b);
         }
@@ -655,11 +684,11 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     auto same = [](int n) { return __builtin_amdgcn_readfirstlane(n); };
     const int longest = same(seq.sees(by_group(min(n_rows, r0 + ROWS) - 1)));
     const int my_row = min(n_rows - 1, r0 + rg * 32 + li), token = by_group(my_row);
-    KvToken found = {true, 0};
+    KvToken found = {0, 0};
     if constexpr (SEES::PREFIX) found = kv_token(v, token, group, sees.few);
-    const bool real = r0 + rg * 32 + li < n_rows && seq.has_row(token) && found.real;
+    const bool real = r0 + rg * 32 + li < n_rows && (SEES::PREFIX ? found.row >= 0 : seq.has_row(token));
     const int limit = SEES::PREFIX && real ? min(found.limit, longest) : seq.sees(token);
-    const int64_t my_out = ((int64_t)(seq.row + token) * n_heads + head * group + (my_row - token * group)) * D;
+    const int64_t my_out = ((int64_t)(SEES::PREFIX ? found.row : seq.row + token) * n_heads + head * group + (my_row - token * group)) * D;
     // of the wavefront's rows: what the first sees, and the last
     const int shortest = SEES::PREFIX ? (__builtin_amdgcn_ballot_w64(limit < longest) == 0 ? longest : 0) : same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32)))), limit_of_wave = same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32 + 31))));
     const int first_limit = same(seq.sees(by_group(r0)));     // of the workgroup's rows: what the first sees
@@ -670,10 +699,8 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     } else {
         span = sees.span(first_limit, longest);
     }
-    if constexpr (SEES::MAPPED) {
-        span = {same(span.front), same(span.skip), same(span.tiles)};
-        find_tiles(0);
-    }
+    if constexpr (SEES::MAPPED) span = {same(span.front), same(span.skip), same(span.tiles)};
+    if constexpr (SEES::MAPPED && !SEES::PREFIX) find_tiles(0);
     uint8_t *stage = s_mem + pg * GROUP;
 
     // queries as B operands: lane (row li, hf) holds components 16u + 8 hf .. +8

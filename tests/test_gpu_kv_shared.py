@@ -1,4 +1,4 @@
-"""GPU parity of iflow_kv_attn_shared against the oracle's causal attention, in 64 bits, and iflow_kv_tables, iflow_kv_append and the attention calls together, as a program that serves makes them.
+"""GPU parity of iflow_kv_attn_shared against causal attention in 64 bits over what the cache holds, and iflow_kv_tables, iflow_kv_append and the attention calls together, as a program that serves makes them.
 
 The tolerance is that of causal attention rounded once (2^-11 of the value, and 2^-15 of the output's rms for what 32 bits leave; half of that is used up: see test_gpu_kv_window.py).  Adding the prefix's
 sums to the others' multiplies each by an exponential once more, 1e-7 of it.
@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from paper_2401_08294_amd import synth
-from test_gpu_kv import BASE, FORMATS, Setup, _guarded
+from test_gpu_kv import BASE, FORMATS, _guarded
 from test_gpu_parity import gpu, say  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -15,108 +15,192 @@ pytestmark = pytest.mark.gpu
 TOL = 2.0 ** -11 + 2.0 ** -15
 
 
-class Shared(Setup):
-    """Sequences whose rows of the table begin with the same pages."""
+class Shared:
+    """A pool whose sequences begin with the same pages, on the device: random bytes (what is no number among them) wherever nothing was appended."""
 
-    def share(self, positions, most=None):
-        self.shared_len, self.max_shared = positions, positions if most is None else most
-        n = self.max_shared // self.page
-        self.table[:, :n] = self.table[0, :n]
-        return self
+    def __init__(self, gpu, name, n_heads, n_kv, d, page, lens, counts, shared, seed, most=None, max_seq=None, n_tokens=None, first=None, max_tokens=None, spare=3):  # noqa: F811
+        self.torch, self.iflow = gpu
+        torch, it = gpu
+        say(f"[case] kv shared {name} {n_heads}/{n_kv} heads of {d}, page {page}, {len(lens)} sequences to {max(lens)}, tokens {counts if counts is None else counts[:6]}, prefix {shared} of {most}")
+        self.fmt, self.n_heads, self.n_kv, self.d, self.page = it.FORMATS[name], n_heads, n_kv, d, page
+        self.shared_len, self.max_shared = shared, shared if most is None else most
+        rng = np.random.default_rng(synth.BASE_SEED + seed)
+        self.g = torch.Generator(device="cuda").manual_seed(seed)
+        self.single = counts is None and first is None
+        counts = [1] * len(lens) if counts is None else counts
+        self.lens = np.array(lens, np.int32)
+        self.first = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32) if first is None else np.array(first, np.int32)
+        self.max_seq = max(int(self.lens.max()), self.max_shared) if max_seq is None else max_seq
+        self.max_tokens = max(1, max(counts)) if max_tokens is None else max_tokens
+        self.n_tokens = max(1, int(self.first.max())) if n_tokens is None else n_tokens
+        self.max_pages = -(-self.max_seq // page)
+        n_pages = len(lens) * self.max_pages + spare
+        self.table = rng.permutation(n_pages)[:len(lens) * self.max_pages].reshape(len(lens), -1).astype(np.int32)
+        self.table[:, :self.max_shared // page] = self.table[0, :self.max_shared // page]
+        size = it.kv_cache_bytes(it.kv_cache(self.fmt, n_kv, d, page, n_pages))
+        self.pool = torch.randint(0, 256, (size,), dtype=torch.uint8, device="cuda", generator=self.g)
+        self.cache = it.kv_cache(self.fmt, n_kv, d, page, n_pages, self.pool)
+        # the prefix by one sequence that has it, then everybody's positions behind it (in the cache's own 16 bits after rotation, as a program appends them)
+        whole = self.max_shared // page * page
+        self.append(self.table[:1], [max(whole, 1)], [max(whole, 1)])
+        self.append(self.table, np.maximum(self.lens, 0), np.maximum(0, self.lens - whole))
+        self.describe()
+
+    def dev(self, a):
+        return self.torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+    def normal(self, shape, scale=1.0):
+        return (scale * self.torch.randn(shape, device="cuda", generator=self.g)).half()
+
+    def batch_of(self, table, lens, counts):
+        first = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        n = max(1, int(first[-1]))
+        return self.iflow.kv_batch(len(lens), table.shape[1], self.dev(table), self.dev(np.asarray(lens, np.int32)), table.shape[1] * self.page, self.dev(first), n, max(1, int(max(counts)))), first, n
+
+    def append(self, table, lens, counts):
+        batch, _, n = self.batch_of(table, lens, counts)
+        q = self.normal((n, self.n_heads, self.d))
+        self.iflow.kv_append(self.cache, batch, q, self.normal((n, self.n_kv, self.d)), self.normal((n, self.n_kv, self.d)), self.n_heads, BASE, 1, q)
+        self.torch.cuda.synchronize()
 
     def describe(self):
-        super().describe()
+        it = self.iflow
+        self.d_lens, self.d_table, self.d_first = self.dev(self.lens), self.dev(self.table), self.dev(self.first)
+        self.batch = it.kv_batch(len(self.lens), self.max_pages, self.d_table, self.d_lens, self.max_seq, None if self.single else self.d_first, self.n_tokens, self.max_tokens)
         self.d_shared = self.dev(np.concatenate([self.table[0, :self.max_shared // self.page], [1 << 30]]).astype(np.int32))
         self.d_shared_len = self.dev(np.array([self.shared_len], np.int32))
 
     def room(self):
-        return self.iflow.kv_attn_shared_workspace_bytes(self.d_cache, self.d_batch, self.n_heads, self.max_shared)
+        return self.iflow.kv_attn_shared_workspace_bytes(self.cache, self.batch, self.n_heads, self.max_shared)
 
-    def attend(self, q, scale, out=None, ws=None):
-        torch, it = self.torch, self.iflow
+    def shares(self):
+        """Whether the call goes another way than causal attention (which needs no room, or another)."""
+        return self.room() != self.iflow.kv_attn_workspace_bytes(self.cache, self.batch, self.n_heads)
+
+    def attend(self, q, scale, ws=None):
+        torch = self.torch
         need = self.room()
-        if ws is None:
-            ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")      # (what a part leaves unwritten is no number)
-        out = torch.full((self.n_tokens, self.n_heads, self.d), 7.0, dtype=torch.float16, device="cuda") if out is None else out
-        it.kv_attn_shared(self.d_cache, self.d_batch, self.d_shared, self.d_shared_len, self.max_shared, self.dev(q), self.n_heads, scale, out, ws, need)
+        ws = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda") if ws is None else ws      # (what a part leaves unwritten is no number)
+        out = torch.full((self.n_tokens, self.n_heads, self.d), 7.0, dtype=torch.float16, device="cuda")
+        self.iflow.kv_attn_shared(self.cache, self.batch, self.d_shared, self.d_shared_len, self.max_shared, q, self.n_heads, scale, out, ws, need)
         torch.cuda.synchronize()
-        return out.cpu().numpy().astype(np.float64)
+        return out
+
+    def reference(self, q, scale):
+        """Causal attention in 64 bits over what the cache reads back, whose bits are the oracle's (test_gpu_kv.py)."""
+        torch, group = self.torch, self.n_heads // self.n_kv
+        lens = np.clip(self.lens, 0, self.max_seq)
+        batch, first, n = self.batch_of(self.table, lens, lens)
+        k, v = [torch.empty((n, self.n_kv, self.d), dtype=torch.float16, device="cuda") for _ in range(2)]
+        self.iflow.kv_read(self.cache, batch, k, v)
+        out = torch.full((self.n_tokens, self.n_heads, self.d), 7.0, dtype=torch.float64, device="cuda")
+        for b in range(len(lens)):
+            row, count = (b, 1) if self.single else (int(self.first[b]), int(self.first[b + 1]) - int(self.first[b]))
+            kept = min(count, self.max_tokens, self.n_tokens - row)
+            if kept <= 0:
+                continue
+            K, V = [x[first[b]:first[b + 1]].double().transpose(0, 1).contiguous() for x in (k, v)]      # [kv head][position][D]
+            there = torch.tensor([0 <= int(self.table[b, p // self.page]) < self.cache.n_pages for p in range(int(lens[b]))], dtype=torch.bool, device="cuda")
+            Q = q[row:row + kept].double().transpose(0, 1).reshape(self.n_kv, group * kept, self.d)              # rows: head of the group, token
+            score = scale * torch.matmul(Q, K.transpose(1, 2).contiguous()).view(self.n_kv, group, kept, -1)
+            at = int(self.lens[b]) - count + torch.arange(kept, device="cuda").unsqueeze(1)
+            seen = (torch.arange(int(lens[b]), device="cuda") <= at) & there
+            score = score.masked_fill(~seen, float("-inf"))
+            weight = torch.softmax(score, -1).nan_to_num(0.0) if score.shape[-1] else score                      # (nothing seen: zeros)
+            out[row:row + kept] = torch.matmul(weight.reshape(self.n_kv, group * kept, -1), V).view(self.n_heads, kept, self.d).transpose(0, 1)
+        return out
+
+    def compare(self, got, want, tol=TOL):
+        got = got.double()
+        rms = want.square().mean(-1, keepdim=True).sqrt()
+        e = ((got - want).abs() / want.abs().maximum(rms.clamp_min(1e-30))).max().item()
+        assert bool(self.torch.isfinite(got).all()) and e <= tol, e
+        say(f"        max rel err {e:.2e}")
 
     def check(self, scale=1.0, tol=TOL):
-        q = self.queries(scale)
-        want = np.full((self.n_tokens, self.n_heads, self.d), 7.0)
-        self.kv_cache.attend(self.cache, *self.args(), q, self.d ** -0.5, want)
-        got = self.attend(q, self.d ** -0.5)
-        rms = np.sqrt(np.mean(want ** 2, axis=-1, keepdims=True))
-        e = np.abs(got - want) / np.maximum(np.abs(want), np.maximum(rms, 1e-30))
-        assert np.isfinite(got).all() and e.max() <= tol, (float(e.max()), np.unravel_index(e.argmax(), e.shape))
-        say(f"        max rel err {e.max():.2e}")
+        q = self.normal((self.n_tokens, self.n_heads, self.d), scale)
+        self.compare(self.attend(q, self.d ** -0.5), self.reference(q, self.d ** -0.5), tol)
 
 
-def make(gpu, name, n_kv, d, page, lens, counts, seed, n_heads, shared, most=None, **kw):  # noqa: F811
-    say(f"[case] kv shared {name} {n_heads}/{n_kv} heads of {d}, page {page}, lengths {lens[:6]}, tokens {counts}, prefix {shared} of {most}")
-    s = Shared(gpu, name, n_kv, d, page, lens, counts, seed, n_heads, **kw).share(shared, most)
-    s.fill()
-    s.describe()
-    return s
+OWN = [0, 1, 31, 32, 33, 100, 64, 200, 5, 300, 2, 77, 96, 95, 128, 11]
 
 
-@pytest.mark.parametrize("shared", [64, 320, 576])
 @pytest.mark.parametrize("name", FORMATS)
-@pytest.mark.parametrize("n_heads,n_kv,d", [(8, 2, 128), (17, 1, 64), (4, 4, 64), (16, 1, 128)])
-def test_one_token_each(gpu, name, n_heads, n_kv, d, shared):  # noqa: F811
-    """Own positions of none, one, a tile and more; a sequence that has ended, and ones that are inside the prefix; prefixes of one part and of several."""
-    own = [0, 1, 31, 32, 33, 100, 64, 200, 5]
-    lens = [shared + n for n in own] + [0, shared // 2, 1, shared - 1]
-    make(gpu, name, n_kv, d, 64, lens, None, 8100 + n_heads, n_heads, shared).check()
+@pytest.mark.parametrize("n_heads,n_kv,d,n,shared,page", [(32, 8, 128, 64, 1024, 64), (71, 1, 64, 40, 4064, 32), (32, 32, 128, 16, 1056, 96), (64, 64, 64, 13, 1024, 256), (128, 8, 128, 17, 4128, 32), (64, 8, 64, 33, 2048, 128),
+                                                        (12, 4, 128, 160, 512, 64)])
+def test_one_token_each(gpu, name, n_heads, n_kv, d, n, shared, page):  # noqa: F811
+    """Own positions of none, one, a tile and more; sequences that have ended, and ones that are inside the prefix; prefixes of one part and of several, tiles of an odd number."""
+    own = (OWN * 10)[:n - 4]
+    s = Shared(gpu, name, n_heads, n_kv, d, page, [shared + x for x in own] + [0, shared // 2, 1, shared - 1], None, shared, 8100 + n_heads)
+    assert s.shares()
+    s.check()
 
 
-@pytest.mark.parametrize("name,n_heads,n_kv,d,own,counts,shared", [
-    ("Q4_B64", 32, 8, 128, [30, 7, 9], [4, 3, 1], 512), ("Q4_B32", 71, 1, 64, [33, 64, 1, 2], [3, 4, 1, 0], 544), ("Q8_B32", 8, 8, 128, [10, 23], [7, 8], 96), ("Q4_B64", 8, 2, 128, [200, 1], [200, 1], 64),
-    ("Q8_B64", 12, 4, 64, [150, 33, 40], [150, 10, 17], 320), ("Q4_B32", 16, 2, 128, [129, 31], [129, 31], 256), ("Q4_B64", 5, 5, 64, [100, 20], [77, 3], 64)])
-def test_several_tokens(gpu, name, n_heads, n_kv, d, own, counts, shared):  # noqa: F811
-    """Drafts and chunks behind the prefix."""
-    make(gpu, name, n_kv, d, 32, [shared + n for n in own], counts, 8200 + n_heads + d, n_heads, shared).check()
+@pytest.mark.parametrize("name,n_heads,n_kv,d,n,most,shared", [("Q4_B64", 32, 8, 128, 40, 5, 2048), ("Q4_B32", 71, 1, 64, 24, 4, 2080), ("Q8_B32", 32, 32, 128, 12, 8, 1024), ("Q8_B64", 64, 8, 64, 20, 17, 1536),
+                                                              ("Q4_B64", 40, 8, 128, 9, 60, 2048), ("Q8_B64", 12, 4, 128, 30, 31, 1056)])
+def test_several_tokens(gpu, name, n_heads, n_kv, d, n, most, shared):  # noqa: F811
+    """Drafts and chunks behind the prefix, of different numbers of tokens, of none."""
+    counts = [(7 * i * i + 3 * i) % (most + 1) for i in range(n - 1)] + [most]
+    s = Shared(gpu, name, n_heads, n_kv, d, 32, [shared + c + (13 * i) % 90 for i, c in enumerate(counts)], counts, shared, 8200 + n_heads)
+    assert s.shares()
+    s.check()
 
 
-@pytest.mark.parametrize("name,n_heads,n_kv,d,own,counts", [
-    ("Q4_B64", 64, 64, 64, [150, 3, 140, 1, 70, 1], [150, 1, 129, 1, 70, 1]), ("Q4_B32", 128, 64, 128, [1, 90, 200, 5, 0], [1, 64, 130, 2, 0]), ("Q8_B64", 64, 64, 128, [129, 130, 1, 127], [129, 128, 1, 127])])
-def test_chunks_beside_single_tokens(gpu, name, n_heads, n_kv, d, own, counts):  # noqa: F811
-    """Sequences of many rows go by blocks of their own, the others share the prefix."""
-    make(gpu, name, n_kv, d, 64, [192 + n for n in own], counts, 8300 + n_heads + d, n_heads, 192).check()
+@pytest.mark.parametrize("name,n_heads,n_kv,d,big,n,shared", [("Q4_B64", 64, 64, 64, [150, 129, 200], 40, 1024), ("Q8_B32", 32, 8, 128, [300, 256, 290, 32, 31], 150, 1024), ("Q4_B32", 128, 64, 128, [64, 63, 140], 30, 640),
+                                                             ("Q8_B64", 64, 8, 128, [600, 16, 15, 500], 130, 1024)])
+def test_chunks_beside_single_tokens(gpu, name, n_heads, n_kv, d, big, n, shared):  # noqa: F811
+    """Sequences of many rows, and of one fewer, go by blocks of their own, before, between and behind the others, which share the prefix; more of these than a wavefront has lanes."""
+    counts = [1] * n
+    for i, c in enumerate(big):
+        counts.insert((i * n) // len(big) + (i == len(big) - 1), c)
+    counts[5] = 0
+    s = Shared(gpu, name, n_heads, n_kv, d, 64, [shared + c + (29 * i) % 70 for i, c in enumerate(counts)], counts, shared, 8300 + n_heads)
+    assert s.shares()
+    s.check()
 
 
-@pytest.mark.parametrize("name,n_heads,n_kv,d,own,counts,shared", [
-    ("Q4_B64", 8, 2, 128, [2100, 5, 1900, 0, 1024], None, 128), ("Q8_B32", 3, 1, 64, [2500, 1281], None, 64), ("Q4_B32", 40, 2, 64, [2000, 1, 1700], [2, 1, 2], 64), ("Q4_B32", 5, 1, 128, [40] * 66 + [1500, 33], None, 32)])
-def test_long_own_positions(gpu, name, n_heads, n_kv, d, own, counts, shared):  # noqa: F811
-    """What lies behind the prefix is cut and merged, and the prefix added to that."""
-    make(gpu, name, n_kv, d, 32, [shared + n for n in own], counts, 8400 + n_heads, n_heads, shared).check()
+@pytest.mark.parametrize("name,n_heads,n_kv,d,n,own,counts,shared", [("Q4_B64", 32, 8, 128, 40, 1500, None, 4096), ("Q8_B32", 64, 8, 64, 140, 3000, None, 1024), ("Q8_B64", 64, 8, 64, 40, 1200, 2, 4096), ("Q4_B32", 71, 1, 64, 30, 2500, 3, 8192), ("Q4_B64", 32, 8, 128, 140, 3000, None, 1024)])
+def test_long_own_positions(gpu, name, n_heads, n_kv, d, n, own, counts, shared):  # noqa: F811
+    """What lies behind the prefix is cut and merged, and the prefix added to that; sequences with little or nothing behind it among them."""
+    lens = [shared + (own if i % 3 == 0 else (53 * i) % own) for i in range(n - 2)] + [shared, shared + 3]
+    s = Shared(gpu, name, n_heads, n_kv, d, 64, lens, None if counts is None else [min(counts, x - shared) for x in lens], shared, 8400 + n_heads)
+    assert s.shares()
+    s.check()
 
 
-@pytest.mark.parametrize("shared", [0, 31, 63, 64, 127, 320, 383, 100000, -5])
-def test_less_of_a_prefix_than_there_might_be(gpu, shared):  # noqa: F811
-    """Any length is right: what is not of a whole page, or past the most, is every sequence's own; none at all is causal attention."""
-    make(gpu, "Q4_B64", 2, 128, 64, [400, 321, 330, 383, 350], None, 8500, 8, shared, most=320).check()
-    make(gpu, "Q4_B64", 2, 64, 64, [400, 321, 330], [3, 1, 2], 8501, 8, shared, most=320).check()
+@pytest.mark.parametrize("counts", [None, 2])
+@pytest.mark.parametrize("shared", [0, 31, 63, 64, 127, 320, 1023, 1024, 100000, -5])
+def test_less_of_a_prefix_than_there_might_be(gpu, shared, counts):  # noqa: F811
+    """Any length is right: what is not of a whole page, or past the most, is every sequence's own."""
+    lens = [1024 + x for x in OWN * 2]
+    s = Shared(gpu, "Q4_B64", 64, 16, 128, 64, lens, counts and [min(counts, x - 1024) for x in lens], shared, 8500, most=1024)
+    assert s.shares()
+    s.check()
 
 
-@pytest.mark.parametrize("lens,counts,n", [([300], None, 256), ([300, 290], None, 20), ([300, 290], None, 0)])
-def test_nothing_to_share(gpu, lens, counts, n):  # noqa: F811
-    """One sequence, or not a page: causal attention, bit for bit."""
-    s = make(gpu, "Q8_B64", 2, 64, 64, lens, counts, 8600, 4, n)
-    q = s.queries()
-    assert np.array_equal(s.attend(q, 0.1), Setup.attend(s, q, 0.1))
+@pytest.mark.parametrize("name,lens,counts,n", [("Q8_B64", [300], None, 256), ("Q8_B64", [300, 290], None, 20), ("Q4_B64", [300, 290], None, 0), ("Q4_B32", [300, 290], None, 256), ("Q4_B64", [600, 590, 580], [80, 3, 580 - 512], 512)])
+def test_nothing_to_share(gpu, name, lens, counts, n):  # noqa: F811
+    """One sequence, not a page, or too little for a second launch: causal attention, bit for bit."""
+    s = Shared(gpu, name, 4, 2, 64, 64, lens, counts, n, 8600)
+    assert not s.shares()
+    q = s.normal((s.n_tokens, 4, 64))
+    need = s.iflow.kv_attn_workspace_bytes(s.cache, s.batch, 4)
+    out, ws = s.torch.full_like(q, 7.0), s.torch.full((max(need, 16),), 0xFF, dtype=s.torch.uint8, device="cuda")
+    s.iflow.kv_attn(s.cache, s.batch, q, 4, 0.1, out, ws, need)
+    assert s.torch.equal(s.attend(q, 0.1), out)
+    s.compare(out, s.reference(q, 0.1))
 
 
 def test_pages_that_are_not_there(gpu):  # noqa: F811
     """A page missing in the prefix, one of a sequence's own, all of one's own, all of the prefix."""
-    s = make(gpu, "Q4_B32", 2, 64, 32, [400, 390, 370, 320], None, 8700, 8, 320)
+    s = Shared(gpu, "Q4_B32", 64, 16, 64, 32, [1024 + x for x in OWN * 3], None, 1024, 8700)
+    assert s.shares()
     s.table[:, 3] = -1
-    s.table[1, 11] = 1 << 20
-    s.table[2, 10:] = -1
+    s.table[5, 33] = 1 << 20
+    s.table[7, 32:] = -1
     s.describe()
     s.check()
-    s.table[:, :10] = -1
+    s.table[:, :32] = -2 ** 31
     s.describe()
     s.check()
 
@@ -124,24 +208,23 @@ def test_pages_that_are_not_there(gpu):  # noqa: F811
 @pytest.mark.parametrize("scale", [20.0, 2000.0])
 def test_peaked_scores(gpu, scale):  # noqa: F811
     """The largest score in the prefix or behind it, the other's sums as good as nothing.  (Scores, and what 32 bits leave of them, are as many times as large; 2^-15 is for scores of about 1.)"""
-    s = make(gpu, "Q4_B64", 2, 128, 64, [700, 600, 577, 640], None, 8800, 16, 576)
+    s = Shared(gpu, "Q4_B64", 32, 8, 128, 64, [1024 + x for x in OWN * 4], None, 1024, 8800)
+    assert s.shares()
     s.check(scale, tol=2.0 ** -11 + scale * 2.0 ** -15)
 
 
 def test_rows_of_no_token(gpu):  # noqa: F811
-    """Rows in front of, between and behind the sequences' tokens, tokens past the limits: kept as they were."""
-    s = Shared(gpu, "Q8_B64", 2, 64, 64, [250, 200, 256], None, 8900, 4, first=[2, 40, 41, 60], n_tokens=70, max_tokens=30, max_seq=256).share(128)
-    s.single = False
-    s.fill()
-    s.describe()
-    q = s.queries()
-    want = np.full((70, 4, 64), 7.0)
-    s.kv_cache.attend(s.cache, *s.args(), q, 0.125, want)
-    got = s.attend(q, 0.125)
-    untouched = (want == 7.0).all(axis=(1, 2))
-    assert untouched.sum() >= 10 and (got[untouched] == 7.0).all()
-    rms = np.sqrt(np.mean(want ** 2, axis=-1, keepdims=True))
-    assert (np.abs(got - want) / np.maximum(np.abs(want), np.maximum(rms, 1e-30))).max() <= TOL
+    """Rows in front of and behind the sequences' tokens, tokens past max_tokens and max_seq: rows of no token are kept as they were."""
+    counts = [3, 40, 1, 2] * 8
+    first = 2 + np.concatenate([[0], np.cumsum(counts)])
+    lens = np.array([1100 + c + 3 * i for i, c in enumerate(counts)])
+    s = Shared(gpu, "Q8_B64", 32, 8, 64, 64, lens, None, 1024, 8900, first=first, n_tokens=int(first[-1]) + 30, max_tokens=30, max_seq=1280)
+    assert s.shares()
+    q = s.normal((s.n_tokens, 32, 64))
+    got, want = s.attend(q, 0.125), s.reference(q, 0.125)
+    untouched = (want == 7.0).all(-1).all(-1)
+    assert int(untouched.sum()) == 2 + 30 + 8 * 10 and bool((got[untouched] == 7.0).all())
+    s.compare(got, want)
 
 
 @pytest.mark.parametrize("seed", range(12))
@@ -150,9 +233,9 @@ def test_arrays_of_any_numbers(gpu, seed):  # noqa: F811
     torch, it = gpu
     rng = np.random.default_rng(synth.BASE_SEED + 9000 + seed)
     fmt, d = it.FORMATS[FORMATS[seed % 4]], (64, 128)[seed // 4 % 2]
-    n_seqs, kv, group = int(rng.choice([2, 3, 64, 70])), int(rng.choice([1, 2, 8])), int(rng.choice([1, 4, 16]))
-    tokens, rows, most = int(rng.choice([1, 7, 300, 4000])), int(rng.choice([80, 900])), int(rng.choice([4000, 9000, 1 << 20]))
-    shared = int(rng.choice([64, 1000, 4000]))
+    n_seqs, kv, group = int(rng.choice([64, 70, 200])), int(rng.choice([8, 16])), int(rng.choice([1, 4, 16]))
+    tokens, rows, most = int(rng.choice([1, 7, 300, 4000])), int(rng.choice([280, 900])), int(rng.choice([4000, 9000, 1 << 20]))
+    shared = int(rng.choice([1024, 2000, 4000]))
     page, n_pages = 64, 50
     max_pages = -(-most // page)
     say(f"[case] kv shared: arrays of any numbers, seed {seed}: {n_seqs} sequences, {kv} x {group} heads of {d}, {tokens} tokens, {rows} rows, {most} positions, prefix {shared}")
@@ -165,6 +248,8 @@ def test_arrays_of_any_numbers(gpu, seed):  # noqa: F811
     table, first, lens, pages, length = [torch.from_numpy(a).cuda() for a in (any_of(n_seqs * max_pages, n_pages), any_of(n_seqs + 1, rows), any_of(n_seqs, most), any_of(shared // page, n_pages), any_of(1, shared))]
     if seed % 2:
         length.fill_(shared)
+    if seed % 3 == 2:
+        first = torch.sort(first.clamp(0, rows)).values.contiguous()
     cache, batch = it.kv_cache(fmt, kv, d, page, n_pages, pool), it.kv_batch(n_seqs, max_pages, table, lens, most, first, rows, tokens)
     heads = kv * group
     need = it.kv_attn_shared_workspace_bytes(cache, batch, heads, shared)
@@ -175,33 +260,47 @@ def test_arrays_of_any_numbers(gpu, seed):  # noqa: F811
     assert pool_whole() and ws_whole() and out_whole()
 
 
-def test_replays_with_other_prefixes_on_another_stream(gpu):  # noqa: F811
-    """A captured call on a stream of its own, replayed at other lengths and another prefix, with eager calls of another shape on the same workspace between; every replay against the oracle."""
+@pytest.mark.parametrize("own,counts", [(200, None), (2000, None), (200, 3)])
+def test_replays_with_other_prefixes_on_another_stream(gpu, own, counts):  # noqa: F811
+    """A captured call on a stream of its own, replayed at other lengths and another prefix, with eager calls on the same workspace between; every replay against the reference, and the eager call's bits."""
     torch, it = gpu
-    say("[case] kv shared under HIP-graph replay")
-    s = make(gpu, "Q4_B64", 4, 128, 64, [704] * 5, None, 9100, 16, 576)
+    most = 1024 + own
+    s = Shared(gpu, "Q4_B64", 32, 8, 128, 64, [most] * 64, counts and [counts] * 64, 1024, 9100)
+    assert s.shares()
     need = s.room()
-    ws, out = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda"), torch.zeros((5, 16, 128), dtype=torch.float16, device="cuda")
-    q = s.queries()
-    qd = s.dev(q)
+    ws, out = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda"), torch.zeros((s.n_tokens, 32, 128), dtype=torch.float16, device="cuda")
+    q = s.normal((s.n_tokens, 32, 128))
     stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
     stream.wait_stream(torch.cuda.current_stream())
     with torch.cuda.graph(graph, stream=stream):
-        it.kv_attn_shared(s.d_cache, s.d_batch, s.d_shared, s.d_shared_len, 576, qd, 16, 0.1, out, ws, need)
-    for lens, shared in (([577, 600, 700, 640, 576], 576), ([300, 200, 640, 195, 0], 192), ([1, 700, 2, 3, 690], 0), ([700, 701, 702, 703, 704], 576)):
-        s.lens = np.array(lens, np.int32)
+        it.kv_attn_shared(s.cache, s.batch, s.d_shared, s.d_shared_len, 1024, q, 32, 0.1, out, ws, need)
+    rng = np.random.default_rng(3)
+    for turn, shared in enumerate((1024, 192, 0, 1000, 1024)):
+        s.lens = (rng.integers(0, most + 1, 64) if turn in (1, 2) else 1024 + rng.integers(3, own + 1, 64)).astype(np.int32)
         s.d_lens.copy_(s.dev(s.lens))
         s.d_shared_len.fill_(shared)
         out.fill_(7.0)
         torch.cuda.synchronize()
         graph.replay()
         torch.cuda.synchronize()
-        got = out.cpu().numpy().astype(np.float64)
-        want = np.full((5, 16, 128), 7.0)
-        s.kv_cache.attend(s.cache, *s.args(), q, 0.1, want)
-        rms = np.maximum(np.sqrt(np.mean(want ** 2, axis=-1, keepdims=True)), 1e-30)
-        assert (np.abs(got - want) / np.maximum(np.abs(want), rms)).max() <= TOL
-        assert np.array_equal(s.attend(q, 0.1, ws=ws), got)
+        s.compare(out, s.reference(q, 0.1))
+        assert torch.equal(s.attend(q, 0.1, ws=ws), out)
+
+
+def test_two_streams_with_workspaces_of_their_own(gpu):  # noqa: F811
+    """Calls side by side, each with its own workspace: the bits of one after the other."""
+    torch, it = gpu
+    both = [Shared(gpu, name, 32, 8, 128, 64, [1024 + x for x in OWN * 4], None, 1024, 9200 + i) for i, name in enumerate(("Q4_B64", "Q8_B32"))]
+    qs = [s.normal((64, 32, 128)) for s in both]
+    want = [s.attend(q, 0.1) for s, q in zip(both, qs)]
+    outs, rooms = [torch.zeros_like(q) for q in qs], [torch.empty((s.room(),), dtype=torch.uint8, device="cuda") for s in both]
+    streams = [torch.cuda.Stream() for _ in both]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, q, out, ws, stream in zip(both, qs, outs, rooms, streams):
+            it.kv_attn_shared(s.cache, s.batch, s.d_shared, s.d_shared_len, 1024, q, 32, 0.1, out, ws, s.room(), stream=stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
 
 
 @pytest.mark.parametrize("captured", [False, True])

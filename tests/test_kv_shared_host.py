@@ -12,7 +12,7 @@ def described(iflow, cache={}, **change):  # noqa: F811
     c, b = iflow.KvCache(), iflow.KvBatch()
     for k, v in {**dict(format=iflow.Q4_B64, n_kv_heads=8, head_dim=128, page_positions=64, n_pages=100, pages=FAR), **cache}.items():
         setattr(c, k, v)
-    for k, v in {**dict(n_seqs=4, max_pages=60, page_table=AT, seq_lens=AT, first_token=AT, n_tokens=9, max_tokens=5, max_seq=3840), **change}.items():
+    for k, v in {**dict(n_seqs=40, max_pages=60, page_table=AT, seq_lens=AT, first_token=AT, n_tokens=99, max_tokens=5, max_seq=3840), **change}.items():
         setattr(b, k, v)
     return c, b
 
@@ -21,10 +21,12 @@ def test_refusals_before_any_launch(iflow):  # noqa: F811
     L = iflow.lib()
     c, b = described(iflow)
     need = iflow.kv_attn_shared_workspace_bytes(c, b, 32, 3000)
-    assert need > 9 * 32 * 130 * 4 and need % 16 == 0
-    # one sequence, less than a page: what causal attention needs
+    assert need > 99 * 32 * 130 * 4 and need != iflow.kv_attn_workspace_bytes(c, b, 32) and need % 16 == 0
+    # one sequence, less than a page, too little to share: what causal attention needs
     one = described(iflow, n_seqs=1)
     assert iflow.kv_attn_shared_workspace_bytes(*one, 32, 3000) == iflow.kv_attn_workspace_bytes(*one, 32)
+    few = described(iflow, n_seqs=3)
+    assert iflow.kv_attn_shared_workspace_bytes(*few, 32, 640) == iflow.kv_attn_workspace_bytes(*few, 32)
     assert iflow.kv_attn_shared_workspace_bytes(c, b, 32, 63) == iflow.kv_attn_shared_workspace_bytes(c, b, 32, 0) == iflow.kv_attn_workspace_bytes(c, b, 32)
 
     def call(pages=5 * AT, length=6 * AT, most=3000, q=2 * AT, heads=32, scale=0.1, out=3 * AT, ws=8 * AT, size=need, of=(c, b)):
@@ -33,9 +35,9 @@ def test_refusals_before_any_launch(iflow):  # noqa: F811
                        (dict(pages=None), iflow.ERR_NULL), (dict(length=None), iflow.ERR_NULL), (dict(q=None), iflow.ERR_NULL), (dict(out=None), iflow.ERR_NULL), (dict(ws=None), iflow.ERR_NULL),
                        (dict(size=need - 1), iflow.ERR_SIZE), (dict(pages=5 * AT + 2), iflow.ERR_ALIGN), (dict(length=6 * AT + 1), iflow.ERR_ALIGN), (dict(q=2 * AT + 2), iflow.ERR_ALIGN),
                        (dict(out=3 * AT + 8), iflow.ERR_ALIGN), (dict(ws=8 * AT + 4), iflow.ERR_ALIGN), (dict(out=2 * AT + 64), iflow.ERR_SHAPE), (dict(ws=2 * AT), iflow.ERR_SHAPE),
-                       (dict(ws=FAR + 4096), iflow.ERR_SHAPE), (dict(out=FAR), iflow.ERR_SHAPE), (dict(out=AT), iflow.ERR_SHAPE), (dict(pages=3 * AT - 4 * 45), iflow.ERR_SHAPE), (dict(length=3 * AT + 9 * 32 * 256 - 4), iflow.ERR_SHAPE),
+                       (dict(ws=FAR + 4096), iflow.ERR_SHAPE), (dict(out=FAR), iflow.ERR_SHAPE), (dict(out=AT), iflow.ERR_SHAPE), (dict(pages=3 * AT - 4 * 45), iflow.ERR_SHAPE), (dict(length=3 * AT + 99 * 32 * 256 - 4), iflow.ERR_SHAPE),
                        (dict(pages=8 * AT + need - 4), iflow.ERR_SHAPE), (dict(length=8 * AT), iflow.ERR_SHAPE), (dict(of=(None, b)), iflow.ERR_NULL), (dict(of=(c, None)), iflow.ERR_NULL),
-                       (dict(of=described(iflow, page_table=None, max_pages=25, max_seq=1600), most=1600), iflow.ERR_NULL), (dict(of=described(iflow, max_seq=3841)), iflow.ERR_SHAPE),
+                       (dict(of=described(iflow, cache=dict(n_pages=1000), page_table=None, max_pages=25, max_seq=1600), most=1600), iflow.ERR_NULL), (dict(of=described(iflow, max_seq=3841)), iflow.ERR_SHAPE),
                        (dict(of=described(iflow, seq_lens=None)), iflow.ERR_NULL), (dict(of=described(iflow, cache=dict(format=77))), iflow.ERR_FORMAT)):
         assert call(**kw) == status, kw
     size = C.c_size_t(0)
@@ -60,7 +62,7 @@ def test_extension_hands_the_call_on(iflow):  # noqa: F811
     try:
         with pytest.raises(iflow.IflowError):
             iflow.kv_attn_shared(c, b, 11, 12, 13, 14, 15, 0.25, 16, None, 17 << 40, stream=18)
-        assert seen.pop() == (100, 9, 11, 12, 13, 14, 15, 0.25, 16, None, 17 << 40, 18)
+        assert seen.pop() == (100, 99, 11, 12, 13, 14, 15, 0.25, 16, None, 17 << 40, 18)
         with pytest.raises((TypeError, ValueError, AttributeError)):
             iflow.kv_attn_shared(c, b, 11, 12, "13", 14, 15, 0.25, 16, None, 17, stream=18)
         assert not seen
