@@ -13,11 +13,13 @@
 namespace iflow {
 
 constexpr int KVT_ONE = 1024, KVT_THREADS = 1024, KVT_WAVES = KVT_THREADS / 64;
-constexpr int KVT_TOKENS = 256, KVT_PAGES = 64;               // of a wavefront at a time
+// Of a wavefront at a time: one of each lane's.  (Four tokens a lane, loads side by side, 4.9 / 6.4 / 6.5 us instead of 3.4 / 4.3 / 5.8 for 64 sequences' next tokens, a mixed step of 256, a third of a million
+// tokens of 1000 prompts: longer code, which the first wavefront of every compute unit waits for.)
+constexpr int KVT_TOKENS = 64, KVT_PAGES = 64;
 
-// What is known of all sequences: sums of tokens (null: one each), of pages taken and given back, [n_seqs + 1]; pages that they held.
+// What is known of all sequences: sums of tokens (null: one each), of pages taken and given back, [n_seqs + 1]; pages that they held, their lengths.
 struct KvSums {
-    const int32_t *tokens, *take, *give, *held;
+    const int32_t *tokens, *take, *give, *held, *lens;
     int32_t start, count, n_tokens, n_take, n_give;
 };
 // work space: {start, count, tokens, taken, given back}, then the sums
@@ -28,13 +30,14 @@ struct KvSumsSpace {
     static size_t bytes(int n) { return ((size_t)(HEAD + 3 * n + 2) * 4 + 15) / 16 * 16; }
 };
 
-struct KvWants { int tokens, held, need; };
+struct KvWants { int tokens, held, need, len; };
 __device__ __forceinline__ KvWants kvt_wants(const KvView &v, const KvTables &t, int b)
 {
     KvWants w;
     w.tokens = !v.first ? 1 : max(0, min(t.new_tokens[b], v.max_tokens));
     w.held = max(0, min(t.held[b], v.max_pages - t.n_shared));
-    const int len = max(0, min(v.lens[b], v.max_seq));
+    w.len = v.lens[b];
+    const int len = max(0, min(w.len, v.max_seq));
     w.need = max(0, v.page_of((len + KV_TILE - 1) / KV_TILE + v.tiles_per_page - 1) - t.n_shared);
     return w;
 }
@@ -83,28 +86,25 @@ __device__ __forceinline__ void kvt_new_range(const KvView &v, const KvTables &t
     t.free_out[2] = s.n_take - taken;
 }
 
-// the last of n with upto[i] <= x (upto[0] is not above x), by the whole wavefront
-__device__ __forceinline__ int kvt_find(const int32_t *upto, int n, int x)
+// the last of n with upto[i] <= x, for a lane's x of x0 .. x1 (upto[0] is not above x0): by the whole wavefront for both ends, then by each lane between them
+__device__ __forceinline__ int kvt_find(const int32_t *upto, int n, int x0, int x1, int x)
 {
     const int lane = threadIdx.x & 63;
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
-        const int m = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < hi && upto[i] <= x));
-        lo += max(0, m - 1) * step;
-        hi = min(lo + step, hi);
+    int lo0 = 0, lo1 = 0, size = n;                           // (they are below lo + size)
+    while (size > 1) {
+        const int step = (size + 63) >> 6, i0 = lo0 + lane * step, i1 = lo1 + lane * step;
+        const int at0 = upto[min(i0, n - 1)], at1 = upto[min(i1, n - 1)];
+        const bool in = lane * step < size;
+        lo0 += max(0, __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && i0 < n && at0 <= x0)) - 1) * step;
+        lo1 += max(0, __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && i1 < n && at1 <= x1)) - 1) * step;
+        size = step;
     }
-    return lo;
-}
-// ... by each lane for its own, between two
-__device__ __forceinline__ int kvt_find(const int32_t *upto, int lo, int hi, int x)
-{
-    while (hi > lo) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (upto[mid] <= x) lo = mid;
-        else hi = mid - 1;
+    const int span = lo1 - lo0;
+    for (int step = span > 0 ? 1 << (31 - __builtin_clz(span)) : 0; step > 0; step >>= 1) {
+        const int i = lo0 + step;
+        if (i <= lo1 && upto[i] <= x) lo0 = i;
     }
-    return lo;
+    return lo0;
 }
 
 // Everything but the sums, by wavefront `wave` of `waves`: the tokens' slots, pages taken, pages given back, the shared pages.  (Every number is checked against its buffer again: in a launch of
@@ -119,47 +119,40 @@ __device__ __forceinline__ void kvt_fill(const KvView &v, const KvTables &t, con
     const int64_t chunks = (int64_t)token_chunks + take_chunks + give_chunks + (int64_t)per_row * n;
     for (int64_t c = wave; c < chunks; c += waves) {
         if (c < token_chunks) {
-            const int r0 = (int)c * KVT_TOKENS, r1 = min(rows, r0 + KVT_TOKENS) - 1;
-            const int b0 = s.tokens ? kvt_find(s.tokens, n, r0) : r0, b1 = s.tokens ? kvt_find(s.tokens, n, r1) : r1;
-#pragma unroll
-            for (int i = 0; i < KVT_TOKENS / 64; ++i) {
-                const int row = r0 + 64 * i + lane;
-                if (row > r1) continue;
-                const int b = s.tokens ? kvt_find(s.tokens, b0, b1, row) : row;
-                const int p = (int)((uint32_t)v.lens[b] - (s.tokens ? (uint32_t)(s.tokens[b + 1] - row) : 1u));
-                int64_t slot = -1;
-                if ((uint32_t)p < (uint32_t)v.max_seq) {
-                    const int page_of = v.page_of(p / KV_TILE), j = page_of - t.n_shared, held = s.held[b];
-                    int page = -1;
-                    if (j < 0) page = t.shared[page_of];
-                    else if (j < held) page = table[(int64_t)b * v.max_pages + page_of];
-                    else if (s.take[b] + (j - held) < s.count) page = t.ring[kvt_ring(v, s.start, s.take[b] + (j - held))];
-                    if (page >= 0 && page < v.n_pages) slot = (int64_t)page * P + (p - page_of * P);
-                }
-                t.slots[row] = slot;
+            const int r0 = (int)c * KVT_TOKENS, r1 = min(rows, r0 + KVT_TOKENS) - 1, row = min(r0 + lane, r1), b = s.tokens ? kvt_find(s.tokens, n, r0, r1, row) : row;
+            const int p = (int)((uint32_t)s.lens[b] - (s.tokens ? (uint32_t)(s.tokens[b + 1] - row) : 1u));
+            int64_t slot = -1;
+            if ((uint32_t)p < (uint32_t)v.max_seq) {
+                const int page_of = v.page_of(p / KV_TILE), j = page_of - t.n_shared, held = s.held[b];
+                // (one load, wherever from: three in branches wait for one another)
+                const int taken = s.take[b] + (j - held);
+                const int32_t *from = j < 0 ? t.shared + page_of : j < held ? table + ((int64_t)b * v.max_pages + page_of) : taken < s.count ? t.ring + kvt_ring(v, s.start, taken) : nullptr;
+                const int page = from ? *from : -1;
+                if (page >= 0 && page < v.n_pages) slot = (int64_t)page * P + (p - page_of * P);
             }
+            if (r0 + lane <= r1) t.slots[row] = slot;
             continue;
         }
         const int64_t d = c - token_chunks;
         if (d < take_chunks) {
             const int k0 = (int)d * KVT_PAGES, k1 = min(s.n_take, k0 + KVT_PAGES) - 1, k = k0 + lane;
-            const int b0 = kvt_find(s.take, n, k0), b1 = kvt_find(s.take, n, k1);
+            const int b = kvt_find(s.take, n, k0, k1, min(k, k1));
             if (k <= k1) {
-                const int b = kvt_find(s.take, b0, b1, k), entry = t.n_shared + s.held[b] + (k - s.take[b]);
+                const int entry = t.n_shared + s.held[b] + (k - s.take[b]);
                 if (entry < v.max_pages) table[(int64_t)b * v.max_pages + entry] = k < s.count ? t.ring[kvt_ring(v, s.start, k)] : -1;
             }
         } else if (d < take_chunks + give_chunks) {
             const int k0 = (int)(d - take_chunks) * KVT_PAGES, k1 = min(s.n_give, k0 + KVT_PAGES) - 1, k = k0 + lane;
-            const int b0 = kvt_find(s.give, n, k0), b1 = kvt_find(s.give, n, k1);
+            const int b = kvt_find(s.give, n, k0, k1, min(k, k1));
             if (k <= k1 && (int64_t)s.count + k < v.n_pages) {
                 // (the last of the sequence's pages that go is its last)
-                const int b = kvt_find(s.give, b0, b1, k), entry = t.n_shared + s.held[b] - (s.give[b + 1] - k);
+                const int entry = t.n_shared + s.held[b] - (s.give[b + 1] - k);
                 if (entry >= 0 && entry < v.max_pages) t.ring[kvt_ring(v, s.start, s.count + k)] = table[(int64_t)b * v.max_pages + entry];
             }
         } else {
             const int64_t e = d - take_chunks - give_chunks;
             const int b = (int)(e / per_row), j = (int)(e - (int64_t)b * per_row) * KVT_PAGES + lane;
-            if (j < t.n_shared && v.lens[b] > 0) table[(int64_t)b * v.max_pages + j] = t.shared[j];
+            if (j < t.n_shared && s.lens[b] > 0) table[(int64_t)b * v.max_pages + j] = t.shared[j];
         }
     }
 }
@@ -167,16 +160,16 @@ __device__ __forceinline__ void kvt_fill(const KvView &v, const KvTables &t, con
 // Up to 1024 sequences: every workgroup's own sums; the first writes what is new of the sequences.
 __global__ __launch_bounds__(KVT_THREADS) void kv_tables_kernel(KvView v, KvTables t)
 {
-    __shared__ int32_t s_tokens[KVT_ONE + 1], s_take[KVT_ONE + 1], s_give[KVT_ONE + 1], s_held[KVT_ONE], s_waves[3][KVT_WAVES];
+    __shared__ int32_t s_tokens[KVT_ONE + 1], s_take[KVT_ONE + 1], s_give[KVT_ONE + 1], s_held[KVT_ONE], s_lens[KVT_ONE], s_waves[3][KVT_WAVES];
     const int b = threadIdx.x;
-    KvSums s = {v.first ? s_tokens : nullptr, s_take, s_give, s_held};
+    KvSums s = {v.first ? s_tokens : nullptr, s_take, s_give, s_held, s_lens};
     kvt_range(v, t, s.start, s.count);
-    KvWants w = {0, 0, 0};
+    KvWants w = {0, 0, 0, 0};
     if (b < v.n_seqs) w = kvt_wants(v, t, b);
     KvScan scan;
     int tokens, take, give;
     scan.step(w, s_waves, tokens, take, give);
-    if (b < v.n_seqs) { s_tokens[b] = tokens; s_take[b] = take; s_give[b] = give; s_held[b] = w.held; }
+    if (b < v.n_seqs) { s_tokens[b] = tokens; s_take[b] = take; s_give[b] = give; s_held[b] = w.held; s_lens[b] = w.len; }
     if (b == 0) { s_tokens[v.n_seqs] = scan.tokens; s_take[v.n_seqs] = scan.take; s_give[v.n_seqs] = scan.give; }
     s.n_tokens = scan.tokens; s.n_take = scan.take; s.n_give = scan.give;
     __syncthreads();                                          // (also: the lengths and states have been read before any is written)
@@ -202,13 +195,13 @@ __global__ __launch_bounds__(KVT_THREADS) void kv_tables_sums_kernel(KvView v, K
     kvt_range(v, t, s.start, s.count);
     __syncthreads();                                          // (before free_out, which may be free_state, is written)
     KvScan scan;
-    KvWants next = {0, 0, 0};
+    KvWants next = {0, 0, 0, 0};
     if ((int)threadIdx.x < v.n_seqs) next = kvt_wants(v, t, threadIdx.x);
     for (int b0 = 0, turn = 0; b0 < v.n_seqs; b0 += KVT_THREADS, turn ^= 1) {
         const int b = b0 + threadIdx.x;
         const KvWants w = next;
         if (b + KVT_THREADS < v.n_seqs) next = kvt_wants(v, t, b + KVT_THREADS);
-        else next = {0, 0, 0};
+        else next = {0, 0, 0, 0};
         int tokens, take, give;
         scan.step(w, s_waves[turn], tokens, take, give);
         if (b >= v.n_seqs) continue;
@@ -227,7 +220,7 @@ __global__ __launch_bounds__(KVT_THREADS) void kv_tables_sums_kernel(KvView v, K
 __global__ __launch_bounds__(256) void kv_tables_fill_kernel(KvView v, KvTables t, void *ws)
 {
     const KvSumsSpace from(ws, v.n_seqs);
-    const KvSums s = {v.first, from.take, from.give, from.held, from.head[0], from.head[1], from.head[2], from.head[3], from.head[4]};
+    const KvSums s = {v.first, from.take, from.give, from.held, v.lens, from.head[0], from.head[1], from.head[2], from.head[3], from.head[4]};
     kvt_fill(v, t, s, __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), gridDim.x * 4);
 }
 
@@ -236,7 +229,8 @@ static int64_t kvt_chunks(const KvView &v, const KvTables &t)
 {
     return (v.n_tokens + KVT_TOKENS - 1) / KVT_TOKENS + (int64_t)v.n_seqs * ((t.n_shared + KVT_PAGES - 1) / KVT_PAGES) + (v.n_tokens / (v.tiles_per_page * KV_TILE) + v.n_seqs) / KVT_PAGES;
 }
-constexpr int KVT_ALONE = 4 * KVT_WAVES;                      // chunks that one workgroup does by itself where more may not
+// Chunks that one workgroup does by itself where more may not (us, in place: 1392 tokens of 64 sequences 4.0, 1901 of 256 5.2, 3753 of 64 5.7; two launches 5.8 to 6.6, 2277 to 6871 tokens).
+constexpr int KVT_ALONE = 4 * KVT_WAVES;
 
 size_t kv_tables_workspace_bytes(const KvView &v) { return KvSumsSpace::bytes(v.n_seqs); }
 
