@@ -1127,13 +1127,14 @@ struct KvPlan {
     int rows, few, direct;
     bool packed, sixteens;
     int64_t blocks, lines;                                    // at most: blocks of `rows` rows of a key/value head if packed; lines of sixteen rows
-    // `seen`: positions that a token sees, at most
-    KvPlan(const KvView &v, int head_dim, int n_heads, int64_t seen)
+    // `seen`: positions that a token sees, at most; `blocks_of_rows`: of a workgroup that decodes for many, where the caller's rule says (-1: the one above)
+    KvPlan(const KvView &v, int head_dim, int n_heads, int64_t seen, int blocks_of_rows = -1)
     {
         const int64_t group = n_heads / v.n_kv_heads, most = v.max_tokens * group, all = v.n_tokens * group, seqs = v.n_seqs, kv = v.n_kv_heads;
         packed = seqs > 1 && 2 * v.n_tokens < seqs * v.max_tokens;
         auto blocks_of = [&](int n) { return packed ? kv * (all / n) : seqs * kv * ((most + n - 1) / n); };
         rows = most < 64 || blocks_of(64) < (seqs == 1 ? 128 : 256) ? 0 : blocks_of(128) >= 512 ? 128 : 64;
+        if (blocks_of_rows >= 0) rows = most < 64 ? 0 : blocks_of_rows;
         few = rows && packed ? KVA_FEW : 0;
         sixteens = !rows || few;
         blocks = rows ? all / rows + std::min(seqs, all / KVA_FEW) : 0;
@@ -1198,11 +1199,10 @@ hipError_t kv_attn_by_blocks(int format, int head_dim, const KvView &v, const ui
 
 // All of a call's launches.
 template <typename SEES>
-hipError_t kv_attn_launches(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace, hipStream_t s, int64_t seen, SEES sees)
+hipError_t kv_attn_launches(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace, hipStream_t s, int64_t seen, const KvPlan &plan, SEES sees)
 {
     const int group = n_heads / v.n_kv_heads;
     const float scale_log2e = scale * 1.4426950408889634f;
-    const KvPlan plan(v, head_dim, n_heads, seen);
     if (plan.rows) {
         const int64_t blocks = ((int64_t)v.max_tokens * group + plan.rows - 1) / plan.rows;      // (at most 2^22 rows: 32768)
         const dim3 grid = plan.packed ? kv_numbered(plan.blocks * v.n_kv_heads) : dim3((unsigned)v.n_kv_heads, (unsigned)blocks, (unsigned)v.n_seqs);

@@ -11,7 +11,7 @@ size_t kv_attn_workspace_bytes(const KvView &v, int head_dim, int n_heads)
 
 hipError_t launch_kv_attn(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale, uint16_t *out, void *workspace, hipStream_t s)
 {
-    return kv_attn_launches(format, head_dim, v, q, n_heads, scale, out, workspace, s, v.max_seq, KvSeesAll{});
+    return kv_attn_launches(format, head_dim, v, q, n_heads, scale, out, workspace, s, v.max_seq, KvPlan(v, head_dim, n_heads, v.max_seq), KvSeesAll{});
 }
 
 hipError_t launch_kv_attn_blocks(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale, uint16_t *out, int rows, int few, hipStream_t s)

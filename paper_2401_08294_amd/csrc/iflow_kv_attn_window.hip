@@ -13,17 +13,31 @@ static int64_t kv_window_seen(const KvView &v, int n_heads, int window, int sink
 // a window, or first positions, that no sequence is longer than: causal attention
 static bool kv_window_is_all(const KvView &v, int window, int sinks) { return window >= v.max_seq || sinks >= v.max_seq; }
 
+// Blocks of rows, or sixteens: a window's tiles are few, and what a block of rows takes to begin and end counts for more than in causal attention; sixteens leave no row of a single head's tokens empty.  By
+// the rows that there are (padded, a batch of a long prompt and short ones would seem to be many).  Us, by sixteens / 64 rows / 128 rows, windows of 64, 512 and 2048:
+//   32/8 heads x 128, 4 bits    128 blocks of 64 rows: 7 / 13 / 16, 13 / 18 / 27, 25 / 29 / 48    296: 14 / 31 / 22, 25 / 44 / 36, 42 / 46 / 57    504: 17 / 26 / 17, 37 / 37 / 30, 90 / 73 / 69
+//                               1064: 37 / 58 / 36, 75 / 85 / 63, 176 / 147 / 111                 2000: 58 / 96 / 43, 129 / 136 / 82, 348 / 285 / 218
+//   64/8 x 64, 4 bits           256: 10 / 11 / 13, 16 / 14 / 23, 27 / 20 / 41    576: 21 / 30 / 21, 32 / 42 / 36, 47 / 49 / 48    1000: 32 / 35 / 17, 51 / 49 / 32, 112 / 89 / 72    4000: 123 / 132 / 57, 192 / 181 / 109, 431 / 360 / 276
+//   32/32 x 128, 8 bits         352: 15 / 22 / 37, 27 / 32 / 56, 45 / 46 / 89    512: 21 / 27 / 35, 39 / 41 / 52, 102 / 85 / 110    1088: 42 / 65 / 58, 78 / 92 / 93, 193 / 173 / 141    2208: 78 / 115 / 82, 147 / 171 / 139, 417 / 337 / 278
+static KvPlan kv_window_plan(const KvView &v, int head_dim, int n_heads, int window, int sinks)
+{
+    const int64_t seen = kv_window_seen(v, n_heads, window, sinks), rows = v.n_tokens * n_heads;          // (of all key/value heads)
+    const bool bits8 = v.page_bytes > (int64_t)v.n_kv_heads * v.tiles_per_page * 50 * head_dim, wide = seen > 1280;
+    const int64_t fills = !bits8 ? 240 : wide ? 500 : 900;
+    return KvPlan(v, head_dim, n_heads, seen, rows / 128 >= fills ? 128 : wide && rows / 64 >= (head_dim == 64 ? 256 : 450) ? 64 : 0);
+}
+
 size_t kv_attn_window_workspace_bytes(const KvView &v, int head_dim, int n_heads, int window, int sinks)
 {
     if (kv_window_is_all(v, window, sinks)) return kv_attn_workspace_bytes(v, head_dim, n_heads);
-    const KvPlan plan(v, head_dim, n_heads, kv_window_seen(v, n_heads, window, sinks));
+    const KvPlan plan = kv_window_plan(v, head_dim, n_heads, window, sinks);
     return plan.sixteens && !plan.direct ? KvPartial::bytes(v.n_seqs, head_dim) : 0;
 }
 
 hipError_t launch_kv_attn_window(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, int window, int sinks, float scale, uint16_t *out, void *workspace, hipStream_t s)
 {
     if (kv_window_is_all(v, window, sinks)) return launch_kv_attn(format, head_dim, v, q, n_heads, scale, out, workspace, s);
-    return kv_attn_launches(format, head_dim, v, q, n_heads, scale, out, workspace, s, kv_window_seen(v, n_heads, window, sinks), KvSeesWindow{window, sinks});
+    return kv_attn_launches(format, head_dim, v, q, n_heads, scale, out, workspace, s, kv_window_seen(v, n_heads, window, sinks), kv_window_plan(v, head_dim, n_heads, window, sinks), KvSeesWindow{window, sinks});
 }
 
 }  // namespace iflow

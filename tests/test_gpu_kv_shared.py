@@ -40,11 +40,14 @@ class Shared:
         size = it.kv_cache_bytes(it.kv_cache(self.fmt, n_kv, d, page, n_pages))
         self.pool = torch.randint(0, 256, (size,), dtype=torch.uint8, device="cuda", generator=self.g)
         self.cache = it.kv_cache(self.fmt, n_kv, d, page, n_pages, self.pool)
-        # the prefix by one sequence that has it, then everybody's positions behind it (in the cache's own 16 bits after rotation, as a program appends them)
-        whole = self.max_shared // page * page
+        self.fill()
+        self.describe()
+
+    def fill(self):
+        """The prefix by one sequence that has it, then everybody's positions behind it."""
+        whole = self.max_shared // self.page * self.page
         self.append(self.table[:1], [max(whole, 1)], [max(whole, 1)])
         self.append(self.table, np.maximum(self.lens, 0), np.maximum(0, self.lens - whole))
-        self.describe()
 
     def dev(self, a):
         return self.torch.from_numpy(np.ascontiguousarray(a)).cuda()
@@ -86,8 +89,8 @@ class Shared:
         torch.cuda.synchronize()
         return out
 
-    def reference(self, q, scale):
-        """Causal attention in 64 bits over what the cache reads back, whose bits are the oracle's (test_gpu_kv.py)."""
+    def reference(self, q, scale, window=1 << 30, sinks=0):
+        """Causal attention, through a window, in 64 bits over what the cache reads back, whose bits are the oracle's (test_gpu_kv.py)."""
         torch, group = self.torch, self.n_heads // self.n_kv
         lens = np.clip(self.lens, 0, self.max_seq)
         batch, first, n = self.batch_of(self.table, lens, lens)
@@ -104,8 +107,10 @@ class Shared:
             Q = q[row:row + kept].double().transpose(0, 1).reshape(self.n_kv, group * kept, self.d)              # rows: head of the group, token
             score = scale * torch.matmul(Q, K.transpose(1, 2).contiguous()).view(self.n_kv, group, kept, -1)
             at = int(self.lens[b]) - count + torch.arange(kept, device="cuda").unsqueeze(1)
-            seen = (torch.arange(int(lens[b]), device="cuda") <= at) & there
+            place = torch.arange(int(lens[b]), device="cuda")
+            seen = (place <= at) & ((place > at - window) | (place < sinks)) & there
             score = score.masked_fill(~seen, float("-inf"))
+            V = torch.where(seen.any(0).unsqueeze(1), V, 0.0)  # (what no token sees may be no number)
             weight = torch.softmax(score, -1).nan_to_num(0.0) if score.shape[-1] else score                      # (nothing seen: zeros)
             out[row:row + kept] = torch.matmul(weight.reshape(self.n_kv, group * kept, -1), V).view(self.n_heads, kept, self.d).transpose(0, 1)
         return out

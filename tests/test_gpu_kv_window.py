@@ -11,6 +11,7 @@ import pytest
 
 from paper_2401_08294_amd import synth
 from test_gpu_kv import FORMATS, Setup, _guarded
+from test_gpu_kv_shared import Shared
 from test_gpu_parity import gpu, say  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -111,10 +112,57 @@ def test_prompts_that_fill_the_device(gpu, name, n_heads, d, lens, counts, windo
 @pytest.mark.parametrize("name,n_heads,d,lens,counts", [("Q4_B64", 64, 64, [400], [129]), ("Q4_B32", 64, 64, [129], [129]), ("Q8_B32", 128, 64, [700], [70]), ("Q8_B64", 64, 64, [330, 65], [65, 65]),
                                                        ("Q4_B64", 64, 128, [300], [130]), ("Q4_B32", 128, 128, [290], [90]), ("Q8_B32", 64, 128, [600], [65]), ("Q8_B64", 64, 128, [200, 1], [129, 1])])
 @pytest.mark.parametrize("window,sinks", [(2, 1), (64, 0), (97, 33)])
-def test_prompts_in_blocks_of_64(gpu, name, n_heads, d, lens, counts, window, sinks):  # noqa: F811
-    """Fewer blocks than fill the device twice: 64 rows, whose positions four groups of wavefronts share."""
+def test_prompts_of_some_hundred_rows(gpu, name, n_heads, d, lens, counts, window, sinks):  # noqa: F811
+    """Too few rows for blocks of them: by sixteens, of a head's tokens."""
     s = make(gpu, name, 64, d, 96, lens, counts, 7400 + n_heads + d, n_heads, window, sinks)
     s.check(s.queries(), d ** -0.5)
+
+
+class Long(Shared):
+    """Longer sequences, filled and checked on the device; what no token sees is left as the pool came."""
+
+    def __init__(self, gpu, name, n_heads, n_kv, d, page, lens, counts, window, sinks, seed):  # noqa: F811
+        self.window, self.sinks = window, sinks
+        say(f"[case] kv window of {window} and the first {sinks}:")
+        super().__init__(gpu, name, n_heads, n_kv, d, page, lens, counts, 0, seed)
+
+    def fill(self):
+        counts = np.ones(len(self.lens), int) if self.single else np.diff(self.first)
+        self.append(self.table, np.minimum(self.lens, self.sinks), np.where(counts > 0, np.minimum(self.lens, self.sinks), 0))
+        self.append(self.table, self.lens, np.where(counts > 0, np.minimum(self.lens, counts - 1 + self.window), 0))
+
+    def attend(self, q, scale):
+        torch = self.torch
+        need = self.iflow.kv_attn_window_workspace_bytes(self.cache, self.batch, self.n_heads, self.window, self.sinks)
+        ws, out = torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda"), torch.full((self.n_tokens, self.n_heads, self.d), 7.0, dtype=torch.float16, device="cuda")
+        self.iflow.kv_attn_window(self.cache, self.batch, q, self.n_heads, self.window, self.sinks, scale, out, ws, need)
+        torch.cuda.synchronize()
+        return out
+
+    def check(self):
+        q = self.normal((self.n_tokens, self.n_heads, self.d))
+        self.compare(self.attend(q, self.d ** -0.5), self.reference(q, self.d ** -0.5, self.window, self.sinks), TOL)
+
+
+@pytest.mark.parametrize("name,n_heads,n_kv,d,lens,counts", [
+    # blocks of 64 rows
+    ("Q4_B64", 64, 64, 64, [1700], [270]), ("Q8_B32", 128, 64, 64, [1500, 1600], [150, 3]), ("Q4_B32", 64, 64, 128, [1800], [460]), ("Q8_B64", 32, 8, 128, [2000, 1700, 10], [800, 200, 10]),
+    ("Q4_B32", 71, 1, 64, [1900, 1], [300, 1]), ("Q4_B64", 32, 4, 128, [3000, 400, 1350], [500, 400, 9]),
+    # of 128
+    ("Q4_B64", 64, 8, 128, [2500, 1500], [400, 200]), ("Q8_B64", 64, 8, 128, [3000], [1100]), ("Q8_B32", 128, 64, 64, [1700, 1400, 300], [300, 250, 0]), ("Q4_B32", 71, 1, 64, [2000, 1305], [300, 140]),
+    # by sixteens, in parts and not
+    ("Q8_B64", 8, 8, 128, [2000, 1800], [64, 9]), ("Q4_B64", 16, 2, 64, [2700], [40])])
+@pytest.mark.parametrize("window,sinks", [(1290, 0), (1313, 5), (1300, 129)])
+def test_wide_windows_of_many_tokens(gpu, name, n_heads, n_kv, d, lens, counts, window, sinks):  # noqa: F811
+    Long(gpu, name, n_heads, n_kv, d, 64, lens, counts, window, sinks, 7450 + n_heads + d).check()
+
+
+@pytest.mark.parametrize("name,n_heads,n_kv,d,lens,counts", [("Q8_B32", 64, 8, 64, [1900], [1850]), ("Q8_B64", 64, 8, 128, [1500, 2000], [1000, 900]), ("Q4_B64", 64, 8, 128, [4000, 2000], [4000, 77]),
+                                                            ("Q4_B32", 32, 32, 64, [1500, 700, 3], [1000, 1, 3]), ("Q4_B64", 64, 8, 64, [700] + [90 + i for i in range(80)], [600] + [1 + i % 3 for i in range(80)])])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (77, 4), (500, 33)])
+def test_prompts_of_many_blocks(gpu, name, n_heads, n_kv, d, lens, counts, window, sinks):  # noqa: F811
+    """More blocks than the device holds at once; long prompts beside sequences of a few tokens."""
+    Long(gpu, name, n_heads, n_kv, d, 128, lens, counts, window, sinks, 7480 + n_heads + d).check()
 
 
 @pytest.mark.parametrize("lens,counts,window", [([700, 33], None, 900), ([2000], None, 2000), ([300, 60], [130, 60], 300)])
