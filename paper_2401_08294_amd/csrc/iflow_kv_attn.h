@@ -850,12 +850,21 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
                 bool low = false;
                 if constexpr (SEES::LOW) low = sees.hides(p0, limit_of_wave);
                 if (there && p0 + KV_TILE <= shortest && !low) continue;
-                int from = p0 + 4 * hf;
+                int from = p0 + 4 * hf, seen = there ? limit : 0;
                 asm volatile("" : "+v"(from));                // (else the compiler keeps 16 positions in registers through the steps)
+                if constexpr (SEES::LOW) {
+                    if (there && p0 >= sees.sinks) {          // behind the first positions: what is not of the window, in one comparison
+                        const int after = from - (limit - sees.window);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if ((uint32_t)(after + 16 * ((e >> 2) & 1) + 8 * (e >> 3) + (e & 3)) >= (uint32_t)sees.window) sacc[tl][e] = -INFINITY;
+                        continue;
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int p = from + 16 * ((e >> 2) & 1) + 8 * (e >> 3) + (e & 3);
-                    bool hidden = !there || p >= limit;
+                    bool hidden = p >= seen;
                     if constexpr (SEES::LOW) hidden = hidden || sees.hidden(p, limit);
                     if (hidden) sacc[tl][e] = -INFINITY;
                 }

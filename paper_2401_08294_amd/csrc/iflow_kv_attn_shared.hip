@@ -39,7 +39,7 @@ struct KvSharedPlan {
         tail.lines = seqs * kv * pieces(big ? std::min<int64_t>(most, KVA_FEW - 1) : most);
         if (tail.packed) tail.lines = std::min(tail.lines, kv * (all / KVA_ROWS + seqs));
         const int64_t behind = std::max<int64_t>(1, v.max_seq - max_shared);
-        tail.direct = head_dim == 64 || tail.lines < 256 ? 8 : 4;
+        tail.direct = head_dim == 64 || tail.lines <= 256 ? 8 : 4;
         if (tail.lines * ((v.max_seq + KV_TILE - 1) / KV_TILE) <= (1LL << 30) && behind > (tail.lines >= 256 ? 2560 : head_dim == 64 ? 1024 : 768)) tail.direct = 0;
         // (of the sequences beside big ones one token each is expected)
         const int64_t lines = big ? seqs * kv * pieces(group) : tail.lines, together = big ? (seqs * group + ROWS - 1) / ROWS : blocks;

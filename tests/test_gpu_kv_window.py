@@ -93,7 +93,7 @@ def test_several_tokens(gpu, name, n_heads, n_kv, d, lens, counts, window, sinks
 
 @pytest.mark.parametrize("name,n_heads,n_kv,d,lens,counts,window,sinks", [
     ("Q4_B64", 8, 2, 128, [2100, 5, 1900, 0, 1024], None, 1500, 4), ("Q8_B64", 4, 4, 128, [2300], None, 1300, 0), ("Q4_B32", 40, 2, 64, [3000, 1, 1700], [2, 1, 2], 1200, 65),
-    ("Q8_B32", 3, 1, 64, [2500, 1281], None, 1281, 33), ("Q4_B32", 5, 1, 128, [40] * 66 + [2500, 33], None, 1000, 4), ("Q4_B64", 16, 1, 128, [9000], None, 4001, 4), ("Q4_B64", 16, 1, 128, [3000, 2000], [40, 9], 900, 4)])
+    ("Q8_B32", 3, 1, 64, [2500, 1281], None, 1281, 33), ("Q4_B32", 5, 1, 128, [40] * 66 + [4500, 33], None, 4200, 4), ("Q4_B64", 16, 1, 128, [9000], None, 4001, 4), ("Q4_B64", 16, 1, 128, [3000, 2000], [40, 9], 1400, 4)])
 def test_parts_of_long_lines(gpu, name, n_heads, n_kv, d, lens, counts, window, sinks):  # noqa: F811
     """Windows that are cut and merged, among sequences shorter than them; more sequences than a wavefront has lanes."""
     s = make(gpu, name, n_kv, d, 64, lens, counts, 7200 + n_heads, n_heads, window, sinks)
@@ -251,10 +251,10 @@ def test_replays_at_other_lengths_on_another_stream(gpu):  # noqa: F811
     """A captured call, replayed while the lengths grow past the window, with eager work between; every replay against the oracle and the eager call."""
     torch, it = gpu
     say("[case] kv window under HIP-graph replay")
-    s = Window(gpu, "Q4_B64", 4, 128, 64, [1500, 1500, 1500], None, 8000, 16, max_seq=1536).narrow(900, 5)
+    s = Window(gpu, "Q4_B64", 4, 128, 64, [1500, 1500, 1500], None, 8000, 16, max_seq=1536).narrow(1300, 5)
     s.fill()
     s.describe()
-    need = it.kv_attn_window_workspace_bytes(s.d_cache, s.d_batch, 16, 900, 5)
+    need = it.kv_attn_window_workspace_bytes(s.d_cache, s.d_batch, 16, 1300, 5)
     assert need > 0
     ws, out = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda"), torch.zeros((3, 16, 128), dtype=torch.float16, device="cuda")
     q = s.queries()
@@ -262,7 +262,7 @@ def test_replays_at_other_lengths_on_another_stream(gpu):  # noqa: F811
     stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
     stream.wait_stream(torch.cuda.current_stream())
     with torch.cuda.graph(graph, stream=stream):
-        it.kv_attn_window(s.d_cache, s.d_batch, qd, 16, 900, 5, 0.1, out, ws, need)
+        it.kv_attn_window(s.d_cache, s.d_batch, qd, 16, 1300, 5, 0.1, out, ws, need)
     for lens in ([3, 900, 1500], [905, 906, 0], [1499, 1, 930], [1500, 1400, 33]):
         s.lens = np.array(lens, np.int32)
         s.d_lens.copy_(s.dev(s.lens))
@@ -271,7 +271,7 @@ def test_replays_at_other_lengths_on_another_stream(gpu):  # noqa: F811
         graph.replay()
         torch.cuda.synchronize()
         want = np.full((3, 16, 128), 7.0)
-        s.kv_cache.attend(s.cache, *s.args(), q, 0.1, want, window=900, sinks=5)
+        s.kv_cache.attend(s.cache, *s.args(), q, 0.1, want, window=1300, sinks=5)
         got = out.cpu().numpy().astype(np.float64)
         rms = np.maximum(np.sqrt(np.mean(want ** 2, axis=-1, keepdims=True)), 1e-30)
         assert (np.abs(got - want) / np.maximum(np.abs(want), rms)).max() <= TOL
