@@ -88,6 +88,26 @@ __device__ __forceinline__ int wave_scan(int x)
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);       // row_bcast:31 into rows 2 and 3
     return x;
 }
+// the last of n with upto[i] <= x, for a lane's x of x0 .. x1 (upto in order, upto[0] not above x0; otherwise any of the n): by the whole wavefront for both ends, then by each lane between them
+__device__ __forceinline__ int kv_last_of(const int32_t *upto, int n, int x0, int x1, int x)
+{
+    const int lane = threadIdx.x & 63;
+    int lo0 = 0, lo1 = 0, size = n;                           // (they are below lo + size)
+    while (size > 1) {
+        const int step = (size + 63) >> 6, i0 = lo0 + lane * step, i1 = lo1 + lane * step;
+        const int at0 = upto[min(i0, n - 1)], at1 = upto[min(i1, n - 1)];
+        const bool in = lane * step < size;
+        lo0 += max(0, __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && i0 < n && at0 <= x0)) - 1) * step;
+        lo1 += max(0, __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && i1 < n && at1 <= x1)) - 1) * step;
+        size = step;
+    }
+    const int span = lo1 - lo0;
+    for (int step = span > 0 ? 1 << (31 - __builtin_clz(span)) : 0; step > 0; step >>= 1) {
+        const int i = lo0 + step;
+        if (i <= lo1 && upto[i] <= x) lo0 = i;
+    }
+    return lo0;
+}
 // Number w of all sequences' units, units(b) of each, in order: whose it is (b), and which of that sequence's (w); false past the last.  By every wavefront alike, 64 sequences at a time.
 // For batches whose longest sequence has many more tokens than most, where a grid of max_tokens for each would be workgroups with nothing to do.
 template <typename Units> __device__ __forceinline__ bool kv_find(const KvView &v, int &w, int &b, Units units)

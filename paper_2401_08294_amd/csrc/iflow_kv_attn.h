@@ -597,13 +597,19 @@ struct KvCallRows {
     __device__ __forceinline__ bool has_row(int i) const { return i < count; }
     __device__ __forceinline__ int sees(int) const { return part; }
 };
-// PREFIX: the w-th of all tokens that share the prefix, those of sequences of less than `few` rows in order, each lane its own: its row in the call's arrays (-1: there is none) and what it sees
+// PREFIX: the w-th of all tokens that share the prefix, each lane its own, in order from lane 0 to 31: its row in the call's arrays (-1: there is none) and what it sees.  Where sequences of `few` rows and
+// more are served otherwise, the others' tokens are counted; else a row is a token's, and its sequence the last that begins at or in front of it.
 struct KvToken { int row, limit; };
 __device__ __forceinline__ KvToken kv_token(const KvView &v, int w, int group, int few)
 {
     if (!v.first) {                                           // one each
         if (w >= v.n_seqs) return {-1, 0};
         return {w, KvSequence(v, w).sees(0)};
+    }
+    if (few == 0x7fffffff) {
+        const KvSequence seq(v, kv_last_of(v.first, v.n_seqs, __builtin_amdgcn_readlane(w, 0), __builtin_amdgcn_readlane(w, 31), w));
+        const int i = (int)((uint32_t)w - (uint32_t)seq.row);
+        return {seq.has_row(i) ? w : -1, seq.sees(i)};
     }
     const int lane = threadIdx.x & 63;
     KvToken token = {-1, 0};

@@ -44,7 +44,7 @@ struct KvSharedPlan {
         // (of the sequences beside big ones one token each is expected)
         const int64_t lines = big ? seqs * kv * pieces(group) : tail.lines, together = big ? (seqs * group + ROWS - 1) / ROWS : blocks;
         const int64_t saved = (10 * lines - 13 * together * kv) * tiles * (head_dim + 64) / (10 * 192);
-        alone = seqs < 2 || all > (1 << 21) || tiles < 2 * PART || saved < (tail.direct ? LEAST : LEAST_CUT);
+        alone = seqs < 2 || all > (1 << 21) || v.n_tokens * n_heads > (1 << 22) || tiles < 2 * PART || saved < (tail.direct ? LEAST : LEAST_CUT);
     }
     size_t prefix_bytes(int64_t n_rows, int head_dim) const { return (size_t)parts * n_rows * (head_dim + 2) * 4 + 32; }      // (the values behind the others, 16-byte aligned)
 };

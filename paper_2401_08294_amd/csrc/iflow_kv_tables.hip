@@ -86,27 +86,6 @@ __device__ __forceinline__ void kvt_new_range(const KvView &v, const KvTables &t
     t.free_out[2] = s.n_take - taken;
 }
 
-// the last of n with upto[i] <= x, for a lane's x of x0 .. x1 (upto[0] is not above x0): by the whole wavefront for both ends, then by each lane between them
-__device__ __forceinline__ int kvt_find(const int32_t *upto, int n, int x0, int x1, int x)
-{
-    const int lane = threadIdx.x & 63;
-    int lo0 = 0, lo1 = 0, size = n;                           // (they are below lo + size)
-    while (size > 1) {
-        const int step = (size + 63) >> 6, i0 = lo0 + lane * step, i1 = lo1 + lane * step;
-        const int at0 = upto[min(i0, n - 1)], at1 = upto[min(i1, n - 1)];
-        const bool in = lane * step < size;
-        lo0 += max(0, __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && i0 < n && at0 <= x0)) - 1) * step;
-        lo1 += max(0, __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && i1 < n && at1 <= x1)) - 1) * step;
-        size = step;
-    }
-    const int span = lo1 - lo0;
-    for (int step = span > 0 ? 1 << (31 - __builtin_clz(span)) : 0; step > 0; step >>= 1) {
-        const int i = lo0 + step;
-        if (i <= lo1 && upto[i] <= x) lo0 = i;
-    }
-    return lo0;
-}
-
 // Everything but the sums, by wavefront `wave` of `waves`: the tokens' slots, pages taken, pages given back, the shared pages.  (Every number is checked against its buffer again: in a launch of
 // its own the lengths may be others than the sums were made of, where another stream changes them.)
 __device__ __forceinline__ void kvt_fill(const KvView &v, const KvTables &t, const KvSums &s, int wave, int waves)
@@ -119,7 +98,7 @@ __device__ __forceinline__ void kvt_fill(const KvView &v, const KvTables &t, con
     const int64_t chunks = (int64_t)token_chunks + take_chunks + give_chunks + (int64_t)per_row * n;
     for (int64_t c = wave; c < chunks; c += waves) {
         if (c < token_chunks) {
-            const int r0 = (int)c * KVT_TOKENS, r1 = min(rows, r0 + KVT_TOKENS) - 1, row = min(r0 + lane, r1), b = s.tokens ? kvt_find(s.tokens, n, r0, r1, row) : row;
+            const int r0 = (int)c * KVT_TOKENS, r1 = min(rows, r0 + KVT_TOKENS) - 1, row = min(r0 + lane, r1), b = s.tokens ? kv_last_of(s.tokens, n, r0, r1, row) : row;
             const int p = (int)((uint32_t)s.lens[b] - (s.tokens ? (uint32_t)(s.tokens[b + 1] - row) : 1u));
             int64_t slot = -1;
             if ((uint32_t)p < (uint32_t)v.max_seq) {
@@ -136,14 +115,14 @@ __device__ __forceinline__ void kvt_fill(const KvView &v, const KvTables &t, con
         const int64_t d = c - token_chunks;
         if (d < take_chunks) {
             const int k0 = (int)d * KVT_PAGES, k1 = min(s.n_take, k0 + KVT_PAGES) - 1, k = k0 + lane;
-            const int b = kvt_find(s.take, n, k0, k1, min(k, k1));
+            const int b = kv_last_of(s.take, n, k0, k1, min(k, k1));
             if (k <= k1) {
                 const int entry = t.n_shared + s.held[b] + (k - s.take[b]);
                 if (entry < v.max_pages) table[(int64_t)b * v.max_pages + entry] = k < s.count ? t.ring[kvt_ring(v, s.start, k)] : -1;
             }
         } else if (d < take_chunks + give_chunks) {
             const int k0 = (int)(d - take_chunks) * KVT_PAGES, k1 = min(s.n_give, k0 + KVT_PAGES) - 1, k = k0 + lane;
-            const int b = kvt_find(s.give, n, k0, k1, min(k, k1));
+            const int b = kv_last_of(s.give, n, k0, k1, min(k, k1));
             if (k <= k1 && (int64_t)s.count + k < v.n_pages) {
                 // (the last of the sequence's pages that go is its last)
                 const int entry = t.n_shared + s.held[b] - (s.give[b + 1] - k);

@@ -132,7 +132,7 @@ OWN = [0, 1, 31, 32, 33, 100, 64, 200, 5, 300, 2, 77, 96, 95, 128, 11]
 
 @pytest.mark.parametrize("name", FORMATS)
 @pytest.mark.parametrize("n_heads,n_kv,d,n,shared,page", [(32, 8, 128, 64, 1024, 64), (71, 1, 64, 40, 4064, 32), (32, 32, 128, 16, 1056, 96), (64, 64, 64, 13, 1024, 256), (128, 8, 128, 17, 4128, 32), (64, 8, 64, 33, 2048, 128),
-                                                        (12, 4, 128, 160, 512, 64)])
+                                                        (12, 4, 128, 160, 512, 64), (8, 8, 64, 1500, 512, 32)])
 def test_one_token_each(gpu, name, n_heads, n_kv, d, n, shared, page):  # noqa: F811
     """Own positions of none, one, a tile and more; sequences that have ended, and ones that are inside the prefix; prefixes of one part and of several, tiles of an odd number."""
     own = (OWN * 10)[:n - 4]
@@ -142,7 +142,7 @@ def test_one_token_each(gpu, name, n_heads, n_kv, d, n, shared, page):  # noqa: 
 
 
 @pytest.mark.parametrize("name,n_heads,n_kv,d,n,most,shared", [("Q4_B64", 32, 8, 128, 40, 5, 2048), ("Q4_B32", 71, 1, 64, 24, 4, 2080), ("Q8_B32", 32, 32, 128, 12, 8, 1024), ("Q8_B64", 64, 8, 64, 20, 17, 1536),
-                                                              ("Q4_B64", 40, 8, 128, 9, 60, 2048), ("Q8_B64", 12, 4, 128, 30, 31, 1056)])
+                                                              ("Q4_B64", 40, 8, 128, 9, 60, 2048), ("Q8_B64", 12, 4, 128, 30, 31, 1056), ("Q4_B64", 16, 4, 64, 700, 3, 1024)])
 def test_several_tokens(gpu, name, n_heads, n_kv, d, n, most, shared):  # noqa: F811
     """Drafts and chunks behind the prefix, of different numbers of tokens, of none."""
     counts = [(7 * i * i + 3 * i) % (most + 1) for i in range(n - 1)] + [most]
