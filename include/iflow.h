@@ -380,8 +380,9 @@ iflow_status_t iflow_kv_attn_window(const iflow_kv_cache_t *cache, const iflow_k
 /* iflow_kv_attn for a batch whose sequences begin with the same positions (an instruction, a document), in the same pages: these are read once for the tokens of all sequences, not once for each.
  *   shared_pages [max_shared / page_positions], device int32: the prefix's pages.  shared_len, device int32: how many positions it has, read when the kernels run, at most max_shared; only whole pages
  *   count, what is left over of a page is read as every sequence's own.  0 <= max_shared <= max_seq.
- * All its positions have been written (a token inside the prefix weighs what lies behind it with zeros).  Every sequence that has tokens in the call has these pages in its row of page_table (which must not be null), entries 0 .. shared_len / page_positions - 1: where a row has others it is unspecified
- * which of the two a token sees.  (iflow_kv_tables writes such rows.)  A token at a position inside the prefix sees it up to its own position.
+ * All its positions have been written (a token inside the prefix weighs what lies behind it with zeros).  Every sequence that has tokens in the call has these pages in its row of page_table (which
+ * must not be null), entries 0 .. shared_len / page_positions - 1: where a row has others it is unspecified which of the two a token sees.  (iflow_kv_tables writes such rows.)  A token at a position
+ * inside the prefix sees it up to its own position.
  * Everything else, the result among it, as for iflow_kv_attn: the sums of the prefix and of what is behind it are taken apart, in fp32, and added. */
 iflow_status_t iflow_kv_attn_shared_workspace_bytes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, int n_heads, int max_shared, size_t *bytes);
 iflow_status_t iflow_kv_attn_shared(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const int32_t *shared_pages, const int32_t *shared_len, int max_shared, const uint16_t *q, int n_heads,

@@ -696,7 +696,8 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     const int limit = SEES::PREFIX && real ? min(found.limit, longest) : seq.sees(token);
     const int64_t my_out = ((int64_t)(SEES::PREFIX ? found.row : seq.row + token) * n_heads + head * group + (my_row - token * group)) * D;
     // of the wavefront's rows: what the first sees, and the last
-    const int shortest = SEES::PREFIX ? (__builtin_amdgcn_ballot_w64(limit < longest) == 0 ? longest : 0) : same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32)))), limit_of_wave = same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32 + 31))));
+    const int shortest = SEES::PREFIX ? (__builtin_amdgcn_ballot_w64(limit < longest) == 0 ? longest : 0) : same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32))));
+    const int limit_of_wave = same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32 + 31))));
     const int first_limit = same(seq.sees(by_group(r0)));     // of the workgroup's rows: what the first sees
     __shared__ int s_row[SEES::PREFIX ? ROWS : 1];            // PREFIX: the rows' numbers among all tokens' queries; -1: none
     if constexpr (SEES::PREFIX) {
