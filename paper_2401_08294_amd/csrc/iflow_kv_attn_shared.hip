@@ -1,5 +1,8 @@
 // Attention over the quantized key/value cache for a batch whose sequences share a prefix: the prefix's positions once, for the rows of all tokens (by blocks of rows, a part of the
-// positions each), what every sequence has behind them by itself, and the sum of both (the kernels: iflow_kv_attn.h).
+// positions each), what every sequence has behind them by itself, and the sum of both (the kernels: iflow_kv_attn.h):
+//   out = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m)      over the prefix's parts and the rest, m the largest reference m_i.
+// 64 sequences behind 4096 positions, up to 905 of their own, 32/8 heads x 128, 4 bits: 31 us, of which the prefix 16 (4.3 GFLOP; two steps of 64 positions to a wavefront, and what it takes to begin and to merge) and the
+// rest 16 (37 MB of codes, unpacked for 4 rows of 16); each sequence by itself 62.
 #include "iflow_kv_attn.h"
 
 namespace iflow {
