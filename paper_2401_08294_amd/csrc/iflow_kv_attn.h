@@ -1170,6 +1170,13 @@ inline dim3 kv_numbered(int64_t n)
     return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
 }
 
+// A batch as the plans below take it: no sequence has more tokens than there are rows (a program may describe many more than a call has; lines and blocks are counted by them).
+inline KvView kv_rows_bound(KvView v)
+{
+    v.max_tokens = (int32_t)std::min<int64_t>(v.max_tokens, v.n_tokens);
+    return v;
+}
+
 // The launches by sixteens, as the plan says; `seen`: positions that a token sees, at most.
 template <typename SEES>
 hipError_t kv_attn_by_sixteens(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, float scale_log2e, uint16_t *out, void *workspace, hipStream_t s, const KvPlan &plan,

@@ -54,16 +54,17 @@ struct KvSharedPlan {
 
 size_t kv_attn_shared_workspace_bytes(const KvView &v, int head_dim, int n_heads, int max_shared)
 {
-    const KvSharedPlan plan(v, head_dim, n_heads, max_shared);
+    const KvSharedPlan plan(kv_rows_bound(v), head_dim, n_heads, max_shared);
     if (plan.alone) return kv_attn_workspace_bytes(v, head_dim, n_heads);
     return (plan.prefix_bytes(v.n_tokens * n_heads, head_dim) + 15) / 16 * 16 + (plan.tail.direct ? 0 : KvPartial::bytes(v.n_seqs, head_dim));
 }
 
-hipError_t launch_kv_attn_shared(int format, int head_dim, const KvView &v, const int32_t *pages, const int32_t *len, int max_shared, const uint16_t *q, int n_heads, float scale, uint16_t *out,
+hipError_t launch_kv_attn_shared(int format, int head_dim, const KvView &batch, const int32_t *pages, const int32_t *len, int max_shared, const uint16_t *q, int n_heads, float scale, uint16_t *out,
                                  void *workspace, hipStream_t s)
 {
+    const KvView v = kv_rows_bound(batch);
     const KvSharedPlan plan(v, head_dim, n_heads, max_shared);
-    if (plan.alone) return launch_kv_attn(format, head_dim, v, q, n_heads, scale, out, workspace, s);
+    if (plan.alone) return launch_kv_attn(format, head_dim, batch, q, n_heads, scale, out, workspace, s);
     const int group = n_heads / v.n_kv_heads;
     const float scale_log2e = scale * 1.4426950408889634f;
     const KvDivide by_group(group);

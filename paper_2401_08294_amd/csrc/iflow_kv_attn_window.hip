@@ -42,13 +42,14 @@ static KvPlan kv_window_plan(const KvView &v, int head_dim, int n_heads, int win
 size_t kv_attn_window_workspace_bytes(const KvView &v, int head_dim, int n_heads, int window, int sinks)
 {
     if (kv_window_is_all(v, window, sinks)) return kv_attn_workspace_bytes(v, head_dim, n_heads);
-    const KvPlan plan = kv_window_plan(v, head_dim, n_heads, window, sinks);
+    const KvPlan plan = kv_window_plan(kv_rows_bound(v), head_dim, n_heads, window, sinks);
     return plan.sixteens && !plan.direct ? KvPartial::bytes(v.n_seqs, head_dim) : 0;
 }
 
-hipError_t launch_kv_attn_window(int format, int head_dim, const KvView &v, const uint16_t *q, int n_heads, int window, int sinks, float scale, uint16_t *out, void *workspace, hipStream_t s)
+hipError_t launch_kv_attn_window(int format, int head_dim, const KvView &batch, const uint16_t *q, int n_heads, int window, int sinks, float scale, uint16_t *out, void *workspace, hipStream_t s)
 {
-    if (kv_window_is_all(v, window, sinks)) return launch_kv_attn(format, head_dim, v, q, n_heads, scale, out, workspace, s);
+    if (kv_window_is_all(batch, window, sinks)) return launch_kv_attn(format, head_dim, batch, q, n_heads, scale, out, workspace, s);
+    const KvView v = kv_rows_bound(batch);
     return kv_attn_launches(format, head_dim, v, q, n_heads, scale, out, workspace, s, kv_window_seen(v, n_heads, window, sinks), kv_window_plan(v, head_dim, n_heads, window, sinks), KvSeesWindow{window, sinks});
 }
 

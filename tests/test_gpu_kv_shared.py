@@ -232,6 +232,18 @@ def test_rows_of_no_token(gpu):  # noqa: F811
     s.compare(got, want)
 
 
+def test_a_description_of_many_more_tokens_than_rows(gpu):  # noqa: F811
+    """max_tokens of 2^18 and max_seq of 2^20, whatever the call has."""
+    counts = [1 + i % 3 for i in range(60)]
+    s = Shared(gpu, "Q4_B64", 64, 16, 64, 64, [1024 + c + 7 * i for i, c in enumerate(counts)], counts, 1024, 8950)
+    want = s.reference(q := s.normal((s.n_tokens, 64, 64)), 0.1)
+    s.max_seq, s.max_tokens, s.max_pages = 1 << 20, 1 << 18, 1 << 14
+    s.table = np.concatenate([s.table, np.full((60, s.max_pages - s.table.shape[1]), -1, np.int32)], 1)
+    s.describe()
+    assert s.shares()
+    s.compare(s.attend(q, 0.1), want)
+
+
 @pytest.mark.parametrize("seed", range(12))
 def test_arrays_of_any_numbers(gpu, seed):  # noqa: F811
     """Lengths, first tokens, pages and the prefix's length of any 32 bits, some of them plausible: nothing is written but the output and the workspace."""

@@ -218,6 +218,18 @@ def test_rows_of_no_token_and_garbage(gpu):  # noqa: F811
     assert (np.abs(got - want) / np.maximum(np.abs(want), np.maximum(rms, 1e-30))).max() <= TOL
 
 
+@pytest.mark.parametrize("name,n_heads,n_kv,d,lens,counts,window", [("Q4_B64", 16, 4, 128, [150], [70], 40), ("Q4_B32", 64, 16, 64, [2000], [300], 1290), ("Q8_B64", 4, 4, 64, [150, 70], [20, 1], 33)])
+def test_a_description_of_many_more_tokens_than_rows(gpu, name, n_heads, n_kv, d, lens, counts, window):  # noqa: F811
+    """max_tokens and max_seq of 2^20 (of several sequences 2^18), whatever the call has: as many workgroups as its rows make."""
+    s = Long(gpu, name, n_heads, n_kv, d, 64, lens, counts, window, 4, 7850)
+    most = 1 << (20 if len(lens) == 1 else 18)
+    s.max_seq = s.max_tokens = most
+    s.table = np.concatenate([s.table, np.full((len(lens), most // 64 - s.table.shape[1]), -1, np.int32)], 1)
+    s.max_pages = most // 64
+    s.describe()
+    s.check()
+
+
 @pytest.mark.parametrize("seed", range(12))
 def test_arrays_of_any_numbers(gpu, seed):  # noqa: F811
     """Lengths, first tokens and pages of any 32 bits, some of them plausible: nothing is written but the output and the workspace."""
