@@ -1201,7 +1201,10 @@ hipError_t kv_attn_by_sixteens(int format, int head_dim, const KvView &v, const 
     const int tiles = (int)((seen + KV_TILE - 1) / KV_TILE);
     const int64_t part = std::max<int64_t>(2 * KVA_SPLIT_WAVES, plan.lines * tiles / (v.n_seqs > 1 ? 2 : 1) / (4 * KVA_CUS));
     const int groups = (int)((tiles / part + 2 + KVA_MERGE - 1) / KVA_MERGE);
-    const dim3 tokens = plan.packed ? dim3((unsigned)std::min<int64_t>(v.n_tokens, 2 * (int64_t)v.n_seqs), (unsigned)n_heads) : dim3((unsigned)n_heads, (unsigned)v.max_tokens, (unsigned)v.n_seqs);
+    // Packed, a workgroup merges one token after another: where all are by sixteens there are as many workgroups as tokens, up to what the device holds (225 tokens of one sequence and one each of two others, 4/1 heads
+    // of 128, 2785 positions: 77 us with two for each sequence, 18 so).
+    const int64_t at_once = std::max<int64_t>(2 * (int64_t)v.n_seqs, plan.few ? 0 : 8192 / n_heads);
+    const dim3 tokens = plan.packed ? dim3((unsigned)std::min(v.n_tokens, at_once), (unsigned)n_heads) : dim3((unsigned)n_heads, (unsigned)v.max_tokens, (unsigned)v.n_seqs);
     hipLaunchKernelGGL(kv_attn_merge_kernel<SEES>, tokens, dim3((unsigned)head_dim, (unsigned)(groups > 8 ? 8 : groups)), 0, s, v, n_heads, group, few, workspace, out, sees);
     return hipGetLastError();
 }
