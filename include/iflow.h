@@ -400,7 +400,7 @@ iflow_status_t iflow_kv_attn_shared(const iflow_kv_cache_t *cache, const iflow_k
  *   slots (may be null) [n_tokens]: where a token's position lies, page * P + position mod P, or -1 without a position or page.  Rows of no token are left as they were.
  * new_tokens is taken as 0 .. max_tokens, a length as at most max_seq.  first_token null: one token each, row b, and new_tokens is not read.
  * All arrays are device arrays, int32 and 4-byte aligned but for slots (int64, 8).  held_out may be held, and free_state_out free_state; nothing else that is written may overlap anything
- * (IFLOW_ERR_SHAPE).  n_seqs * max_pages < 2^31.  Whatever the arrays hold, what is read and written lies inside them; a ring of fewer entries than are given back loses the rest.
+ * (IFLOW_ERR_SHAPE).  n_seqs * max_pages <= 2^30.  Whatever the arrays hold, what is read and written lies inside them; a ring of fewer entries than are given back loses the rest.
  * workspace: iflow_kv_tables_workspace_bytes() bytes, 16-byte aligned.  Calls that share one must be ordered. */
 typedef struct iflow_kv_pages_t {
     const int32_t *held, *free_state;

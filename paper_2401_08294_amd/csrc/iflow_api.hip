@@ -561,7 +561,7 @@ static iflow_status_t kv_tables_shapes(const iflow_kv_cache_t *cache, const iflo
 {
     const iflow_status_t st = kv_shapes(cache, batch, false, 0, v);
     if (st != IFLOW_OK) return st;
-    return (int64_t)v->n_seqs * v->max_pages >= (1LL << 31) ? IFLOW_ERR_SHAPE : IFLOW_OK;      // (pages are numbered in 32 bits)
+    return (int64_t)v->n_seqs * v->max_pages > (1LL << 30) ? IFLOW_ERR_SHAPE : IFLOW_OK;      // (pages are numbered in 32 bits)
 }
 
 iflow_status_t iflow_kv_tables_workspace_bytes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, size_t *bytes)

@@ -60,7 +60,7 @@ def test_refusals_before_any_launch(iflow):  # noqa: F811
     assert need >= 4 * (3 * 4 + 2) and need % 16 == 0
     assert call(cache=dict(format=77)) == iflow.ERR_FORMAT
     for kw in (dict(cache=dict(page_positions=48)), dict(batch=dict(n_seqs=0)), dict(batch=dict(max_seq=1281)), dict(batch=dict(max_tokens=0)), dict(batch=dict(n_tokens=0)), dict(pages=dict(n_shared=-1)),
-               dict(pages=dict(n_shared=21)), dict(batch=dict(n_seqs=65535, max_pages=32770, max_tokens=1), cache=dict(n_pages=(1 << 31) - 1, n_kv_heads=1, head_dim=64, page_positions=32))):
+               dict(pages=dict(n_shared=21)), dict(batch=dict(n_seqs=65535, max_pages=32770, max_tokens=1)), dict(batch=dict(n_seqs=1 << 15, max_pages=(1 << 15) + 1, max_tokens=1))):
         assert call(**kw) == iflow.ERR_SHAPE, kw
     for name in ("page_table", "seq_lens"):
         assert call(batch={name: None}) == iflow.ERR_NULL
@@ -70,6 +70,8 @@ def test_refusals_before_any_launch(iflow):  # noqa: F811
     assert call(new=None) == iflow.ERR_NULL and call(ws=None) == iflow.ERR_NULL
     assert call(new=10 * AT + 1) == iflow.ERR_ALIGN and call(slots=11 * AT + 4) == iflow.ERR_ALIGN and call(ws=12 * AT + 8) == iflow.ERR_ALIGN
     assert call(size=need - 1) == iflow.ERR_SIZE
+    most = described(iflow, batch=dict(n_seqs=1 << 15, max_pages=1 << 15, max_tokens=1))
+    assert iflow.kv_tables_workspace_bytes(*most[:2]) > 12 << 15
     c, b, p = described(iflow)
     for args in ((None, b, p), (c, None, p), (c, b, None)):
         assert L.iflow_kv_tables(*args, AT, AT, AT, 1 << 30, None) == iflow.ERR_NULL
