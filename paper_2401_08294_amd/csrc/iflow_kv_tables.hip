@@ -5,7 +5,7 @@
 // nothing waits for anything but the sums: what is taken lies in front of the ring's end as it was, what is given back behind it, and a token's page is one that its sequence had (in the table as it
 // was) or one that it takes (in the ring).
 // The work is launches and latencies.  Up to 1024 sequences every workgroup adds up all of them for itself, in LDS, and the rest is shared among the wavefronts of all; more
-// sequences, and a larger batch whose state is updated in place (its workgroups would read what one of them has written), take a launch for the sums.
+// sequences, and a larger batch whose state is updated in place (its workgroups would read what one of them has written), take launches of their own for the sums.
 // 64 sequences' next tokens 3.5 us, a mixed step of 256 sequences and 30 thousand tokens 4.3, a third of a million tokens of 1000 sequences 5.8 (graph replay): lengths -> sums -> search -> page -> slot, one after another.
 #include <algorithm>
 
@@ -23,11 +23,11 @@ struct KvSums {
     const int32_t *tokens, *take, *give, *held, *lens;
     int32_t start, count, n_tokens, n_take, n_give;
 };
-// work space: {start, count, tokens, taken, given back}, then the sums
+// work space: {start, count, tokens, taken, given back}, tokens, pages taken and given back of every 1024 sequences, then the sums
 struct KvSumsSpace {
-    static constexpr int HEAD = 8;
-    int32_t *head, *take, *give, *held;
-    __device__ __forceinline__ KvSumsSpace(void *ws, int n) : head(static_cast<int32_t *>(ws)), take(head + HEAD), give(take + n + 1), held(give + n + 1) {}
+    static constexpr int CHUNKS = 64, HEAD = 8 + 3 * CHUNKS;
+    int32_t *head, *chunk, *take, *give, *held;
+    __device__ __forceinline__ KvSumsSpace(void *ws, int n) : head(static_cast<int32_t *>(ws)), chunk(head + 8), take(head + HEAD), give(take + n + 1), held(give + n + 1) {}
     static size_t bytes(int n) { return ((size_t)(HEAD + 3 * n + 2) * 4 + 15) / 16 * 16; }
 };
 
@@ -166,31 +166,42 @@ __global__ __launch_bounds__(KVT_THREADS) void kv_tables_kernel(KvView v, KvTabl
     kvt_fill(v, t, s, __builtin_amdgcn_readfirstlane(blockIdx.x * KVT_WAVES + (b >> 6)), gridDim.x * KVT_WAVES);
 }
 
-// Any number of sequences: the sums, by one workgroup; then the rest.  (Us, both launches: 2000 sequences 8.6, 8000 17, 60000 72, which is what one compute unit loads and stores; four sequences a thread, in a row or 1024 apart, 10.5 / 23 /
-// 115 and 9.4 / 16 / 64.)
+// Any number of sequences, 1024 to a workgroup: what they want together; the sums; then the rest.  (The ring's ends go by way of the work space, or one workgroup has read them: free_out may be free_state.
+// Us, 1025, 8000 and 60000 sequences' next tokens 8.8, 12.1, 13.2; the sums by one workgroup, without the first launch, 7.8, 17.2, 72: what one compute unit loads and stores.)
+__global__ __launch_bounds__(KVT_THREADS) void kv_tables_totals_kernel(KvView v, KvTables t, void *ws)
+{
+    __shared__ int32_t s_waves[3][KVT_WAVES];
+    const KvSumsSpace to(ws, v.n_seqs);
+    const int b = blockIdx.x * KVT_THREADS + threadIdx.x;
+    KvWants w = {0, 0, 0, 0};
+    if (b < v.n_seqs) w = kvt_wants(v, t, b);
+    KvScan scan;
+    int tokens, take, give;
+    scan.step(w, s_waves, tokens, take, give);
+    if (threadIdx.x == 0) { to.chunk[3 * blockIdx.x] = scan.tokens; to.chunk[3 * blockIdx.x + 1] = scan.take; to.chunk[3 * blockIdx.x + 2] = scan.give; }
+    if (b == 0) kvt_range(v, t, to.head[0], to.head[1]);
+}
 __global__ __launch_bounds__(KVT_THREADS) void kv_tables_sums_kernel(KvView v, KvTables t, void *ws)
 {
-    __shared__ int32_t s_waves[2][3][KVT_WAVES];
+    __shared__ int32_t s_waves[3][KVT_WAVES];
     const KvSumsSpace to(ws, v.n_seqs);
+    const int b = blockIdx.x * KVT_THREADS + threadIdx.x, lane = threadIdx.x & 63;
+    KvWants w = {0, 0, 0, 0};
+    if (b < v.n_seqs) w = kvt_wants(v, t, b);
     KvSums s = {};
-    kvt_range(v, t, s.start, s.count);
-    __syncthreads();                                          // (before free_out, which may be free_state, is written)
+    if (gridDim.x > 1) { s.start = to.head[0]; s.count = to.head[1]; }
+    else kvt_range(v, t, s.start, s.count);
     KvScan scan;
-    KvWants next = {0, 0, 0, 0};
-    if ((int)threadIdx.x < v.n_seqs) next = kvt_wants(v, t, threadIdx.x);
-    for (int b0 = 0, turn = 0; b0 < v.n_seqs; b0 += KVT_THREADS, turn ^= 1) {
-        const int b = b0 + threadIdx.x;
-        const KvWants w = next;
-        if (b + KVT_THREADS < v.n_seqs) next = kvt_wants(v, t, b + KVT_THREADS);
-        else next = {0, 0, 0, 0};
-        int tokens, take, give;
-        scan.step(w, s_waves[turn], tokens, take, give);
-        if (b >= v.n_seqs) continue;
+    auto before = [&](int i) { return __builtin_amdgcn_readlane(wave_scan(lane < (int)blockIdx.x ? to.chunk[3 * lane + i] : 0), 63); };
+    if (gridDim.x > 1) { scan.tokens = before(0); scan.take = before(1); scan.give = before(2); }
+    int tokens, take, give;
+    scan.step(w, s_waves, tokens, take, give);
+    if (b < v.n_seqs) {
         if (v.first) const_cast<int32_t *>(v.first)[b] = tokens;
         to.take[b] = take; to.give[b] = give; to.held[b] = w.held;
         t.held_out[b] = w.held - max(0, w.held - w.need) + max(0, min(s.count - take, w.need - w.held));
     }
-    if (threadIdx.x == 0) {
+    if (b == v.n_seqs - 1) {
         s.n_tokens = scan.tokens; s.n_take = scan.take; s.n_give = scan.give;
         if (v.first) const_cast<int32_t *>(v.first)[v.n_seqs] = s.n_tokens;
         to.take[v.n_seqs] = s.n_take; to.give[v.n_seqs] = s.n_give;
@@ -224,8 +235,15 @@ hipError_t launch_kv_tables(const KvView &v, const KvTables &t, void *workspace,
         hipLaunchKernelGGL(kv_tables_kernel, dim3((unsigned)groups), dim3(KVT_THREADS), 0, s, v, t);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL(kv_tables_sums_kernel, dim3(1), dim3(KVT_THREADS), 0, s, v, t, workspace);
-    const hipError_t e = hipGetLastError();
+    const dim3 thousands((unsigned)((v.n_seqs + KVT_THREADS - 1) / KVT_THREADS));
+    hipError_t e = hipSuccess;
+    if (thousands.x > 1) {
+        hipLaunchKernelGGL(kv_tables_totals_kernel, thousands, dim3(KVT_THREADS), 0, s, v, t, workspace);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kv_tables_sums_kernel, thousands, dim3(KVT_THREADS), 0, s, v, t, workspace);
+    e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kv_tables_fill_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(2048, (chunks + 3) / 4))), dim3(256), 0, s, v, t, workspace);
     return hipGetLastError();
