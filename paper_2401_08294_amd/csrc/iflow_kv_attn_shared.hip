@@ -52,17 +52,26 @@ struct KvSharedPlan {
     size_t prefix_bytes(int64_t n_rows, int head_dim) const { return (size_t)parts * n_rows * (head_dim + 2) * 4 + 32; }      // (the values behind the others, 16-byte aligned)
 };
 
-size_t kv_attn_shared_workspace_bytes(const KvView &v, int head_dim, int n_heads, int max_shared)
+// Positions of a prefix's whole pages.  The kernels ask for its pages before they know its length: what bounds them is how many entries the array has.
+static int kv_whole_pages(const KvView &v, int positions)
 {
+    const int page = v.tiles_per_page * KV_TILE;
+    return positions / page * page;
+}
+
+size_t kv_attn_shared_workspace_bytes(const KvView &v, int head_dim, int n_heads, int most)
+{
+    const int max_shared = kv_whole_pages(v, most);
     const KvSharedPlan plan(kv_rows_bound(v), head_dim, n_heads, max_shared);
     if (plan.alone) return kv_attn_workspace_bytes(v, head_dim, n_heads);
     return (plan.prefix_bytes(v.n_tokens * n_heads, head_dim) + 15) / 16 * 16 + (plan.tail.direct ? 0 : KvPartial::bytes(v.n_seqs, head_dim));
 }
 
-hipError_t launch_kv_attn_shared(int format, int head_dim, const KvView &batch, const int32_t *pages, const int32_t *len, int max_shared, const uint16_t *q, int n_heads, float scale, uint16_t *out,
+hipError_t launch_kv_attn_shared(int format, int head_dim, const KvView &batch, const int32_t *pages, const int32_t *len, int most, const uint16_t *q, int n_heads, float scale, uint16_t *out,
                                  void *workspace, hipStream_t s)
 {
     const KvView v = kv_rows_bound(batch);
+    const int max_shared = kv_whole_pages(v, most);
     const KvSharedPlan plan(v, head_dim, n_heads, max_shared);
     if (plan.alone) return launch_kv_attn(format, head_dim, batch, q, n_heads, scale, out, workspace, s);
     const int group = n_heads / v.n_kv_heads;

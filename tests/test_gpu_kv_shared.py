@@ -386,3 +386,32 @@ def test_a_program_that_serves(gpu, captured):  # noqa: F811
             got = out.cpu().numpy().astype(np.float64)
             rms = np.maximum(np.sqrt(np.mean(want ** 2, axis=-1, keepdims=True)), 1e-30)
             assert (np.abs(got - want) / np.maximum(np.abs(want), rms)).max() <= TOL, turn
+
+
+@pytest.mark.parametrize("page,most,shared", [(64, 2000, 2000), (1024, 2000, 2000), (256, 1500, 1300), (96, 1100, 1100), (64, 1055, 1024)])
+@pytest.mark.parametrize("counts", [None, 3])
+def test_prefixes_of_no_whole_pages(gpu, page, most, shared, counts):  # noqa: F811
+    """shared_pages as it is described, max_shared / page_positions entries between others, which are pages of the cache: the positions past the last whole page are every sequence's own."""
+    torch, it = gpu
+    whole = most // page * page
+    lens = [most + x for x in OWN * 4]
+    s = Shared(gpu, "Q8_B32", 32, 8, 128, page, lens, counts and [min(counts, x - whole) for x in lens], shared, 9300, most=most)
+    assert s.shares()
+    others = torch.from_numpy(np.random.default_rng(1).permutation(s.cache.n_pages)[:8].astype(np.int32)).cuda()
+    array = torch.cat([others, s.dev(s.table[0, :most // page]), others])
+    s.d_shared = array[8:8 + most // page]
+    s.check()
+
+
+def test_a_page_longer_than_the_prefix(gpu):  # noqa: F811
+    """No whole page: causal attention's bits, without pages."""
+    torch, it = gpu
+    s = Shared(gpu, "Q4_B64", 32, 8, 128, 1024, [1024 + x for x in OWN * 4], None, 0, 9310, most=1000)
+    q = s.normal((64, 32, 128))
+    need = it.kv_attn_workspace_bytes(s.cache, s.batch, 32)
+    assert s.room() == need
+    out, ws = torch.full_like(q, 7.0), torch.full((max(need, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    it.kv_attn(s.cache, s.batch, q, 32, 0.1, out, ws, need)
+    s.d_shared = None
+    assert torch.equal(s.attend(q, 0.1), out)
+    s.compare(out, s.reference(q, 0.1))

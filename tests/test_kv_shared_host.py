@@ -68,3 +68,17 @@ def test_extension_hands_the_call_on(iflow):  # noqa: F811
         assert not seen
     finally:
         native.bind(*real)
+
+
+@pytest.mark.parametrize("page,most", [(1024, 1000), (1024, 1023), (1024, 1025), (1024, 2000), (512, 4000), (256, 1000), (96, 1100), (64, 2000), (2048, 4095), (1 << 20, 4096)])
+@pytest.mark.parametrize("n_seqs,n_heads", [(64, 32), (64, 8), (200, 64)])
+def test_a_prefix_is_whole_pages(iflow, page, most, n_seqs, n_heads):  # noqa: F811
+    """shared_pages has max_shared / page_positions entries: the call counts with the positions of these, as its workspace shows, and where there is none (the array may be null) it is causal attention."""
+    of = described(iflow, cache=dict(page_positions=page, n_pages=1000), n_seqs=n_seqs, n_tokens=n_seqs, max_tokens=1, first_token=None, max_pages=128, max_seq=4096)
+    whole = most // page * page
+    room = iflow.kv_attn_shared_workspace_bytes(*of, n_heads, most)
+    assert room == iflow.kv_attn_shared_workspace_bytes(*of, n_heads, whole)
+    if whole == 0:
+        assert room == iflow.kv_attn_workspace_bytes(*of, n_heads)
+        # (every check but that of the output's place is passed without pages: no launch)
+        assert iflow.lib().iflow_kv_attn_shared(*of, None, 6 * AT, most, 2 * AT, n_heads, 0.1, 2 * AT + 16, 64 * AT, room, None) == iflow.ERR_SHAPE
