@@ -383,7 +383,8 @@ iflow_status_t iflow_kv_attn_window(const iflow_kv_cache_t *cache, const iflow_k
  * All its positions have been written (a token inside the prefix weighs what lies behind it with zeros).  Every sequence that has tokens in the call has these pages in its row of page_table (which
  * must not be null), entries 0 .. shared_len / page_positions - 1: where a row has others it is unspecified which of the two a token sees.  (iflow_kv_tables writes such rows.)  A token at a position
  * inside the prefix sees it up to its own position.
- * Everything else, the result among it, as for iflow_kv_attn: the sums of the prefix and of what is behind it are taken apart, in fp32, and added. */
+ * Everything else, the result among it, as for iflow_kv_attn: the sums of the prefix and of what is behind it are taken apart, in fp32, and added.  (Where first_token goes back anywhere, a row may also
+ * be left as it was: a row's sequence is searched for.) */
 iflow_status_t iflow_kv_attn_shared_workspace_bytes(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, int n_heads, int max_shared, size_t *bytes);
 iflow_status_t iflow_kv_attn_shared(const iflow_kv_cache_t *cache, const iflow_kv_batch_t *batch, const int32_t *shared_pages, const int32_t *shared_len, int max_shared, const uint16_t *q, int n_heads,
                                     float scale, uint16_t *out, void *workspace, size_t workspace_bytes, void *stream);

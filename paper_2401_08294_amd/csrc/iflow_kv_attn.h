@@ -24,6 +24,7 @@ constexpr int KVA_ROWS = 16;                                  // rows of a workg
 // workgroups that a compute unit holds at once (by their registers), and the whole device
 template <typename T> constexpr int KVA_PER_CU = T::D == 64 ? 4 : 3;
 constexpr int KVA_CUS = 256;
+constexpr int KVA_ALL = 0x7fffffff;                           // `few` where sequences of any number of rows are served
 constexpr float KVA_BELOW = 7.f, KVA_LAG = 15.f, KVA_SPARE = 16.f;       // in units of log2: see attn_decode_mfma_kernel
 // A score's distance from the reference is one multiply-add, rounded once, while the reference is a rounded product: they differ by half a step of it, 2^-4 at 2^20.  Where a reference is as large, the scores
 // are multiplied and rounded first, as it was (else the largest probability is two to that difference: no number from 2^32 on).
@@ -92,10 +93,14 @@ struct KvSeesWindow {
     // of tokens whose limits are at most `longest`: some position of tile p0 / 32 may be hidden
     __device__ __forceinline__ bool hides(int p0, int longest) const { return p0 < longest - window && p0 + KV_TILE > sinks; }
 };
-// A prefix that sequences share: its whole pages' positions, and what the rows of all tokens' queries [token][head] have of it: in so many parts their references, sums and values, [part][row].
+// Of a row of the call's tokens: the sequence for whose token the prefix was attended over, and which of the tokens that share it that is (-1: none).  Of a row that two sequences claim it is one of them: the
+// other's position may be inside the prefix, so it must not add what this one sees.
+struct alignas(8) KvServed { int32_t seq, number; };
+// A prefix that sequences share: its whole pages' positions, and what the rows of all tokens' queries [number][head] have of it: in so many parts their references, sums and values, [part][row].
 struct KvShared {
     const int32_t *pages, *len;
     float *m, *l, *o;
+    KvServed *served;                                         // [token]
     int64_t rows;
     int max_len, parts;
     __device__ __forceinline__ int tiles(const KvView &v) const { return v.page_of(max(0, min(len[0], max_len)) / KV_TILE) * v.tiles_per_page; }
@@ -110,6 +115,8 @@ struct KvSeesTail : KvShared {
     int start;                                                // tiles of the prefix: the kernel asks for them first
     __device__ __forceinline__ KvSpan span(int, int longest) const { return {0, start, max(0, (longest + KV_TILE - 1) / KV_TILE - start)}; }
     __device__ __forceinline__ int line_tiles(const KvSequence &seq, int) const { return max(0, (seq.sees(seq.count - 1) + KV_TILE - 1) / KV_TILE - start); }
+    // The states' number of a token (where all share it is the token's row, which need not be waited for; always one that there is).
+    __device__ __forceinline__ int64_t state_of(const KvServed &token, int row, int few) const { return few == KVA_ALL ? row : max(0, token.number); }
     // N of a row's values, from component d on, and its sum, relative to `base` (-inf: it has none): with the prefix's, relative to the largest reference.  Eight parts are asked for at once.
     template <int N> __device__ __forceinline__ void add(int64_t row, int d, float base, float &sum, float (&values)[N]) const
     {
@@ -489,7 +496,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? KVA_PER_CU<T> : 1) void kv
                 if (r < rows && seq.has_row(tok)) {
                     if constexpr (SEES::TAIL) {
                         float with[4] = {O[0], O[1], O[2], O[3]};
-                        sees.add((int64_t)(seq.row + tok) * n_heads + head * group + (r0 + r - tok * group), d, M == -INFINITY ? M : to_base, L, with);
+                        const KvServed served = sees.served[seq.row + tok];
+                        sees.add(sees.state_of(served, seq.row + tok, few) * n_heads + head * group + (r0 + r - tok * group), d, M == -INFINITY ? M : to_base, L, with);
+                        if (served.seq != b) continue;        // (another sequence's row)
                         O = (kv_float4){with[0], with[1], with[2], with[3]};
                     }
                     const float div = L > 0.f ? L : 1.f;      // (nothing seen: zeros)
@@ -560,7 +569,9 @@ __device__ __forceinline__ void kv_attn_merge(const KvView &v, int b, int i, int
     }
     if constexpr (SEES::TAIL) {
         float with[1] = {O};
-        sees.add((int64_t)(seq.row + i) * n_heads + h, d, M == -INFINITY ? M : to_base(M), L, with);
+        const KvServed served = sees.served[seq.row + i];
+        sees.add(sees.state_of(served, seq.row + i, few) * n_heads + h, d, M == -INFINITY ? M : to_base(M), L, with);
+        if (served.seq != b) return;                          // (another sequence's row)
         O = with[0];
     }
     out[((int64_t)(seq.row + i) * n_heads + h) * D + d] = as_u16((half_t)(L > 0.f ? O / L : 0.f));
@@ -597,22 +608,23 @@ struct KvCallRows {
     __device__ __forceinline__ bool has_row(int i) const { return i < count; }
     __device__ __forceinline__ int sees(int) const { return part; }
 };
-// PREFIX: the w-th of all tokens that share the prefix, each lane its own, in order from lane 0 to 31: its row in the call's arrays (-1: there is none) and what it sees.  Where sequences of `few` rows and
+// PREFIX: the w-th of all tokens that share the prefix, each lane its own, in order from lane 0 to 31: its row in the call's arrays (-1: there is none), what it sees, and its sequence.  Where sequences of `few` rows and
 // more are served otherwise, the others' tokens are counted; else a row is a token's, and its sequence the last that begins at or in front of it.
-struct KvToken { int row, limit; };
+struct KvToken { int row, limit, seq; };
 __device__ __forceinline__ KvToken kv_token(const KvView &v, int w, int group, int few)
 {
     if (!v.first) {                                           // one each
-        if (w >= v.n_seqs) return {-1, 0};
-        return {w, KvSequence(v, w).sees(0)};
+        if (w >= v.n_seqs) return {-1, 0, -1};
+        return {w, KvSequence(v, w).sees(0), w};
     }
-    if (few == 0x7fffffff) {
-        const KvSequence seq(v, kv_last_of(v.first, v.n_seqs, __builtin_amdgcn_readlane(w, 0), __builtin_amdgcn_readlane(w, 31), w));
+    if (few == KVA_ALL) {
+        const int b = kv_last_of(v.first, v.n_seqs, __builtin_amdgcn_readlane(w, 0), __builtin_amdgcn_readlane(w, 31), w);
+        const KvSequence seq(v, b);
         const int i = (int)((uint32_t)w - (uint32_t)seq.row);
-        return {seq.has_row(i) ? w : -1, seq.sees(i)};
+        return {seq.has_row(i) ? w : -1, seq.sees(i), b};
     }
     const int lane = threadIdx.x & 63;
-    KvToken token = {-1, 0};
+    KvToken token = {-1, 0, -1};
     for (int b = 0; b < v.n_seqs; b += 64) {
         int mine = 0, row = 0, position = 0;
         if (b + lane < v.n_seqs) {
@@ -628,7 +640,7 @@ __device__ __forceinline__ KvToken kv_token(const KvView &v, int w, int group, i
         const int i = w - __shfl(upto - mine, at & 63), first = __shfl(row, at & 63), p = __shfl(position, at & 63);
         if (w >= 0 && w < all) {
             const int to = (int)((uint32_t)first + (uint32_t)i);
-            token = {(uint32_t)to < (uint32_t)v.n_tokens ? to : -1, max(0, min((int)((uint32_t)p + (uint32_t)i + 1u), v.max_seq))};
+            token = {(uint32_t)to < (uint32_t)v.n_tokens ? to : -1, max(0, min((int)((uint32_t)p + (uint32_t)i + 1u), v.max_seq)), b + at};
         }
         w -= all;
         if (__builtin_amdgcn_ballot_w64(w >= 0) == 0) break;
@@ -690,7 +702,7 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     auto same = [](int n) { return __builtin_amdgcn_readfirstlane(n); };
     const int longest = same(seq.sees(by_group(min(n_rows, r0 + ROWS) - 1)));
     const int my_row = min(n_rows - 1, r0 + rg * 32 + li), token = by_group(my_row);
-    KvToken found = {0, 0};
+    KvToken found = {0, 0, 0};
     if constexpr (SEES::PREFIX) found = kv_token(v, token, group, sees.few);
     const bool real = r0 + rg * 32 + li < n_rows && (SEES::PREFIX ? found.row >= 0 : seq.has_row(token));
     const int limit = SEES::PREFIX && real ? min(found.limit, longest) : seq.sees(token);
@@ -699,9 +711,15 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     const int shortest = SEES::PREFIX ? (__builtin_amdgcn_ballot_w64(limit < longest) == 0 ? longest : 0) : same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32))));
     const int limit_of_wave = same(seq.sees(by_group(min(n_rows - 1, r0 + rg * 32 + 31))));
     const int first_limit = same(seq.sees(by_group(r0)));     // of the workgroup's rows: what the first sees
-    __shared__ int s_row[SEES::PREFIX ? ROWS : 1];            // PREFIX: the rows' numbers among all tokens' queries; -1: none
+    __shared__ int s_row[SEES::PREFIX ? ROWS : 1];            // PREFIX: the rows' numbers among the queries of all tokens that share; -1: none
     if constexpr (SEES::PREFIX) {
-        if (pg == 0 && hf == 0) s_row[rg * 32 + li] = real ? (int)(my_out / D) : -1;
+        const int query = my_row - token * group;
+        if (pg == 0 && hf == 0) s_row[rg * 32 + li] = real ? token * n_heads + head * group + query : -1;
+        // (by one lane of all workgroups for each token; where all share, for every row, whether it is a token's or not)
+        if (b == 0 && head == 0 && pg == 0 && hf == 0 && query == 0 && r0 + rg * 32 + li < n_rows) {
+            if (real) sees.served[found.row] = {found.seq, token};
+            else if (sees.few == KVA_ALL) sees.served[token] = {-1, -1};
+        }
         if (!__syncthreads_or(real)) return;
     } else {
         span = sees.span(first_limit, longest);
@@ -1184,7 +1202,7 @@ hipError_t kv_attn_by_sixteens(int format, int head_dim, const KvView &v, const 
 {
     const int group = n_heads / v.n_kv_heads;
     const KvDivide by_group(group), by_heads(v.n_kv_heads);
-    const int few = plan.few ? plan.few : 0x7fffffff;
+    const int few = plan.few ? plan.few : KVA_ALL;
     hipError_t e = for_kv_tile(format, head_dim, [&](auto tag) {
         typedef decltype(tag) T;
         const dim3 direct = plan.packed ? kv_numbered(plan.lines) : dim3((unsigned)(plan.lines / v.n_seqs), (unsigned)v.n_seqs);

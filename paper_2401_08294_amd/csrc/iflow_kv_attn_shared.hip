@@ -49,8 +49,16 @@ struct KvSharedPlan {
         const int64_t saved = (10 * lines - 13 * together * kv) * tiles * (head_dim + 64) / (10 * 192);
         alone = seqs < 2 || all > (1 << 21) || v.n_tokens * n_heads > (1 << 22) || tiles < 2 * PART || saved < (tail.direct ? LEAST : LEAST_CUT);
     }
-    size_t prefix_bytes(int64_t n_rows, int head_dim) const { return (size_t)parts * n_rows * (head_dim + 2) * 4 + 32; }      // (the values behind the others, 16-byte aligned)
+    size_t prefix_bytes(int64_t n_rows, int head_dim) const { return ((size_t)parts * n_rows * (head_dim + 2) * 4 + 32 + 15) / 16 * 16; }      // (the values behind the others, 16-byte aligned)
+    static size_t served_bytes(int64_t n_tokens) { return (n_tokens * sizeof(KvServed) + 15) / 16 * 16; }
 };
+
+// Rows of the call's tokens that no sequence has yet.  (Where sequences of `few` rows and more are served otherwise the prefix's blocks write only the others', and find those that there are rows for: first
+// tokens that go back may claim more.)
+__global__ __launch_bounds__(256) void kv_served_none_kernel(KvServed *__restrict__ served, int64_t n)
+{
+    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) served[i] = {-1, -1};
+}
 
 // Positions of a prefix's whole pages.  The kernels ask for its pages before they know its length: what bounds them is how many entries the array has.
 static int kv_whole_pages(const KvView &v, int positions)
@@ -64,7 +72,7 @@ size_t kv_attn_shared_workspace_bytes(const KvView &v, int head_dim, int n_heads
     const int max_shared = kv_whole_pages(v, most);
     const KvSharedPlan plan(kv_rows_bound(v), head_dim, n_heads, max_shared);
     if (plan.alone) return kv_attn_workspace_bytes(v, head_dim, n_heads);
-    return (plan.prefix_bytes(v.n_tokens * n_heads, head_dim) + 15) / 16 * 16 + (plan.tail.direct ? 0 : KvPartial::bytes(v.n_seqs, head_dim));
+    return plan.prefix_bytes(v.n_tokens * n_heads, head_dim) + plan.served_bytes(v.n_tokens) + (plan.tail.direct ? 0 : KvPartial::bytes(v.n_seqs, head_dim));
 }
 
 hipError_t launch_kv_attn_shared(int format, int head_dim, const KvView &batch, const int32_t *pages, const int32_t *len, int most, const uint16_t *q, int n_heads, float scale, uint16_t *out,
@@ -79,21 +87,22 @@ hipError_t launch_kv_attn_shared(int format, int head_dim, const KvView &batch, 
     const KvDivide by_group(group);
     const int64_t n_rows = v.n_tokens * n_heads;
     float *const m = static_cast<float *>(workspace), *const l = m + plan.parts * n_rows, *const o = m + (2 * plan.parts * n_rows + 3) / 4 * 4;
-    const KvShared shared = {pages, len, m, l, o, n_rows, max_shared, plan.parts};
+    uint8_t *const behind = static_cast<uint8_t *>(workspace) + plan.prefix_bytes(n_rows, head_dim);
+    const KvShared shared = {pages, len, m, l, o, reinterpret_cast<KvServed *>(behind), n_rows, max_shared, plan.parts};
     if (plan.big) {
+        hipLaunchKernelGGL(kv_served_none_kernel, dim3((unsigned)std::min<int64_t>(1024, (v.n_tokens + 255) / 256)), dim3(256), 0, s, shared.served, v.n_tokens);
         const hipError_t e = launch_kv_attn_blocks(format, head_dim, v, q, n_heads, scale, out, plan.big, KVA_FEW, s);
         if (e != hipSuccess) return e;
     }
     const hipError_t e = for_kv_tile(format, head_dim, [&](auto tag) {
         typedef decltype(tag) T;
-        const KvSeesPrefix sees = {shared, plan.big ? KVA_FEW : 0x7fffffff, plan.per};
+        const KvSeesPrefix sees = {shared, plan.big ? KVA_FEW : KVA_ALL, plan.per};
         hipLaunchKernelGGL((kv_attn_rows_kernel<T, 2, 4, 1, KvSeesPrefix>), dim3((unsigned)v.n_kv_heads, (unsigned)plan.blocks, (unsigned)plan.parts), dim3(512), 0, s, v, q, n_heads, group, 0, by_group,
                            scale_log2e, out, sees);
         return hipGetLastError();
     });
     if (e != hipSuccess) return e;
-    uint8_t *const rest = static_cast<uint8_t *>(workspace) + (plan.prefix_bytes(n_rows, head_dim) + 15) / 16 * 16;
-    return kv_attn_by_sixteens(format, head_dim, v, q, n_heads, scale_log2e, out, rest, s, plan.tail, std::max<int64_t>(1, v.max_seq - max_shared), KvSeesTail{shared, head_dim, 0});
+    return kv_attn_by_sixteens(format, head_dim, v, q, n_heads, scale_log2e, out, behind + plan.served_bytes(v.n_tokens), s, plan.tail, std::max<int64_t>(1, v.max_seq - max_shared), KvSeesTail{shared, head_dim, 0});
 }
 
 }  // namespace iflow

@@ -415,3 +415,36 @@ def test_a_page_longer_than_the_prefix(gpu):  # noqa: F811
     s.d_shared = None
     assert torch.equal(s.attend(q, 0.1), out)
     s.compare(out, s.reference(q, 0.1))
+
+
+@pytest.mark.parametrize("name,n_heads,n_kv,d,own,big,enough", [("Q4_B64", 32, 8, 128, 100, 0, True), ("Q8_B32", 64, 16, 64, 100, 0, False), ("Q4_B32", 32, 8, 128, 2500, 0, True), ("Q8_B64", 64, 64, 64, 60, 150, True),
+                                                               ("Q4_B64", 64, 64, 64, 60, 150, False), ("Q4_B64", 32, 8, 128, 60, 40, True)])
+def test_rows_that_two_sequences_claim(gpu, name, n_heads, n_kv, d, own, big, enough):  # noqa: F811
+    """First tokens that go back: a row of the result is that of a sequence that claims it, at its own position (some are inside the prefix), or as it was; also where fewer rows are there than are claimed."""
+    torch, it = gpu
+    first = [0]
+    for b in range(90):                                       # steps of 2 to 4 tokens forwards and, at every fifth sequence, of 1 to 5 backwards
+        step = big if big and b % 30 == 7 else -(1 + b % 3) - (2 if b % 10 == 2 else 0) if b % 5 == 2 else 2 + b % 3
+        first.append(max(0, first[-1] + step))
+    counts = np.maximum(np.diff(first), 0)
+    claimed = int(counts.sum())
+    lens = [1024 + int(c) + (29 * b) % own if b % 4 else int(c) + (37 * b) % 900 for b, c in enumerate(counts)]
+    s = Shared(gpu, name, n_heads, n_kv, d, 64, lens, None, 1024, 9400 + own, first=first, n_tokens=claimed if enough else max(first) + 1, max_tokens=int(counts.max()), max_seq=max(lens))
+    assert s.shares() and claimed > max(first) + 1
+    q = s.normal((s.n_tokens, n_heads, d))
+    got = s.attend(q, d ** -0.5).double()
+    rows = np.concatenate([np.arange(first[b], first[b] + c) for b, c in enumerate(counts)])
+    s.first, s.n_tokens = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32), claimed                  # the same tokens, each with a row of its own
+    want = s.reference(q[torch.from_numpy(rows).cuda()].contiguous(), d ** -0.5)
+    served = np.zeros(len(got), int)
+    for row in range(len(got)):
+        x = got[row]
+        left = (x == 7.0).all(-1)                             # by heads
+        fits = left
+        for i in np.nonzero(rows == row)[0]:
+            rms = want[i].square().mean(-1, keepdim=True).sqrt()
+            fits = fits | (((x - want[i]).abs() / want[i].abs().maximum(rms)).amax(-1) <= TOL)
+        assert bool(fits.all()), (row, rows[rows == row].size, x.abs().max().item())
+        served[row] = int((~left).any())
+    assert served[np.setdiff1d(np.arange(len(got)), rows)].sum() == 0
+    say(f"        {served.sum()} of {len(set(rows.tolist()))} rows served")
