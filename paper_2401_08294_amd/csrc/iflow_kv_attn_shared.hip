@@ -44,10 +44,10 @@ struct KvSharedPlan {
         const int64_t behind = std::max<int64_t>(1, v.max_seq - max_shared);
         tail.direct = head_dim == 64 || tail.lines <= 256 ? 8 : 4;
         if (tail.lines * ((v.max_seq + KV_TILE - 1) / KV_TILE) <= (1LL << 30) && behind > (tail.lines >= 256 ? 2560 : head_dim == 64 ? 1024 : 768)) tail.direct = 0;
-        // (of the sequences beside big ones one token each is expected)
+        // (of the sequences beside big ones one token each is expected; where that is the most, and `few` rows, nobody is left to share)
         const int64_t lines = big ? seqs * kv * pieces(group) : tail.lines, together = big ? (seqs * group + ROWS - 1) / ROWS : blocks;
         const int64_t saved = (10 * lines - 13 * together * kv) * tiles * (head_dim + 64) / (10 * 192);
-        alone = seqs < 2 || all > (1 << 21) || v.n_tokens * n_heads > (1 << 22) || tiles < 2 * PART || saved < (tail.direct ? LEAST : LEAST_CUT);
+        alone = seqs < 2 || (big && most == group) || all > (1 << 21) || v.n_tokens * n_heads > (1 << 22) || tiles < 2 * PART || saved < (tail.direct ? LEAST : LEAST_CUT);
     }
     size_t prefix_bytes(int64_t n_rows, int head_dim) const { return ((size_t)parts * n_rows * (head_dim + 2) * 4 + 32 + 15) / 16 * 16; }      // (the values behind the others, 16-byte aligned)
     static size_t served_bytes(int64_t n_tokens) { return (n_tokens * sizeof(KvServed) + 15) / 16 * 16; }

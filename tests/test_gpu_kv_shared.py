@@ -448,3 +448,12 @@ def test_rows_that_two_sequences_claim(gpu, name, n_heads, n_kv, d, own, big, en
         served[row] = int((~left).any())
     assert served[np.setdiff1d(np.arange(len(got)), rows)].sum() == 0
     say(f"        {served.sum()} of {len(set(rows.tolist()))} rows served")
+
+
+@pytest.mark.parametrize("n_heads,n_kv,n,counts", [(512, 4, 64, None), (512, 4, 64, 1), (256, 2, 90, 3)])
+def test_tokens_that_fill_blocks_by_themselves(gpu, n_heads, n_kv, n, counts):  # noqa: F811
+    """128 query heads to a key/value head: every sequence goes by blocks of its own, one token each as in causal attention."""
+    own = [x for x in OWN * 6 if x >= 3][:n]
+    s = Shared(gpu, "Q4_B64", n_heads, n_kv, 64, 64, [1024 + x for x in own], counts and [1 + i % counts for i in range(n)], 1024, 9500)
+    assert s.shares() == (counts == 3)
+    s.check()

@@ -82,3 +82,11 @@ def test_a_prefix_is_whole_pages(iflow, page, most, n_seqs, n_heads):  # noqa: F
         assert room == iflow.kv_attn_workspace_bytes(*of, n_heads)
         # (every check but that of the output's place is passed without pages: no launch)
         assert iflow.lib().iflow_kv_attn_shared(*of, None, 6 * AT, most, 2 * AT, n_heads, 0.1, 2 * AT + 16, 64 * AT, room, None) == iflow.ERR_SHAPE
+
+
+@pytest.mark.parametrize("first", [None, AT])
+@pytest.mark.parametrize("n_heads,n_kv,n_seqs", [(512, 4, 64), (256, 2, 200), (128, 1, 300), (130, 1, 700)])
+def test_tokens_that_fill_blocks_by_themselves(iflow, n_heads, n_kv, n_seqs, first):  # noqa: F811
+    """With 128 query heads and more per key/value head every token of a larger batch goes by blocks of its own: nobody is left to share, and a step of one token each is causal attention."""
+    of = described(iflow, cache=dict(n_kv_heads=n_kv, n_pages=1 << 20), n_seqs=n_seqs, n_tokens=n_seqs, max_tokens=1, first_token=first, max_pages=128, max_seq=8192)
+    assert iflow.kv_attn_shared_workspace_bytes(*of, n_heads, 4096) == iflow.kv_attn_workspace_bytes(*of, n_heads)
