@@ -25,12 +25,14 @@ struct KvSharedPlan {
     int big;                                                  // rows of a block of a sequence of `few` rows and more (0: there are none)
     int parts, per;                                           // of the prefix's positions, tiles of one
     int64_t blocks;                                           // of the prefix's rows, at most
+    int64_t sharing;                                          // tokens that share, at most: with big sequences beside them, those of fewer rows than `few`
     KvPlan tail;                                              // of what lies behind the prefix
     KvSharedPlan(const KvView &v, int head_dim, int n_heads, int max_shared) : tail(v, head_dim, n_heads, v.max_seq)
     {
         const int64_t group = n_heads / v.n_kv_heads, most = v.max_tokens * group, all = v.n_tokens * group, seqs = v.n_seqs, kv = v.n_kv_heads, tiles = max_shared / KV_TILE;
         auto pieces = [](int64_t n) { return (n + KVA_ROWS - 1) / KVA_ROWS; };
         big = most < KVA_FEW || kv * (all / 64) < 256 ? 0 : kv * (all / 128) >= 512 ? 128 : 64;
+        sharing = big ? std::min(v.n_tokens, seqs * ((KVA_FEW - 1) / group)) : v.n_tokens;
         blocks = ((big ? std::min(all, seqs * (KVA_FEW - 1)) : all) + ROWS - 1) / ROWS;
         parts = (int)std::max<int64_t>(1, std::min<int64_t>(KVA_CUS / (blocks * kv), (tiles + PART - 1) / PART));
         per = (int)(((tiles + parts - 1) / parts + 1) / 2 * 2);
@@ -72,7 +74,7 @@ size_t kv_attn_shared_workspace_bytes(const KvView &v, int head_dim, int n_heads
     const int max_shared = kv_whole_pages(v, most);
     const KvSharedPlan plan(kv_rows_bound(v), head_dim, n_heads, max_shared);
     if (plan.alone) return kv_attn_workspace_bytes(v, head_dim, n_heads);
-    return plan.prefix_bytes(v.n_tokens * n_heads, head_dim) + plan.served_bytes(v.n_tokens) + (plan.tail.direct ? 0 : KvPartial::bytes(v.n_seqs, head_dim));
+    return plan.prefix_bytes(plan.sharing * n_heads, head_dim) + plan.served_bytes(v.n_tokens) + (plan.tail.direct ? 0 : KvPartial::bytes(v.n_seqs, head_dim));
 }
 
 hipError_t launch_kv_attn_shared(int format, int head_dim, const KvView &batch, const int32_t *pages, const int32_t *len, int most, const uint16_t *q, int n_heads, float scale, uint16_t *out,
@@ -85,7 +87,7 @@ hipError_t launch_kv_attn_shared(int format, int head_dim, const KvView &batch, 
     const int group = n_heads / v.n_kv_heads;
     const float scale_log2e = scale * 1.4426950408889634f;
     const KvDivide by_group(group);
-    const int64_t n_rows = v.n_tokens * n_heads;
+    const int64_t n_rows = plan.sharing * n_heads;
     float *const m = static_cast<float *>(workspace), *const l = m + plan.parts * n_rows, *const o = m + (2 * plan.parts * n_rows + 3) / 4 * 4;
     uint8_t *const behind = static_cast<uint8_t *>(workspace) + plan.prefix_bytes(n_rows, head_dim);
     const KvShared shared = {pages, len, m, l, o, reinterpret_cast<KvServed *>(behind), n_rows, max_shared, plan.parts};

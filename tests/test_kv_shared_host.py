@@ -90,3 +90,13 @@ def test_tokens_that_fill_blocks_by_themselves(iflow, n_heads, n_kv, n_seqs, fir
     """With 128 query heads and more per key/value head every token of a larger batch goes by blocks of its own: nobody is left to share, and a step of one token each is causal attention."""
     of = described(iflow, cache=dict(n_kv_heads=n_kv, n_pages=1 << 20), n_seqs=n_seqs, n_tokens=n_seqs, max_tokens=1, first_token=first, max_pages=128, max_seq=8192)
     assert iflow.kv_attn_shared_workspace_bytes(*of, n_heads, 4096) == iflow.kv_attn_workspace_bytes(*of, n_heads)
+
+
+@pytest.mark.parametrize("n_heads,n_kv,n_seqs,tokens,most,shared", [(64, 1, 8, 32768, 4096, 32000), (71, 1, 16, 16384, 4096, 32000), (64, 8, 130, 60000, 2000, 4096), (32, 8, 1000, 100000, 512, 1024), (64, 64, 120, 16000, 300, 2048)])
+def test_workspace_of_chunks_beside_single_tokens(iflow, n_heads, n_kv, n_seqs, tokens, most, shared):  # noqa: F811
+    """Sequences of 128 rows and more leave nothing in the workspace: it holds a part's sums of at most 127 rows of the others each, in as many parts as fill the device once, and 8 bytes a token."""
+    of = described(iflow, cache=dict(n_kv_heads=n_kv, n_pages=1 << 20), n_seqs=n_seqs, n_tokens=tokens, max_tokens=most, max_pages=1 << 14, max_seq=1 << 20)
+    rows = min(tokens, n_seqs * (127 // (n_heads // n_kv))) * n_heads
+    room = iflow.kv_attn_shared_workspace_bytes(*of, n_heads, shared)
+    cut = iflow.kv_attn_workspace_bytes(*described(iflow, cache=dict(n_kv_heads=n_kv, n_pages=1 << 20), n_seqs=n_seqs, n_tokens=n_seqs, max_tokens=1, max_pages=1 << 14, max_seq=1 << 20), n_heads)
+    assert room <= max(256 * 64, rows) * 130 * 4 + 8 * tokens + cut + 64
