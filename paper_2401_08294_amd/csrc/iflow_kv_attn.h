@@ -659,6 +659,7 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
     constexpr int KEYS = STEP * D * 2, GROUP = 2 * STAGES * KEYS;      // bytes of a step's keys (its values are as many), of what a group of wavefronts stages
     constexpr int ROWS = 32 * RG;
     static_assert(SPLIT ? 2 * UNITS == RG : UNITS % RG == 0, "the wavefronts share the decoding evenly");
+    static_assert(!SEES::PREFIX || PG > 1, "a prefix's sums are written where the groups of wavefronts meet");
     constexpr int MERGE = (PG > 1 ? PG * ROWS * (D + 4) * 4 : 0), LDS = GROUP * PG > MERGE ? GROUP * PG : MERGE;
     __shared__ __align__(16) uint8_t s_mem[LDS];
     __shared__ float s_m[PG][ROWS], s_l[PG][ROWS];
@@ -1070,16 +1071,7 @@ __global__ __launch_bounds__(64 * RG * PG, RG * PG == 4 ? 2 : 1) void kv_attn_ro
 
     // element 4 y + e of oacc[c] is component 32 c + 8 y + 4 hf + e of row li
     l += __shfl_xor(l, 32);
-    if constexpr (PG == 1 && SEES::PREFIX) {
-        if (!real) return;
-        const int64_t to = b * sees.rows + my_out / D;
-        if (hf == 0) { sees.m[to] = m; sees.l[to] = l; }
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int y = 0; y < 4; ++y)
-                *reinterpret_cast<kv_float4 *>(sees.o + to * D + 32 * c + 8 * y + 4 * hf) = (kv_float4){oacc[c][4 * y], oacc[c][4 * y + 1], oacc[c][4 * y + 2], oacc[c][4 * y + 3]};
-    } else if constexpr (PG == 1) {
+    if constexpr (PG == 1) {
         if (!real) return;
         const float f = l > 0.f ? 1.f / l : 0.f;              // (nothing seen: zeros; 64 divisions would take as long as two steps)
 #pragma unroll
