@@ -1212,8 +1212,10 @@ hipError_t kv_attn_by_sixteens(int format, int head_dim, const KvView &v, const 
     const int64_t part = std::max<int64_t>(2 * KVA_SPLIT_WAVES, plan.lines * tiles / (v.n_seqs > 1 ? 2 : 1) / (4 * KVA_CUS));
     const int groups = (int)((tiles / part + 2 + KVA_MERGE - 1) / KVA_MERGE);
     // Packed, a workgroup merges one token after another: where all are by sixteens there are as many workgroups as tokens, up to what the device holds (225 tokens of one sequence and one each of two others, 4/1 heads
-    // of 128, 2785 positions: 77 us with two for each sequence, 18 so).
-    const int64_t at_once = std::max<int64_t>(2 * (int64_t)v.n_seqs, plan.few ? 0 : 8192 / n_heads);
+    // of 128, 2785 positions: 76 us with two for each sequence, 17 so).  More are hardly faster, and those without a token cost a call that has fewer than it describes (us, two for each sequence / up to 2048 /
+    // up to 8192 in all, 500 rows of eight sequences of 4000 positions, 32/8 heads of 128, with 8 tokens, 184, 496: 17.8 / 19.6 / 21.1, 70 / 61 / 58, 109 / 105 / 99; 1900 rows, 8/8 heads, with 8, 534, 1896: 16.4 / 18.4 /
+    // 18.8, 85 / 48 / 47, 152 / 95 / 94; 500 rows of forty, 64 components, with 40, 84, 480: 28.1 / 27.8 / 30.0, 37.2 / 37.1 / 37.7, 73 / 73 / 71).
+    const int64_t at_once = std::max<int64_t>(2 * (int64_t)v.n_seqs, plan.few ? 0 : 2048 / n_heads);
     const dim3 tokens = plan.packed ? dim3((unsigned)std::min(v.n_tokens, at_once), (unsigned)n_heads) : dim3((unsigned)n_heads, (unsigned)v.max_tokens, (unsigned)v.n_seqs);
     hipLaunchKernelGGL(kv_attn_merge_kernel<SEES>, tokens, dim3((unsigned)head_dim, (unsigned)(groups > 8 ? 8 : groups)), 0, s, v, n_heads, group, few, workspace, out, sees);
     return hipGetLastError();
