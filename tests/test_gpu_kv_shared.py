@@ -457,3 +457,32 @@ def test_tokens_that_fill_blocks_by_themselves(gpu, n_heads, n_kv, n, counts):  
     s = Shared(gpu, "Q4_B64", n_heads, n_kv, 64, 64, [1024 + x for x in own], counts and [1 + i % counts for i in range(n)], 1024, 9500)
     assert s.shares() == (counts == 3)
     s.check()
+
+
+class Exact(Shared):
+    """Keys of which one block is 64 everywhere and one is whole numbers 0 .. 255, which a block of 8 bits holds as they are.  (The base is so large that their components are not turned.)"""
+
+    def append(self, table, lens, counts):
+        batch, _, n = self.batch_of(table, lens, counts)
+        q, k = [self.normal((n, h, self.d)) for h in (self.n_heads, self.n_kv)]
+        k[..., 32:64] = self.torch.randint(0, 256, (n, self.n_kv, 32), device="cuda", generator=self.g).half()
+        k[..., 32], k[..., 33], k[..., 96:] = 0.0, 255.0, 64.0
+        self.iflow.kv_append(self.cache, batch, q, k, self.normal((n, self.n_kv, self.d)), self.n_heads, 2.9e38, 1, q)
+        self.torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("own,counts", [(200, None), (200, 3), (2500, None)])
+def test_references_around_2_to_the_20(gpu, own, counts):  # noqa: F811
+    """Scores of 0, 2^20 and 3 2^19, and up to 32 more or less in steps of an eighth, which 32 bits hold exactly: the prefix's reference and the others' are either side of where scores are rounded before they
+    are compared, the largest is in the prefix for some rows and behind it for others.  No error but the output's own rounding: the tolerance is the one of small scores.  (scale log2 e is 1 in 32 bits, and
+    within 2^-23 of it in 64: of differences of 64, 8e-6, inside the 2^-15.)"""
+    scale = float(np.float32(np.log(2.0)))
+    assert np.float32(scale) * np.float32(1.4426950408889634) == np.float32(1.0)
+    lens = [1024 + (37 * i) % own for i in range(63)] + [1024 + own]
+    s = Exact(gpu, "Q8_B32", 24, 8, 128, 64, lens, counts and [min(counts, n - 1000) for n in lens], 1024, 9600 + own)
+    assert s.shares()
+    q = s.torch.zeros((s.n_tokens, 24, 128), dtype=s.torch.float16, device="cuda")
+    for h in range(24):
+        q[:, h, 96] = (0.0, 16384.0, 24576.0)[h % 3]
+        q[s.torch.arange(s.n_tokens), h, 34 + (s.torch.arange(s.n_tokens) * 7 + h) % 30] = 0.125 if h % 2 else -0.125
+    s.compare(s.attend(q, scale), s.reference(q, scale))
