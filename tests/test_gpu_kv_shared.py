@@ -486,3 +486,15 @@ def test_references_around_2_to_the_20(gpu, own, counts):  # noqa: F811
         q[:, h, 96] = (0.0, 16384.0, 24576.0)[h % 3]
         q[s.torch.arange(s.n_tokens), h, 34 + (s.torch.arange(s.n_tokens) * 7 + h) % 30] = 0.125 if h % 2 else -0.125
     s.compare(s.attend(q, scale), s.reference(q, scale))
+
+
+@pytest.mark.parametrize("name,n_heads,n_kv,d,big,n,shared", [("Q4_B64", 32, 8, 128, [300, 256, 290], 90, 1024), ("Q8_B32", 64, 8, 64, [200, 16, 400], 70, 2048)])
+def test_chunks_beside_single_tokens_of_long_sequences(gpu, name, n_heads, n_kv, d, big, n, shared):  # noqa: F811
+    """What lies behind the prefix is cut and merged for the sequences of few rows, some of a few tokens; those of many rows go by blocks of their own."""
+    counts = [1 + (i % 4 == 3) * (i % 5) for i in range(n)]
+    for i, c in enumerate(big):
+        counts.insert((i * n) // len(big) + 3, c)
+    lens = [shared + c + (2700 if i % 3 == 0 else (53 * i) % 2700) for i, c in enumerate(counts)]
+    s = Shared(gpu, name, n_heads, n_kv, d, 64, lens, counts, shared, 9700 + n_heads)
+    assert s.shares() and s.room() > s.iflow.kv_attn_workspace_bytes(s.cache, s.batch, n_heads) > 1 << 20
+    s.check()
