@@ -378,7 +378,9 @@ iflow_status_t iflow_kv_attn_window(const iflow_kv_cache_t *cache, const iflow_k
                                     void *workspace, size_t workspace_bytes, void *stream);
 
 /* iflow_kv_attn for a batch whose sequences begin with the same positions (an instruction, a document), in the same pages: these are read once for the tokens of all sequences, not once for each.
- *   shared_pages [max_shared / page_positions], device int32: the prefix's pages.  shared_len, device int32: how many positions it has, read when the kernels run, at most max_shared; only whole pages
+ * (Sequences of 128 rows and more in the call - tokens times query heads of a key/value head - fill the matrix instructions by themselves and read the prefix as in iflow_kv_attn; so does every sequence
+ * where sharing would save less than its second launch costs.)
+ *   shared_pages [max_shared / page_positions], device int32: the prefix's pages (null where that is 0).  shared_len, device int32: how many positions it has, read when the kernels run, at most max_shared; only whole pages
  *   count, what is left over of a page is read as every sequence's own.  0 <= max_shared <= max_seq.
  * All its positions have been written (a token inside the prefix weighs what lies behind it with zeros).  Every sequence that has tokens in the call has these pages in its row of page_table (which
  * must not be null), entries 0 .. shared_len / page_positions - 1: where a row has others it is unspecified which of the two a token sees.  (iflow_kv_tables writes such rows.)  A token at a position
@@ -398,7 +400,9 @@ iflow_status_t iflow_kv_attn_shared(const iflow_kv_cache_t *cache, const iflow_k
  *   sequences and of a sequence's positions, and given back behind its end in the same order: what is given back can be taken from the next call on.  free_state_out = {first, how many, how many
  *   pages were wanted and not there}.  Where none is left the entry becomes -1, the page that is not there, and is wanted again in the next call.
  *   The entries of a sequence's shared pages are written where it has positions; those of pages that it had or gives back stay as they were.
- *   slots (may be null) [n_tokens]: where a token's position lies, page * P + position mod P, or -1 without a position or page.  Rows of no token are left as they were.
+ *   (Only a sequence's last pages are given back: those that a sliding window has left behind are its own until it ends.)
+ *   slots (may be null) [n_tokens]: where a token's position lies, page * P + position mod P, or -1 without a position or page.  Rows of no token are left as they were.  (For programs that
+ *   write other arrays by position, beside the cache: iflow_kv_append goes by page_table.)
  * new_tokens is taken as 0 .. max_tokens, a length as at most max_seq.  first_token null: one token each, row b, and new_tokens is not read.
  * All arrays are device arrays, int32 and 4-byte aligned but for slots (int64, 8).  held_out may be held, and free_state_out free_state; nothing else that is written may overlap anything
  * (IFLOW_ERR_SHAPE).  n_seqs * max_pages <= 2^30.  Whatever the arrays hold, what is read and written lies inside them; a ring of fewer entries than are given back loses the rest.

@@ -1,6 +1,6 @@
 // Attention over the quantized key/value cache with a sliding window and a few first positions that stay visible: the kernels of iflow_kv_attn.h over the tiles that a workgroup's tokens see, the first
 // ones and those from the first token's window on, as one list; what of a tile a row does not see is hidden where its scores are made.
-// 32 sequences' next tokens, window 1024, 32/8 heads x 128, 4 bits: 11.0 us, 3.5 TB/s of codes; three prompts of up to 4001 tokens, window 512, 64/8 heads: 209 to 228, 0.5 PFLOP/s (vector issue and matrix cores in turn).
+// 32 sequences' next tokens, window 1024, 32/8 heads x 128, 4 bits: 11.0 us, 3.5 TB/s of codes; three prompts of up to 4001 tokens, window 512, 64/8 heads: 228, 0.5 PFLOP/s (vector issue and matrix cores in turn).
 #include "iflow_kv_attn.h"
 
 namespace iflow {

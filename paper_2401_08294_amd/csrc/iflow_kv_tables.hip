@@ -6,7 +6,7 @@
 // was) or one that it takes (in the ring).
 // The work is launches and latencies.  Up to 1024 sequences every workgroup adds up all of them for itself, in LDS, and the rest is shared among the wavefronts of all; more
 // sequences, and a larger batch whose state is updated in place (its workgroups would read what one of them has written), take launches of their own for the sums.
-// 64 sequences' next tokens 3.5 us, a mixed step of 256 sequences and 30 thousand tokens 4.3, a third of a million tokens of 1000 sequences 5.8 (graph replay): lengths -> sums -> search -> page -> slot, one after another.
+// 64 sequences' next tokens 3.5 us, a mixed step of 256 sequences and 30 thousand tokens 4.3 (in place 6.3), a third of a million tokens of 1000 sequences 5.8 (7.9) (graph replay): lengths -> sums -> search -> page -> slot, one after another.
 #include <algorithm>
 
 #include "iflow_kv.h"
